@@ -1,0 +1,567 @@
+"""The calls of the paged 4-bit cache: planning its pages, writing it, reading it back, attending over it and selecting
+from its scores, from one token of a small batch to a layer at 128K.
+
+The cache holds tokens in pages.  A page holds `page` tokens (a power of two, 16 to 256) of every KV head, head after head,
+in tiles of 16 tokens; a tile is 16 rows of 128 bytes (the key's 128 values and the value's 128, 4 bits each, even
+dimension in the low half of a byte) and 8 x 16 scale bytes (four groups of 32 dimensions of the key, four of the value;
+16 tokens): 2176 bytes.  A 4-bit value is a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6; it counts times 2^(scale byte - 127),
+a scale byte of 255 makes its group NaN.  Writing rounds x / 2^e to the nearest of these, ties to the even code, with e the
+smallest integer with max |x| <= 6 * 2^e in the group, within [-125, 125].  A slot is page * `page` + place in the page.
+
+A case is a dict of sizes:
+  op        "plan"    a serving step's bookkeeping: finished requests give their pages back, the others get pages for their
+                      new tokens, every new token gets its slot
+            "append"  the step's new keys and values are written, and read back as rows
+            "read"    whole sequences leave the cache as bf16 rows (for the calls that work on those)
+            "attn"    one layer's decode attention: retrieval heads over the whole sequence, sparse heads over a set
+            "select"  the k best positions of every row of scores
+  batch, q_heads, kv_heads, page, k     (k: entries of an index set)
+  len_lo, len_hi   tokens the requests hold are spread over this range
+  new_lo, new_hi   "plan", "append": every `chunked`-th request gets a number of tokens out of this range (a piece of a
+                   prompt), the others one
+  done             "plan": requests that have finished
+  retrieval        "attn", "select": retrieval heads; `scores`: their pooled scores are written too ("attn")
+  planted          query-aligned key rows per KV head ("attn"), high scores ("select")
+
+Head types, lengths and token counts belong to the case; values, pages and sets come from the seed.
+"""
+from __future__ import annotations
+
+import math
+import random
+
+import numpy as np
+import torch
+
+own = False
+
+D = 128
+TILE = 16
+TILE_BYTES = 16 * 128 + 8 * 16
+ROW_BYTES = 136
+DEV = "cuda"
+
+
+def _case(name=None, **kw):
+    c = dict(op="attn", batch=1, q_heads=32, kv_heads=8, page=64, k=1, len_lo=0, len_hi=0, new_lo=1, new_hi=1, chunked=1,
+             done=0, retrieval=32, scores=False, planted=0)
+    c.update(kw)
+    c["len_lo"] = c["len_lo"] if "len_lo" in kw else c["len_hi"]
+    if name is not None:
+        c["name"] = name
+    return c
+
+
+def listed():
+    return [
+        # a small decode batch's bookkeeping: sixteen conversations, a token each
+        _case("plan_b16_decode", op="plan", batch=16, len_lo=61, len_hi=8191, done=1),
+        # a full serving step: 256 requests, every sixteenth a piece of a prompt, some finished
+        _case("plan_b256_mixed", op="plan", batch=256, page=16, len_lo=0, len_hi=16384, new_lo=512, new_hi=4099, chunked=16,
+              done=9),
+        # the decoded tokens of a batch of 16, a small model's two KV heads
+        _case("append_b16_decode", op="append", batch=16, q_heads=8, kv_heads=2, len_lo=61, len_hi=3001),
+        # prompts of up to 33K written at once
+        _case("append_prompts_33k", op="append", batch=4, len_lo=0, len_hi=1000, new_lo=2049, new_hi=33333),
+        # a short conversation handed to the calls that read bf16 rows
+        _case("read_4k", op="read", q_heads=8, kv_heads=2, len_hi=4099),
+        # a batch of long ones, in large pages
+        _case("read_b8_16k_96k", op="read", batch=8, page=256, len_lo=16411, len_hi=98304),
+        # the smallest layer: a small model at 4K, every head dense
+        _case("attn_4k", q_heads=8, kv_heads=2, len_hi=4096, retrieval=8, planted=32),
+        # a serving batch of many short sequences, eight query heads a KV head, small pages
+        _case("attn_b64_short", batch=64, q_heads=64, page=16, len_lo=61, len_hi=3001, retrieval=64, planted=24),
+        # a batch of long conversations of unequal lengths: four retrieval heads with their scores, the others sparse
+        _case("attn_b8_16k_96k_hybrid", batch=8, len_lo=16411, len_hi=98304, k=2048, retrieval=4, scores=True, planted=256),
+        # a layer that keeps every head dense at 128K
+        _case("attn_128k", len_hi=131072, planted=1024),
+        # the sets of one sequence's layer: four retrieval heads at 32K
+        _case("select_32k", op="select", len_hi=32768, k=2048, retrieval=4, planted=512),
+        # the sets of a batch of long sequences, every KV head selecting
+        _case("select_b8_16k_96k", op="select", batch=8, len_lo=16411, len_hi=98304, k=4096, retrieval=32, planted=1024),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    """One more case of the same ranges: any of the calls, 1 to 256 requests of 1 to 128K tokens, 1 to 16 KV heads, groups
+    of 1 to 16 query heads, pages of 16 to 256 tokens, sets of 16 to 8192; sizes mostly odd."""
+    op = rng.choice(["plan", "append", "read", "attn", "attn", "attn", "select", "select"])
+    kv = rng.choice([1, 2, 3, 4, 8, 8, 8, 16])
+    group = rng.choice([1, 2, 4, 4, 4, 5, 8, 16])
+    page = rng.choice([16, 32, 64, 64, 128, 256])
+    c = dict(op=op, q_heads=kv * group, kv_heads=kv, page=page)
+    if op == "plan":
+        batch = _log(rng, 1, 256)
+        c.update(batch=batch, len_hi=_log(rng, 16, 16384), new_lo=1, new_hi=rng.choice([1, _log(rng, 16, 4096)]),
+                 chunked=rng.choice([1, 4, 16]) if batch <= 16 else 16, done=rng.randint(0, max(0, batch // 8)))
+        c["len_lo"] = int(c["len_hi"] * rng.uniform(0.0, 0.9))
+    elif op == "append":
+        batch = _log(rng, 1, 64)
+        c.update(batch=batch, len_hi=_log(rng, 16, 4096), new_hi=rng.choice([1, _log(rng, 16, max(17, 500000 // (batch * kv)))]))
+        c["new_hi"] = min(c["new_hi"], 32768)
+        c["new_lo"] = max(1, int(c["new_hi"] * rng.uniform(0.1, 0.9)))
+        c["len_lo"] = int(c["len_hi"] * rng.uniform(0.0, 0.9))
+    else:
+        batch = rng.choice([1, 1, 1, 2, 3, 8, 17, 64, 200])
+        most = max(64, min(131072, 3_000_000 // (batch * kv)))
+        hi = _log(rng, 64, most)
+        c.update(batch=batch, len_hi=hi, len_lo=hi if batch == 1 else max(1, int(hi * rng.uniform(0.02, 0.9))))
+        c["planted"] = min(1024, c["len_lo"] // 32)
+        if op != "read":
+            c["k"] = _log(rng, 16, max(17, min(8192, hi // 2 if op == "select" else 8192)))
+        c["retrieval"] = c["q_heads"]
+        if op == "select" or (op == "attn" and rng.random() < 0.6):
+            c["retrieval"] = rng.randint(1, c["q_heads"])
+        c["scores"] = op == "attn" and rng.random() < 0.5
+    return _case(**c)
+
+
+# ------------------------------------------------------------------ what belongs to the case
+
+
+def _spread(lo, hi, n, key):
+    v = [hi if n == 1 else lo + (hi - lo) * i // (n - 1) for i in range(n)]
+    random.Random(key).shuffle(v)
+    return v
+
+
+def _lengths(c):
+    return _spread(c["len_lo"], c["len_hi"], c["batch"], 7)
+
+
+def _done(c):
+    at = set(random.Random(5).sample(range(c["batch"]), c["done"]))
+    return [int(b in at) for b in range(c["batch"])]
+
+
+def _new(c):
+    big = _spread(c["new_lo"], c["new_hi"], -(-c["batch"] // c["chunked"]), 3)
+    return [0 if gone else big[b // c["chunked"]] if b % c["chunked"] == 0 else 1 for b, gone in enumerate(_done(c))]
+
+
+def _mask(c):
+    m = np.zeros(c["q_heads"], np.uint8)
+    m[random.Random(11).sample(range(c["q_heads"]), min(c["retrieval"], c["q_heads"]))] = 1
+    return m
+
+
+def _ceil(a, b):
+    return -(-a // b)
+
+
+def _max_pages(c):
+    """Width of the block table: the longest request, and a little room."""
+    most = max(_lengths(c)) + (c["new_hi"] if c["op"] in ("plan", "append") else 0)
+    return _ceil(max(1, most), c["page"]) + 1
+
+
+def work(case):
+    c = case
+    lens, new, B, H = _lengths(c), _new(c), c["batch"], c["kv_heads"]
+    if c["op"] == "plan":
+        pages = sum(_ceil(l + n, c["page"]) - _ceil(l, c["page"]) for l, n in zip(lens, new))
+        back = sum(_ceil(l, c["page"]) for l, d in zip(lens, _done(c)) if d)
+        return {"bytes": 4 * (5 * B + 2 * pages + 2 * back + sum(new)), "flops": 0}
+    if c["op"] == "append":
+        n = sum(new)
+        return {"bytes": n * H * 2 * (4 * D + ROW_BYTES) + 4 * n, "flops": 0}
+    if c["op"] == "read":
+        return {"bytes": sum(lens) * H * (4 * D + ROW_BYTES), "flops": 0}
+    m = _mask(c).reshape(H, -1)
+    if c["op"] == "select":
+        rows = int(m.any(1).sum())
+        return {"bytes": 4 * (rows * sum(lens) + (2 * H - rows) * B * c["k"]), "flops": 0}
+    rows = pairs = scores = sets = 0
+    for length in lens:
+        n = min(c["k"], length)
+        rows += int(m.any(1).sum()) * length + int((m == 0).any(1).sum()) * n
+        sets += int((m == 0).any(1).sum()) * n
+        scores += int(m.any(1).sum()) * length if c["scores"] else 0
+        pairs += int(m.sum()) * length + int((m == 0).sum()) * n
+    return {"bytes": rows * ROW_BYTES + 4 * (sets + scores) + 2 * 2 * B * c["q_heads"] * D, "flops": pairs * 4 * D}
+
+
+# ------------------------------------------------------------------ the cache in plain operations
+
+
+def _encode(x):
+    """Codes (uint8) and scale bytes of bf16 values [..., 128]: groups of 32."""
+    v = x.float().unflatten(-1, (4, 32))
+    m, e = torch.frexp(v.abs().amax(-1))  # amax = m 2^e, m in [0.5, 1): amax <= 6 * 2^(e - 3) where m <= 0.75
+    e = torch.where(m == 0, -125, torch.where(m <= 0.75, e - 3, e - 2)).clamp(-125, 125)
+    a = torch.ldexp(v, -e.unsqueeze(-1))
+    b = a.abs()
+    code = ((b > 0.25).to(torch.uint8) + (b >= 0.75) + (b > 1.25) + (b >= 1.75) + (b > 2.5) + (b >= 3.5) + (b > 5)
+            + 8 * torch.signbit(a))
+    return code.to(torch.uint8).flatten(-2), (e + 127).to(torch.uint8)
+
+
+def _decode(codes, scales):
+    """Values in 32 bits of packed rows (uint8 [..., 64]) and their scale bytes [..., 4]."""
+    grid = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6, 0, -0.5, -1, -1.5, -2, -3, -4, -6], device=codes.device)
+    v = grid[torch.stack((codes & 15, codes >> 4), -1).flatten(-2).int()].unflatten(-1, (4, 32))
+    return (v * torch.exp2(scales.float() - 127).unsqueeze(-1)).flatten(-2)
+
+
+def _tile_of(c, pages, head):
+    """First tile of a head in pages."""
+    return (pages * c["kv_heads"] + head) * (c["page"] // TILE)
+
+
+def _write(c, cache, slots, k, v):
+    """Rows of tokens ([T, H, 128]) into the cache, in place."""
+    tiles = cache.view(-1, TILE_BYTES)
+    head = torch.arange(c["kv_heads"], device=DEV)
+    page, off = slots.long() // c["page"], slots.long() % c["page"]
+    tile = _tile_of(c, page.unsqueeze(1), head) + (off // TILE).unsqueeze(1)
+    row = (off % TILE).unsqueeze(1).expand_as(tile)
+    rows, scales = tiles[:, :2048].unflatten(1, (TILE, 2, 64)), tiles[:, 2048:].unflatten(1, (2, 4, TILE))
+    for i, x in enumerate((k, v)):
+        code, scale = _encode(x)
+        rows[tile, row, i] = code[..., 0::2] | (code[..., 1::2] << 4)
+        scales[:, i].transpose(1, 2)[tile, row] = scale
+
+
+def _rows(c, cache, table, length):
+    """K and V [B, H, length, 128] in 32 bits of the pages that a block table names (absent ones: page 0)."""
+    n, H, t = _ceil(length, c["page"]), c["kv_heads"], c["page"] // TILE
+    pages = table[:, :n].long().clamp(min=0)
+    tiles = cache.view(-1, H, t, TILE_BYTES)[pages].transpose(1, 2)  # [B, H, n, t, bytes]
+    rows = tiles[..., :2048].unflatten(-1, (TILE, 2, 64)).flatten(2, 4)[:, :, :length]
+    scales = tiles[..., 2048:].unflatten(-1, (2, 4, TILE)).permute(0, 1, 2, 3, 6, 4, 5).flatten(2, 4)[:, :, :length]
+    return _decode(rows[..., 0, :], scales[..., 0, :]), _decode(rows[..., 1, :], scales[..., 1, :])
+
+
+# ------------------------------------------------------------------ values
+
+
+def _pages(c, tokens, gen):
+    """A block table that holds so many tokens of every request, in pages of a shuffled pool, and the pool's size."""
+    held = [_ceil(n, c["page"]) for n in tokens]
+    table = torch.full((c["batch"], _max_pages(c)), -1, dtype=torch.int32, device=DEV)
+    mine = torch.arange(_max_pages(c), device=DEV) < torch.tensor(held, device=DEV).unsqueeze(1)
+    size = sum(held) + 8
+    table[mine] = torch.randperm(size, device=DEV, generator=gen)[:sum(held)].int()
+    return table, size
+
+
+def _filled(c, table, size, lens, q, gen):
+    """A cache of N(0, 1) tokens in those pages, with `planted` keys along the group's first query."""
+    H, n, cap = c["kv_heads"], table.shape[1], max(1, max(lens))
+    cache = torch.zeros(size, H * (c["page"] // TILE) * TILE_BYTES, dtype=torch.uint8, device=DEV)
+    for b, length in enumerate(lens):
+        k, v = (torch.randn((length, H, D), dtype=torch.bfloat16, device=DEV, generator=gen) for _ in range(2))
+        if c["planted"] and q is not None:
+            qh = q[b].view(H, -1, D)[:, 0].float()
+            at = torch.randperm(length, device=DEV, generator=gen)[:c["planted"]]
+            a = 3.0 * math.sqrt(D) - 1.2 * torch.arange(1, len(at) + 1, device=DEV).log()
+            k[at] = (k[at].float() + a.view(-1, 1, 1) * math.sqrt(D) * qh / qh.square().sum(-1, keepdim=True)).bfloat16()
+        t = torch.arange(length, device=DEV)
+        _write(c, cache, table[b, t // c["page"]] * c["page"] + t % c["page"], k, v)
+    return cache
+
+
+def _sets(c, lens, gen):
+    """Sets of distinct positions, ascending, -1 padded."""
+    out = torch.full((c["batch"], c["kv_heads"], c["k"]), -1, dtype=torch.int32, device=DEV)
+    for b, length in enumerate(lens):
+        n = min(c["k"], length)
+        u = torch.rand((c["kv_heads"], length), device=DEV, generator=gen)
+        out[b, :, :n] = u.topk(n).indices.sort().values.int()
+    return out
+
+
+def prepare(case, seed):
+    c = case
+    B, H, P = c["batch"], c["kv_heads"], c["page"]
+    gen = torch.Generator(DEV)
+    gen.manual_seed(seed)
+    lens = _lengths(c)
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device=DEV)  # noqa: E731
+    s = {"case": c, "lens": ints(lens), "mask": _mask(c)}
+    if c["op"] == "plan":
+        s["new"], s["done"] = ints(_new(c)), torch.tensor(_done(c), dtype=torch.uint8, device=DEV)
+        s["table"], used = _pages(c, lens, gen)
+        size = used + sum(_ceil(n, P) + 1 for n in _new(c))  # a pool that serves the step
+        s["free"] = torch.full((size,), -1, dtype=torch.int32, device=DEV)
+        left = torch.ones(size, dtype=torch.bool, device=DEV)
+        left[s["table"][s["table"] >= 0].long()] = False
+        left = left.nonzero().flatten()
+        s["free"][:len(left)] = left[torch.randperm(len(left), device=DEV, generator=gen)].int()
+        s["count"] = ints([len(left)])
+        s["slots"] = torch.zeros(sum(_new(c)) + 5, dtype=torch.int32, device=DEV)  # a batch's buffer, a little too long
+        s["out"] = {k: torch.zeros(n, dtype=torch.int32, device=DEV)
+                    for k, n in (("lens", B), ("count", 1), ("start", B + 1), ("status", 1), ("lens1", B), ("count1", 1))}
+        return s
+    if c["op"] == "append":
+        new = _new(c)
+        s["table"], size = _pages(c, [a + b for a, b in zip(lens, new)], gen)
+        s["last"] = s["lens"] + ints(new)
+        pos = [torch.arange(a, a + b, device=DEV) for a, b in zip(lens, new)]
+        s["slots"] = torch.cat([s["table"][b, p // P] * P + p % P for b, p in enumerate(pos)]).int()
+        s["cache"] = torch.zeros(size, H * (P // TILE) * TILE_BYTES, dtype=torch.uint8, device=DEV)
+        kv = torch.randn((sum(new), 2, H, D), dtype=torch.bfloat16, device=DEV, generator=gen)  # as a projection leaves them
+        kv[:, 0, :, 5] *= 8  # (keys have channels that stand out)
+        s["k"], s["v"] = kv[:, 0], kv[:, 1]
+        s["rows"] = torch.zeros((2, B, H, max(new), D), dtype=torch.bfloat16, device=DEV)
+        return s
+    if c["op"] == "select":
+        cap = _max_pages(c) * P
+        x = torch.randn((B, H, cap), device=DEV, generator=gen)
+        if c["planted"]:
+            at = torch.randint(0, max(lens), (B, H, c["planted"]), device=DEV, generator=gen)
+            x.scatter_(2, at, 34.0 - 1.2 * torch.arange(1, c["planted"] + 1, device=DEV).log().expand_as(at))
+        # the same key again and again scores the same: every eighth position repeats one before it
+        t = torch.arange(cap, device=DEV)
+        s["scores"] = torch.where(t % 8 == 7, x[:, :, t // 2], x).contiguous()
+        s["sets"] = _sets(c, lens, gen)
+        s["idx"] = torch.zeros_like(s["sets"])
+        return s
+    s["q"] = torch.randn((B, c["q_heads"], D), dtype=torch.bfloat16, device=DEV, generator=gen)
+    s["table"], size = _pages(c, lens, gen)
+    s["cache"] = _filled(c, s["table"], size, lens, s["q"] if c["op"] == "attn" else None, gen)
+    if c["op"] == "read":
+        s["rows"] = torch.zeros((2, B, H, max(lens), D), dtype=torch.bfloat16, device=DEV)
+        return s
+    s["sets"] = _sets(c, lens, gen) if c["retrieval"] < c["q_heads"] else None
+    s["out"] = torch.zeros_like(s["q"])
+    s["scores"] = torch.zeros((B, H, _max_pages(c) * P), device=DEV) if c["scores"] else None
+    return s
+
+
+# ------------------------------------------------------------------ the plain forms
+
+
+def _plan(s, c):
+    P, lens, done, table = c["page"], s["lens"].long(), s["done"].bool(), s["table"].clone()
+    j = torch.arange(table.shape[1], device=DEV)
+    held = (lens + P - 1) // P
+    back = torch.where(done, held, 0)
+    at = s["count"] + (back.cumsum(0) - back).unsqueeze(1) + j
+    free = torch.cat((s["free"], s["free"][:1]))  # (the last place takes what is not given back)
+    free[torch.where(j < back.unsqueeze(1), at, len(free) - 1)] = table
+    free = free[:-1]
+    count = s["count"] + back.sum()
+    lens, held = torch.where(done, 0, lens), torch.where(done, 0, held)
+    after = lens + s["new"]
+    need = (after + P - 1) // P - held
+    first = (need.cumsum(0) - need).unsqueeze(1)
+    fresh = (j >= held.unsqueeze(1)) & (j < (held + need).unsqueeze(1))
+    table = torch.where(fresh, free[(count - 1 - first - (j - held.unsqueeze(1))).clamp(min=0)], table)
+    start = torch.cat((torch.zeros_like(lens[:1]), s["new"].long().cumsum(0)))
+    i = torch.arange(len(s["slots"]), device=DEV)
+    b = torch.searchsorted(start[1:], i, right=True).clamp(max=c["batch"] - 1)
+    pos = (lens[b] + i - start[b]).clamp(max=table.shape[1] * P - 1)
+    slots = torch.where(i < start[-1], table[b, pos // P] * P + pos % P, -1)
+    return {"lengths": after.int(), "free_pages": free, "free_count": (count - need.sum()).int(), "block_table": table,
+            "slots": slots.int(), "token_start": start.int(), "status": torch.zeros(1, dtype=torch.int32, device=DEV)}
+
+
+def _read(s, c, first, last):
+    """bf16 rows of the tokens [first, last) of every request; rows behind them stay zero."""
+    n = s["rows"].shape[3]
+    t = torch.arange(n, device=DEV)
+    pos = (first.unsqueeze(1) + t).clamp(max=s["table"].shape[1] * c["page"] - 1)  # [B, n]
+    page = s["table"].gather(1, pos.long() // c["page"]).clamp(min=0)
+    tile = _tile_of(c, page.unsqueeze(1), torch.arange(c["kv_heads"], device=DEV).view(1, -1, 1)) + (pos % c["page"] // TILE).unsqueeze(1)
+    row = (pos % TILE).unsqueeze(1).expand_as(tile)
+    tiles = s["cache"].view(-1, TILE_BYTES)
+    rows = tiles[:, :2048].unflatten(1, (TILE, 2, 64))[tile, row]  # [B, H, n, 2, 64]
+    scales = tiles[:, 2048:].unflatten(1, (2, 4, TILE)).permute(0, 3, 1, 2)[tile, row]
+    keep = (t < (last - first).unsqueeze(1)).view(-1, 1, n, 1)
+    for i in range(2):
+        s["rows"][i] = torch.where(keep, _decode(rows[..., i, :], scales[..., i, :]), 0.0).bfloat16()
+    return {"k": s["rows"][0], "v": s["rows"][1]}
+
+
+def _attend(s, c):
+    B, H, G, L = c["batch"], c["kv_heads"], c["q_heads"] // c["kv_heads"], max(_lengths(c))
+    k, v = _rows(c, s["cache"], s["table"], L)
+    z = torch.matmul(s["q"].view(B, H, G, D).float(), k.transpose(2, 3)) / math.sqrt(D)
+    inside = (torch.arange(L, device=DEV) < s["lens"].unsqueeze(1)).view(B, 1, 1, L)
+    mask = torch.from_numpy(s["mask"]).to(DEV).bool().view(1, H, G, 1)
+    seen = inside
+    if s["sets"] is not None:
+        mine = torch.zeros((B, H, L + 1), dtype=torch.bool, device=DEV)
+        mine.scatter_(2, torch.where(s["sets"] < 0, L, s["sets"]).long(), True)
+        seen = inside & (mask | mine[:, :, None, :L])
+    zm = torch.where(seen, z, -math.inf)
+    top = zm.amax(-1, keepdim=True)
+    p = (zm - torch.where(top == -math.inf, 0.0, top)).exp()
+    total = p.sum(-1, keepdim=True)
+    o = torch.matmul(p / torch.where(total == 0, 1.0, total), v)
+    got = {"out": o.reshape(B, H * G, D).bfloat16()}
+    if s["scores"] is not None:
+        n = mask.sum(2)
+        mean = torch.where(mask, z, 0.0).sum(2) / n.clamp(min=1)
+        got["scores"] = torch.zeros_like(s["scores"])
+        got["scores"][:, :, :L] = torch.where(inside[:, 0] & (n > 0), mean, 0.0)
+    return got
+
+
+def _select(s, c):
+    n, k = s["scores"].shape[2], c["k"]
+    lens = s["lens"].view(-1, 1, 1)
+    x = torch.where(torch.arange(n, device=DEV) < lens, s["scores"], -math.inf)
+    at = x.sort(dim=-1, descending=True, stable=True).indices[:, :, :k]
+    at = torch.nn.functional.pad(at, (0, k - at.shape[2]), value=n)
+    at = torch.where(torch.arange(k, device=DEV) < lens.clamp(max=k), at, n).sort(-1).values
+    new = torch.where(at < n, at, -1).int()
+    mask = torch.from_numpy(s["mask"].reshape(c["kv_heads"], -1).any(1)).to(DEV)
+    return {"idx": torch.where(mask.view(1, -1, 1), new, s["sets"])}
+
+
+def _plain(s):
+    c = s["case"]
+    if c["op"] == "plan":
+        return _plan(s, c)
+    if c["op"] == "append":
+        _write(c, s["cache"], s["slots"], s["k"], s["v"])
+        return _read(s, c, s["lens"], s["last"])
+    if c["op"] == "read":
+        return _read(s, c, torch.zeros_like(s["lens"]), s["lens"])
+    return _attend(s, c) if c["op"] == "attn" else _select(s, c)
+
+
+# ------------------------------------------------------------------ the framework's calls
+
+_context = []
+
+
+def _own(s):
+    from paper_2602_04541_amd import binding as lb
+    c = s["case"]
+    if not _context:
+        _context.append(lb.Context(0))
+    ctx = _context[0]
+    if "paged" not in s:  # what a program keeps beside its cache: the shape, and the workspace of its calls
+        size = s["cache"].shape[0] if "cache" in s else len(s["free"]) if "free" in s else 1
+        s["paged"] = lb.make_paged(c["batch"], c["q_heads"], c["kv_heads"], size, c["page"], _max_pages(c), c["k"])
+        if c["op"] in ("attn", "select"):
+            s["ws"] = lb.alloc_paged_workspace(s["paged"], DEV)
+    p = s["paged"]
+    if c["op"] == "plan":
+        o = s["out"]
+        ctx.release_pages(p, s["done"], s["lens"], s["table"], s["free"], s["count"], o["lens1"], o["count1"])
+        ctx.plan_pages(p, o["lens1"], s["new"], s["table"], s["free"], o["count1"], o["lens"], o["count"], s["slots"],
+                       o["start"], o["status"])
+        return {"lengths": o["lens"], "free_pages": s["free"], "free_count": o["count"], "block_table": s["table"],
+                "slots": s["slots"], "token_start": o["start"], "status": o["status"]}
+    if c["op"] == "append":
+        ctx.q4_append(p, s["k"], s["v"], s["slots"], s["cache"])
+        ctx.q4_read(p, s["cache"], s["table"], s["lens"], s["last"], s["rows"][0], s["rows"][1])
+        return {"k": s["rows"][0], "v": s["rows"][1]}
+    if c["op"] == "read":
+        ctx.q4_read(p, s["cache"], s["table"], None, s["lens"], s["rows"][0], s["rows"][1])
+        return {"k": s["rows"][0], "v": s["rows"][1]}
+    if c["op"] == "select":
+        ctx.select_scores(p, s["scores"], s["lens"], s["mask"], s["sets"], s["idx"], s["ws"])
+        return {"idx": s["idx"]}
+    ctx.q4_decode_attn(p, s["q"], s["cache"], s["table"], s["lens"], s["mask"], s["sets"], s["out"], s["scores"], s["ws"])
+    return {"out": s["out"]} if s["scores"] is None else {"out": s["out"], "scores": s["scores"]}
+
+
+def run(state):
+    return _own(state) if own else _plain(state)
+
+
+# ------------------------------------------------------------------ the same in 64 bits
+
+
+def _value(code, scale):
+    """What packed bytes [n, 64] under scale bytes [n, 4] stand for, in 64 bits."""
+    magnitude = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+    grid = torch.tensor(magnitude + tuple(-g for g in magnitude), dtype=torch.float64, device=DEV)
+    both = torch.empty((len(code), D), dtype=torch.float64, device=DEV)
+    both[:, 0::2], both[:, 1::2] = grid[(code % 16).long()], grid[(code // 16).long()]
+    return both * torch.pow(2.0, scale.double() - 127.0).repeat_interleave(32, dim=1)
+
+
+def _sequence(c, cache, table, h, n):
+    """K and V [n, 128] of one request's head, in 64 bits, page by page."""
+    tiles = cache.view(cache.shape[0], c["kv_heads"], -1, TILE_BYTES)[table[:_ceil(n, c["page"])].long(), h].reshape(-1, TILE_BYTES)
+    data, scale = tiles[:, :2048].reshape(-1, 128)[:n], tiles[:, 2048:].reshape(-1, 8, 16).permute(0, 2, 1).reshape(-1, 8)[:n]
+    return _value(data[:, :64], scale[:, :4]), _value(data[:, 64:], scale[:, 4:])
+
+
+def _nearest(x):
+    """x [n, 128] as the cache holds it, in 64 bits: the nearest of the eight magnitudes, of two equally near the even code."""
+    g = x.double().view(-1, 4, 32)
+    big = g.abs().amax(2)
+    e = torch.full_like(big, -125.0)
+    for _ in range(251):
+        e = torch.where((big > 6 * torch.pow(2.0, e)) & (e < 125), e + 1, e)
+    unit = g / torch.pow(2.0, e).unsqueeze(2)
+    best, far = torch.zeros_like(unit), unit.abs()
+    for code, m in enumerate((0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0), 1):
+        d = (unit.abs() - m).abs()
+        take = (d < far) | ((d == far) & (code % 2 == 0))
+        best, far = torch.where(take, m, best), torch.where(take, d, far)
+    return (best * unit.sign() * torch.pow(2.0, e).unsqueeze(2)).view(-1, D)
+
+
+def exact(case, seed):
+    c = case
+    s = prepare(c, seed)
+    B, H, P, G = c["batch"], c["kv_heads"], c["page"], c["q_heads"] // c["kv_heads"]
+    lens, new, mask = _lengths(c), _new(c), _mask(c)
+    if c["op"] == "plan":
+        table, free, left = s["table"].tolist(), s["free"].tolist(), int(s["count"])
+        for b in range(B):
+            if _done(c)[b]:
+                for j in range(_ceil(lens[b], P)):
+                    free[left] = table[b][j]
+                    left += 1
+                lens[b] = 0
+        slots, start = [], [0]
+        for b in range(B):
+            for t in range(lens[b], lens[b] + new[b]):
+                if t % P == 0:
+                    left -= 1
+                    table[b][t // P] = free[left]
+                slots.append(table[b][t // P] * P + t % P)
+            lens[b] += new[b]
+            start.append(len(slots))
+        slots += [-1] * (len(s["slots"]) - len(slots))
+        ints = lambda v: torch.tensor(v, dtype=torch.int32, device=DEV)  # noqa: E731
+        return {"lengths": ints(lens), "free_pages": ints(free), "free_count": ints([left]), "block_table": ints(table),
+                "slots": ints(slots), "token_start": ints(start), "status": ints([0])}
+    if c["op"] in ("append", "read"):
+        out = torch.zeros(s["rows"].shape, dtype=torch.float64, device=DEV)
+        at = 0
+        for b in range(B):
+            n = new[b] if c["op"] == "append" else lens[b]
+            for h in range(H):
+                if c["op"] == "append":
+                    out[0, b, h, :n], out[1, b, h, :n] = _nearest(s["k"][at:at + n, h]), _nearest(s["v"][at:at + n, h])
+                else:
+                    out[0, b, h, :n], out[1, b, h, :n] = _sequence(c, s["cache"], s["table"][b], h, n)
+            at += n
+        return {"k": out[0], "v": out[1]}
+    if c["op"] == "select":
+        idx = s["sets"].clone()
+        for b in range(B):
+            for h in range(H):
+                if mask[h * G:(h + 1) * G].any():
+                    x = s["scores"][b, h, :lens[b]].cpu().numpy()
+                    best = np.lexsort((np.arange(lens[b]), -x))[:c["k"]]
+                    idx[b, h] = -1
+                    idx[b, h, :len(best)] = torch.from_numpy(np.sort(best)).int()
+        return {"idx": idx}
+    out = torch.zeros(s["q"].shape, dtype=torch.float64, device=DEV)
+    scores = torch.zeros(s["scores"].shape, dtype=torch.float64, device=DEV) if c["scores"] else None
+    for b in range(B):
+        for h in range(H):
+            k, v = _sequence(c, s["cache"], s["table"][b], h, lens[b])
+            logit = (k @ s["q"][b, h * G:(h + 1) * G].double().T) / math.sqrt(D)  # [n, G]
+            m = mask[h * G:(h + 1) * G]
+            if m.any() and c["scores"]:
+                scores[b, h, :lens[b]] = logit[:, torch.from_numpy(m).bool().to(DEV)].mean(1)
+            for i in range(G):
+                at = slice(None) if m[i] else s["sets"][b, h][s["sets"][b, h] >= 0].long()
+                out[b, h * G + i] = logit[at, i].softmax(0) @ v[at]
+    return {"out": out, "scores": scores} if c["scores"] else {"out": out}
