@@ -272,6 +272,135 @@ int lychee_dense_decode_step(lychee_ctx *ctx, const lychee_shape *shape, int32_t
                              const void *const *v_cache, void *const *out, const int32_t *lengths,
                              void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* ==========================================================================================
+ * The paged 4-bit cache: a layer's keys and values in pages of a pool shared by all requests, 4 bits
+ * a value, and the hybrid-head decode layer that runs on it (Eq. 1 to 3 of Alg. 1's per-head loop).  A
+ * serving step is: lychee_release_pages (finished requests), lychee_plan_pages (pages and slots of
+ * the step's new tokens), and per layer lychee_q4_append, lychee_q4_decode_attn and, where retrieval
+ * heads choose sets for the next layer, lychee_select_scores.
+ *
+ *   - A page holds page_size tokens (16, 32, 64, 128 or 256) of every KV head, in tiles of 16 tokens
+ *     of one head: tile i of head g of page p is number p*page_tiles + g*(page_size/16) + i, at
+ *     cache + number*LYCHEE_Q4_TILE_BYTES.  page_tiles, the tiles from one page to the next, is at
+ *     least n_kv_heads*page_size/16 (more where the pages of several layers lie interleaved).
+ *   - A tile is 16 rows of 128 bytes, then 128 bytes of scales.  A row is a token's key (64 bytes)
+ *     and value (64 bytes): dimension 2j in the low, 2j+1 in the high half of byte j.  The scales are
+ *     [8][16] bytes: dimensions 0-31, 32-63, 64-95, 96-127 of the key, then of the value; 16 tokens.
+ *   - 4 bits are a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (the e2m1 format that gfx950 converts);
+ *     the value is that times 2^(scale byte - 127), and NaN under a scale byte of 255.
+ *   - Writing a group of 32 values takes the smallest e in [-125, 125] with max |x| <= 6 * 2^e and
+ *     rounds x / 2^e to the nearest of these values, ties to the even code (what lies beyond 6 * 2^125
+ *     becomes 6 * 2^125); a group that holds a NaN or an infinity gets the scale byte 255.
+ *   - A slot names a token's place in a layer's cache: page * page_size + place in the page.
+ *   - block_table is int32 [batch][table_stride]: entry t / page_size of a request's row is the page
+ *     of its token t.  Entries outside [0, n_pages) are never followed: tokens there are not
+ *     written, and attention leaves them out.  Several requests may share a page that none writes.
+ *   - lengths is int32 [batch], tokens a request holds: values outside [0, max_pages * page_size] are
+ *     clamped into it, except by lychee_plan_pages, which refuses them.  A request of length 0 is
+ *     legal everywhere: its outputs are zero.
+ *   - bf16 operands need 16-byte alignment, int32 and float ones 4-byte, the cache 128-byte.
+ *   - Each call enqueues one kernel launch (none where there is nothing to do), may be captured, and
+ *     leaves the caller's current device as it was.  Launches of these calls are not timed by
+ *     lychee_timing_enable.  What else the conventions above say holds here too.
+ * ========================================================================================== */
+#define LYCHEE_Q4_TILE_BYTES 2176
+#define LYCHEE_Q4_MAX_GROUP    16  /* query heads per KV head served by lychee_q4_decode_attn (1..16) */
+
+typedef struct lychee_paged {
+    int32_t batch;        /* requests, in [1, LYCHEE_MAX_BATCH]                                   */
+    int32_t n_q_heads;    /* a multiple of n_kv_heads                                            */
+    int32_t n_kv_heads;   /* in [1, LYCHEE_MAX_KV_HEADS]                                         */
+    int32_t head_dim;     /* must be LYCHEE_HEAD_DIM                                             */
+    int32_t n_pages;      /* pages of the pool; n_pages * page_size < 2^31                       */
+    int32_t page_size;    /* 16, 32, 64, 128 or 256                                              */
+    int32_t max_pages;    /* pages a request can hold; max_pages * page_size <= 2^24             */
+    int32_t table_stride; /* entries from one row of the block table to the next, >= max_pages   */
+    int32_t page_tiles;   /* tiles from one page to the next, >= n_kv_heads * page_size / 16     */
+    int32_t k;            /* entries of an index set, >= 1                                       */
+} lychee_paged;
+
+/* Pure host functions.  lychee_check_paged: validates `paged` and, if `head_type_mask` (HOST, [H_q]) is
+ * given, that sparse heads come with a set.  lychee_paged_workspace_bytes: scratch of
+ * lychee_q4_decode_attn and lychee_select_scores (256-byte aligned, contents don't care); 0 if
+ * `paged` is invalid. */
+int    lychee_check_paged(const lychee_paged *paged, const uint8_t *head_type_mask, int has_idx_in);
+size_t lychee_paged_workspace_bytes(const lychee_paged *paged);
+
+/* Gives the pages of finished requests back to the pool.  The free pages are a stack: entries
+ * free_pages[0 .. *free_count-1], taken and given at its end.
+ *   done           uint8 [B]: not 0 = the request's pages go back, in order of the request and of its
+ *                  table, and its length becomes 0
+ *   lengths, lengths_out         int32 [B]; may be one array
+ *   free_pages     int32 [n_pages]; pages that do not fit any more (given back twice) are dropped
+ *   free_count, free_count_out   int32 [1]; may be one word
+ * The block table is only read. */
+int lychee_release_pages(lychee_ctx *ctx, const lychee_paged *paged, const uint8_t *done, const int32_t *lengths,
+                         const int32_t *block_table, int32_t *free_pages, const int32_t *free_count,
+                         int32_t *lengths_out, int32_t *free_count_out, void *hip_stream);
+
+/* Block table, slots and lengths of a step in which request b gets new_tokens[b] >= 0 more tokens.
+ *   block_table    entries of the pages taken are written: requests in order take pages off the end of
+ *                  free_pages; other entries are left as they are
+ *   lengths_out    lengths[b] + new_tokens[b]; may be `lengths`.  free_count_out may be `free_count`
+ *   slots          int32 [n_slots]: the slots of the new tokens, request after request, then -1
+ *                  (-1 also for a token whose table entry is no page)
+ *   token_start    int32 [B + 1]: where each request's tokens begin in `slots`; the last is their number
+ *   status         int32 [1]: 0, or why nothing was planned: the number of pages missing; -1: a length or
+ *                  count is negative or makes a request longer than max_pages hold, or *free_count is
+ *                  not in [0, n_pages]; -2: more new tokens than n_slots.  Then lengths_out and
+ *                  free_count_out repeat the inputs, the table is unchanged, `slots` is all -1 and
+ *                  `token_start` all 0. */
+int lychee_plan_pages(lychee_ctx *ctx, const lychee_paged *paged, const int32_t *lengths, const int32_t *new_tokens,
+                      int32_t *block_table, const int32_t *free_pages, const int32_t *free_count,
+                      int32_t *lengths_out, int32_t *free_count_out, int32_t *slots, int32_t n_slots,
+                      int32_t *token_start, int32_t *status, void *hip_stream);
+
+/* Writes tokens into a layer's cache.
+ *   k_new, v_new   bf16, element (i, g, d) of token i at base + i*stride_tok + g*stride_head + d; the
+ *                  strides are in elements, multiples of 8, both operands share them
+ *   slots          int32 [n_tokens]; a token whose slot is outside [0, n_pages * page_size) is not
+ *                  written.  No slot may occur twice in a call. */
+int lychee_q4_append(lychee_ctx *ctx, const lychee_paged *paged, const void *k_new, const void *v_new,
+                     int64_t stride_tok, int64_t stride_head, const int32_t *slots, int32_t n_tokens, void *cache,
+                     void *hip_stream);
+
+/* Reads tokens back as bf16 rows (exactly the values the cache stands for), for example into a cache of the
+ * calls above: token t of request b, first[b] <= t < last[b], becomes row t - first[b].
+ *   first          int32 [B], or NULL for 0; last int32 [B]; clamped like lengths
+ *   k_out, v_out   bf16, element (b, g, row, d) at base + b*stride_batch + g*stride_head + row*stride_tok + d
+ *                  (elements, multiples of 8, stride_tok >= 128); rows beyond n_rows and behind a request's
+ *                  last token are left as they were, a row whose token has no page is zero */
+int lychee_q4_read(lychee_ctx *ctx, const lychee_paged *paged, const void *cache, const int32_t *block_table,
+                   const int32_t *first, const int32_t *last, void *k_out, void *v_out, int64_t stride_batch,
+                   int64_t stride_head, int64_t stride_tok, int32_t n_rows, void *hip_stream);
+
+/* One layer of Alg. 1's per-head loop on the 4-bit cache, one query token a request.
+ *   q, out          bf16 [B][H_q][128]
+ *   head_type_mask  HOST uint8 [H_q]: 1 = retrieval head (Eq. 1 over t < L_b), 0 = sparse head (Eq. 3 over its KV
+ *                   head's set); NULL: every head is a retrieval head
+ *   idx_in          int32 [B][H_kv][k], sets as in the conventions; may be NULL if there is no sparse head.  Of a
+ *                   set the first min(k, L_b) entries are read; those negative or >= L_b are ignored
+ *   scores          NULL, or float, row (b, g) at scores + (b*H_kv + g)*score_stride: the mean logit of the
+ *                   group's retrieval heads at every t < L_b (-infinity where the token has no page).  Rows of
+ *                   KV heads without a retrieval head, and what lies behind L_b, are left as they were.
+ *                   score_stride >= max_pages * page_size
+ * A head with nothing to attend to (L_b = 0, an empty set, no page) gives zeros.  Scores and sums are
+ * fp32; the softmax weights multiply V as the sum of two bf16 numbers (about 2^-17 of a weight).
+ * Errors: EUNSUPPORTED for a group of more than LYCHEE_Q4_MAX_GROUP, or more than 2^31 blocks of work. */
+int lychee_q4_decode_attn(lychee_ctx *ctx, const lychee_paged *paged, const void *q, const void *cache,
+                          const int32_t *block_table, const int32_t *lengths, const uint8_t *head_type_mask,
+                          const int32_t *idx_in, void *out, float *scores, int64_t score_stride, void *workspace,
+                          size_t workspace_bytes, void *hip_stream);
+
+/* Eq. 2 on rows of scores: idx_out [B][H_kv][k] gets, for a KV head whose group holds a retrieval head, the
+ * min(k, L_b) positions t < L_b with the highest scores[(b*H_kv + g)*score_stride + t], ties to the lower
+ * position, ascending, -1 behind them; for any other KV head a verbatim copy of idx_in.  NaN ranks like
+ * -infinity, -0 like 0.  head_type_mask as above (NULL: every KV head selects; then idx_in may be NULL); idx_out
+ * must not be idx_in; score_stride >= max_pages * page_size. */
+int lychee_select_scores(lychee_ctx *ctx, const lychee_paged *paged, const float *scores, int64_t score_stride,
+                         const int32_t *lengths, const uint8_t *head_type_mask, const int32_t *idx_in,
+                         int32_t *idx_out, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 const char *lychee_strerror(int code);
 
 /* ==========================================================================================
@@ -339,7 +468,7 @@ int lychee_select_stats(lychee_ctx *ctx, int64_t *too_few, int64_t *too_many, vo
 int lychee_wait_timeouts(lychee_ctx *ctx, int64_t *timeouts, void *hip_stream);
 
 /* Per-launch timing with HIP events on the caller's stream.  While enabled, every launch of
- * the library's kernels is bracketed by an event pair.  lychee_timing_read waits for the
+ * the library's kernels but those of the paged 4-bit cache is bracketed by an event pair.  lychee_timing_read waits for the
  * recorded events, adds up the milliseconds and launches per launch class since the last
  * read and clears the record (arrays of LYCHEE_N_KERNEL_CLASSES entries). */
 #define LYCHEE_KERNEL_STREAM  0   /* retrieval streaming of a phased step; a layer launch       */

@@ -24,6 +24,7 @@ OPT_DEFAULTS = 0
 OPT_SELECT_LEAD = 10
 OPT_WAIT_POLLS = 11
 STATIC_SCRATCH_BYTES = 32 << 20
+Q4_TILE_TOKENS, Q4_TILE_BYTES, Q4_MAX_GROUP = 16, 2176, 16
 OPT_WG_PER_CU, OPT_STEP_MODE, OPT_GATHER_BLOCK, OPT_N_WG, OPT_TAIL_PERMILLE, OPT_SELECT_MARGIN = 1, 2, 6, 7, 8, 9
 STEP_PHASED, STEP_LAYERWISE = 1, 0
 RULE_THRESHOLD, RULE_TOP_P = 1, 2
@@ -37,6 +38,8 @@ EXPORTS = [
     "lychee_wait_timeouts",
     "lychee_validate_idx", "lychee_set_option", "lychee_timing_enable",
     "lychee_timing_read", "lychee_probe_read", "lychee_probe_copy", "lychee_strerror",
+    "lychee_check_paged", "lychee_paged_workspace_bytes", "lychee_release_pages", "lychee_plan_pages",
+    "lychee_q4_append", "lychee_q4_read", "lychee_q4_decode_attn", "lychee_select_scores",
 ]
 
 
@@ -49,6 +52,14 @@ class Shape(ctypes.Structure):
                 ("kv_stride_tok", ctypes.c_int64), ("keep_ppm", ctypes.c_int32),
                 ("block_size", ctypes.c_int32), ("prob_rule", ctypes.c_int32),
                 ("prob_param", ctypes.c_float)]
+
+
+class Paged(ctypes.Structure):
+    """Mirror of `lychee_paged`."""
+    _fields_ = [("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("table_stride", ctypes.c_int32), ("page_tiles", ctypes.c_int32),
+                ("k", ctypes.c_int32)]
 
 
 class LycheeError(RuntimeError):
@@ -88,10 +99,21 @@ def _load() -> ctypes.CDLL:
     lib.lychee_timing_read.argtypes = [vp, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(i32)]
     lib.lychee_probe_read.argtypes = [vp, vp, sz, vp, vp]
     lib.lychee_probe_copy.argtypes = [vp, vp, vp, sz, vp]
+    pgd = ctypes.POINTER(Paged)
+    lib.lychee_check_paged.argtypes = [pgd, vp, ctypes.c_int]
+    lib.lychee_paged_workspace_bytes.argtypes = [pgd]
+    lib.lychee_paged_workspace_bytes.restype = sz
+    lib.lychee_release_pages.argtypes = [vp, pgd, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.lychee_plan_pages.argtypes = [vp, pgd, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp]
+    lib.lychee_q4_append.argtypes = [vp, pgd, vp, vp, i64, i64, vp, i32, vp, vp]
+    lib.lychee_q4_read.argtypes = [vp, pgd, vp, vp, vp, vp, vp, vp, i64, i64, i64, i32, vp]
+    lib.lychee_q4_decode_attn.argtypes = [vp, pgd, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp, sz, vp]
+    lib.lychee_select_scores.argtypes = [vp, pgd, vp, i64, vp, vp, vp, vp, vp, sz, vp]
     lib.lychee_strerror.argtypes = [ctypes.c_int]
     lib.lychee_strerror.restype = ctypes.c_char_p
     for name in EXPORTS:
-        if name not in ("lychee_workspace_bytes", "lychee_step_workspace_bytes", "lychee_strerror"):
+        if name not in ("lychee_workspace_bytes", "lychee_step_workspace_bytes", "lychee_paged_workspace_bytes",
+                        "lychee_strerror"):
             getattr(lib, name).restype = ctypes.c_int
     return lib
 
@@ -154,6 +176,37 @@ def workspace_bytes(shape: Shape) -> int:
 
 def step_workspace_bytes(shape: Shape, n_layers: int) -> int:
     return int(_lib.lychee_step_workspace_bytes(ctypes.byref(shape), n_layers))
+
+
+def make_paged(batch: int, n_q_heads: int, n_kv_heads: int, n_pages: int, page_size: int, max_pages: int, k: int = 1,
+               table_stride: int = 0, page_tiles: int = 0, head_dim: int = 128) -> Paged:
+    """A `lychee_paged`; table rows and pages lie one behind the other unless strides are given."""
+    return Paged(batch, n_q_heads, n_kv_heads, head_dim, n_pages, page_size, max_pages, table_stride or max_pages,
+                 page_tiles or n_kv_heads * (page_size // Q4_TILE_TOKENS), k)
+
+
+def check_paged(paged: Paged, head_type_mask: Optional[np.ndarray] = None, has_idx_in: bool = True) -> int:
+    """lychee_check_paged: returns the status code (pure host)."""
+    m = None if head_type_mask is None else np.ascontiguousarray(head_type_mask, dtype=np.uint8)
+    return _lib.lychee_check_paged(ctypes.byref(paged), None if m is None else m.ctypes.data, int(has_idx_in))
+
+
+def paged_workspace_bytes(paged: Paged) -> int:
+    return int(_lib.lychee_paged_workspace_bytes(ctypes.byref(paged)))
+
+
+def _mask_ptr(head_type_mask, n_q_heads: int):
+    """The host array of head types and its address (None: every head is a retrieval head)."""
+    if head_type_mask is None:
+        return None, None
+    m = np.ascontiguousarray(head_type_mask, dtype=np.uint8)
+    assert m.shape == (n_q_heads,)
+    return m, m.ctypes.data
+
+
+def _is_rows(scores) -> bool:
+    """Whether row (b, g) of [B, H_kv, n] lies (b * H_kv + g) strides behind the first."""
+    return scores.stride(2) == 1 and (scores.shape[0] == 1 or scores.stride(0) == scores.shape[1] * scores.stride(1))
 
 
 class Context:
@@ -261,6 +314,60 @@ class Context:
                                              workspace.numel() * workspace.element_size(),
                                              _stream(stream)), "lychee_dense_decode_step")
 
+    # -- the paged 4-bit cache ----------------------------------------------------------
+    def release_pages(self, paged: Paged, done, lengths, block_table, free_pages, free_count, lengths_out=None,
+                      free_count_out=None, stream=None) -> None:
+        """lychee_release_pages; lengths and count are updated in place unless outputs are given."""
+        _check(_lib.lychee_release_pages(self._h, ctypes.byref(paged), _ptr(done), _ptr(lengths), _ptr(block_table),
+                                         _ptr(free_pages), _ptr(free_count),
+                                         _ptr(lengths if lengths_out is None else lengths_out),
+                                         _ptr(free_count if free_count_out is None else free_count_out),
+                                         _stream(stream)), "lychee_release_pages")
+
+    def plan_pages(self, paged: Paged, lengths, new_tokens, block_table, free_pages, free_count, lengths_out,
+                   free_count_out, slots, token_start, status, stream=None) -> None:
+        """lychee_plan_pages; lengths_out / free_count_out None: in place."""
+        _check(_lib.lychee_plan_pages(self._h, ctypes.byref(paged), _ptr(lengths), _ptr(new_tokens), _ptr(block_table),
+                                      _ptr(free_pages), _ptr(free_count),
+                                      _ptr(lengths if lengths_out is None else lengths_out),
+                                      _ptr(free_count if free_count_out is None else free_count_out), _ptr(slots),
+                                      slots.numel(), _ptr(token_start), _ptr(status), _stream(stream)),
+               "lychee_plan_pages")
+
+    def q4_append(self, paged: Paged, k_new, v_new, slots, cache, stream=None) -> None:
+        """lychee_q4_append; k_new and v_new are [n_tokens, H_kv, 128] with the same strides."""
+        assert k_new.stride() == v_new.stride() and k_new.stride(2) == 1
+        _check(_lib.lychee_q4_append(self._h, ctypes.byref(paged), _ptr(k_new), _ptr(v_new), k_new.stride(0),
+                                     k_new.stride(1), _ptr(slots), slots.numel(), _ptr(cache), _stream(stream)),
+               "lychee_q4_append")
+
+    def q4_read(self, paged: Paged, cache, block_table, first, last, k_out, v_out, stream=None) -> None:
+        """lychee_q4_read; k_out and v_out are [B, H_kv, rows, 128] with the same strides."""
+        assert k_out.stride() == v_out.stride() and k_out.stride(3) == 1
+        _check(_lib.lychee_q4_read(self._h, ctypes.byref(paged), _ptr(cache), _ptr(block_table), _ptr(first), _ptr(last),
+                                   _ptr(k_out), _ptr(v_out), k_out.stride(0), k_out.stride(1), k_out.stride(2),
+                                   k_out.shape[2], _stream(stream)), "lychee_q4_read")
+
+    def q4_decode_attn(self, paged: Paged, q, cache, block_table, lengths, head_type_mask, idx_in, out, scores, workspace,
+                       stream=None) -> None:
+        """lychee_q4_decode_attn; scores None or [B, H_kv, row] with contiguous (b, g) rows."""
+        mask, at = _mask_ptr(head_type_mask, paged.n_q_heads)
+        assert scores is None or _is_rows(scores)
+        _check(_lib.lychee_q4_decode_attn(self._h, ctypes.byref(paged), _ptr(q), _ptr(cache), _ptr(block_table),
+                                          _ptr(lengths), at, _ptr(idx_in), _ptr(out), _ptr(scores),
+                                          0 if scores is None else scores.stride(1), _ptr(workspace),
+                                          workspace.numel() * workspace.element_size(), _stream(stream)),
+               "lychee_q4_decode_attn")
+
+    def select_scores(self, paged: Paged, scores, lengths, head_type_mask, idx_in, idx_out, workspace,
+                      stream=None) -> None:
+        mask, at = _mask_ptr(head_type_mask, paged.n_q_heads)
+        assert _is_rows(scores)
+        _check(_lib.lychee_select_scores(self._h, ctypes.byref(paged), _ptr(scores), scores.stride(1), _ptr(lengths), at,
+                                         _ptr(idx_in), _ptr(idx_out), _ptr(workspace),
+                                         workspace.numel() * workspace.element_size(), _stream(stream)),
+               "lychee_select_scores")
+
     # -- helpers ------------------------------------------------------------------------
     def select_stats(self, stream=None):
         """(too_few, too_many): score rows the select ranked whole since the context was created."""
@@ -309,3 +416,18 @@ def alloc_workspace(shape: Shape, device="cuda", n_layers: int = 1) -> torch.Ten
     if n == 0:
         raise LycheeError(_lib.lychee_check_shape(ctypes.byref(shape), None, 1), "lychee_workspace_bytes")
     return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def alloc_paged_workspace(paged: Paged, device="cuda") -> torch.Tensor:
+    """A device buffer of lychee_paged_workspace_bytes(paged) bytes."""
+    n = paged_workspace_bytes(paged)
+    if n == 0:
+        raise LycheeError(check_paged(paged), "lychee_paged_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def alloc_q4_cache(paged: Paged, device="cuda") -> torch.Tensor:
+    """The pages of one layer's cache, [n_pages, page_tiles * Q4_TILE_BYTES] bytes."""
+    if check_paged(paged) != OK:
+        raise LycheeError(check_paged(paged), "lychee_check_paged")
+    return torch.empty((paged.n_pages, paged.page_tiles * Q4_TILE_BYTES), dtype=torch.uint8, device=device)

@@ -8,7 +8,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblychee.so")
-SOURCES = ["lychee_api.hip", "lychee_units.hip", "lychee_layer.hip"]
+SOURCES = ["lychee_api.hip", "lychee_units.hip", "lychee_layer.hip", "lychee_paged_api.hip", "lychee_pages.hip", "lychee_q4.hip",
+           "lychee_topk.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-command-line-argument"]
