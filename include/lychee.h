@@ -386,7 +386,7 @@ int lychee_q4_read(lychee_ctx *ctx, const lychee_paged *paged, const void *cache
  *                   score_stride >= max_pages * page_size
  * A head with nothing to attend to (L_b = 0, an empty set, no page) gives zeros.  Scores and sums are
  * fp32; the softmax weights multiply V as the sum of two bf16 numbers (about 2^-17 of a weight).
- * Errors: EUNSUPPORTED for a group of more than LYCHEE_Q4_MAX_GROUP, or more than 2^31 blocks of work. */
+ * Errors: EUNSUPPORTED for a group of more than LYCHEE_Q4_MAX_GROUP, or more than 2^30 blocks of work. */
 int lychee_q4_decode_attn(lychee_ctx *ctx, const lychee_paged *paged, const void *q, const void *cache,
                           const int32_t *block_table, const int32_t *lengths, const uint8_t *head_type_mask,
                           const int32_t *idx_in, void *out, float *scores, int64_t score_stride, void *workspace,

@@ -204,6 +204,20 @@ def _mask_ptr(head_type_mask, n_q_heads: int):
     return m, m.ctypes.data
 
 
+def _at(t) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def _raw_stream(device: int) -> Optional[int]:
+    """torch's current stream of a device as a hipStream_t."""
+    return _current_raw_stream(device) or None
+
+
+# (torch.cuda.current_stream builds a Stream object, 2.9 us of a call; the getter behind it takes 0.07)
+_current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                              lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
 def _is_rows(scores) -> bool:
     """Whether row (b, g) of [B, H_kv, n] lies (b * H_kv + g) strides behind the first."""
     return scores.stride(2) == 1 and (scores.shape[0] == 1 or scores.stride(0) == scores.shape[1] * scores.stride(1))
@@ -315,57 +329,64 @@ class Context:
                                              _stream(stream)), "lychee_dense_decode_step")
 
     # -- the paged 4-bit cache ----------------------------------------------------------
+    # (calls of a few microseconds: what marshals their arguments is kept short)
+    def _on(self, stream):
+        """The stream of a call: the given one, or the current one of the context's device (not of the current device)."""
+        if stream is None:
+            return _raw_stream(self.device)
+        return _stream(stream)
+
     def release_pages(self, paged: Paged, done, lengths, block_table, free_pages, free_count, lengths_out=None,
                       free_count_out=None, stream=None) -> None:
         """lychee_release_pages; lengths and count are updated in place unless outputs are given."""
-        _check(_lib.lychee_release_pages(self._h, ctypes.byref(paged), _ptr(done), _ptr(lengths), _ptr(block_table),
-                                         _ptr(free_pages), _ptr(free_count),
-                                         _ptr(lengths if lengths_out is None else lengths_out),
-                                         _ptr(free_count if free_count_out is None else free_count_out),
-                                         _stream(stream)), "lychee_release_pages")
+        _check(_lib.lychee_release_pages(self._h, ctypes.byref(paged), _at(done), _at(lengths), _at(block_table),
+                                         _at(free_pages), _at(free_count),
+                                         _at(lengths if lengths_out is None else lengths_out),
+                                         _at(free_count if free_count_out is None else free_count_out),
+                                         self._on(stream)), "lychee_release_pages")
 
     def plan_pages(self, paged: Paged, lengths, new_tokens, block_table, free_pages, free_count, lengths_out,
                    free_count_out, slots, token_start, status, stream=None) -> None:
         """lychee_plan_pages; lengths_out / free_count_out None: in place."""
-        _check(_lib.lychee_plan_pages(self._h, ctypes.byref(paged), _ptr(lengths), _ptr(new_tokens), _ptr(block_table),
-                                      _ptr(free_pages), _ptr(free_count),
-                                      _ptr(lengths if lengths_out is None else lengths_out),
-                                      _ptr(free_count if free_count_out is None else free_count_out), _ptr(slots),
-                                      slots.numel(), _ptr(token_start), _ptr(status), _stream(stream)),
+        _check(_lib.lychee_plan_pages(self._h, ctypes.byref(paged), _at(lengths), _at(new_tokens), _at(block_table),
+                                      _at(free_pages), _at(free_count),
+                                      _at(lengths if lengths_out is None else lengths_out),
+                                      _at(free_count if free_count_out is None else free_count_out), _at(slots),
+                                      slots.numel(), _at(token_start), _at(status), self._on(stream)),
                "lychee_plan_pages")
 
     def q4_append(self, paged: Paged, k_new, v_new, slots, cache, stream=None) -> None:
         """lychee_q4_append; k_new and v_new are [n_tokens, H_kv, 128] with the same strides."""
         assert k_new.stride() == v_new.stride() and k_new.stride(2) == 1
-        _check(_lib.lychee_q4_append(self._h, ctypes.byref(paged), _ptr(k_new), _ptr(v_new), k_new.stride(0),
-                                     k_new.stride(1), _ptr(slots), slots.numel(), _ptr(cache), _stream(stream)),
+        _check(_lib.lychee_q4_append(self._h, ctypes.byref(paged), _at(k_new), _at(v_new), k_new.stride(0),
+                                     k_new.stride(1), _at(slots), slots.numel(), _at(cache), self._on(stream)),
                "lychee_q4_append")
 
     def q4_read(self, paged: Paged, cache, block_table, first, last, k_out, v_out, stream=None) -> None:
         """lychee_q4_read; k_out and v_out are [B, H_kv, rows, 128] with the same strides."""
         assert k_out.stride() == v_out.stride() and k_out.stride(3) == 1
-        _check(_lib.lychee_q4_read(self._h, ctypes.byref(paged), _ptr(cache), _ptr(block_table), _ptr(first), _ptr(last),
-                                   _ptr(k_out), _ptr(v_out), k_out.stride(0), k_out.stride(1), k_out.stride(2),
-                                   k_out.shape[2], _stream(stream)), "lychee_q4_read")
+        _check(_lib.lychee_q4_read(self._h, ctypes.byref(paged), _at(cache), _at(block_table), _at(first), _at(last),
+                                   _at(k_out), _at(v_out), k_out.stride(0), k_out.stride(1), k_out.stride(2),
+                                   k_out.shape[2], self._on(stream)), "lychee_q4_read")
 
     def q4_decode_attn(self, paged: Paged, q, cache, block_table, lengths, head_type_mask, idx_in, out, scores, workspace,
                        stream=None) -> None:
         """lychee_q4_decode_attn; scores None or [B, H_kv, row] with contiguous (b, g) rows."""
         mask, at = _mask_ptr(head_type_mask, paged.n_q_heads)
         assert scores is None or _is_rows(scores)
-        _check(_lib.lychee_q4_decode_attn(self._h, ctypes.byref(paged), _ptr(q), _ptr(cache), _ptr(block_table),
-                                          _ptr(lengths), at, _ptr(idx_in), _ptr(out), _ptr(scores),
-                                          0 if scores is None else scores.stride(1), _ptr(workspace),
-                                          workspace.numel() * workspace.element_size(), _stream(stream)),
+        _check(_lib.lychee_q4_decode_attn(self._h, ctypes.byref(paged), _at(q), _at(cache), _at(block_table),
+                                          _at(lengths), at, _at(idx_in), _at(out), _at(scores),
+                                          0 if scores is None else scores.stride(1), _at(workspace),
+                                          workspace.numel() * workspace.element_size(), self._on(stream)),
                "lychee_q4_decode_attn")
 
     def select_scores(self, paged: Paged, scores, lengths, head_type_mask, idx_in, idx_out, workspace,
                       stream=None) -> None:
         mask, at = _mask_ptr(head_type_mask, paged.n_q_heads)
         assert _is_rows(scores)
-        _check(_lib.lychee_select_scores(self._h, ctypes.byref(paged), _ptr(scores), scores.stride(1), _ptr(lengths), at,
-                                         _ptr(idx_in), _ptr(idx_out), _ptr(workspace),
-                                         workspace.numel() * workspace.element_size(), _stream(stream)),
+        _check(_lib.lychee_select_scores(self._h, ctypes.byref(paged), _at(scores), scores.stride(1), _at(lengths), at,
+                                         _at(idx_in), _at(idx_out), _at(workspace),
+                                         workspace.numel() * workspace.element_size(), self._on(stream)),
                "lychee_select_scores")
 
     # -- helpers ------------------------------------------------------------------------

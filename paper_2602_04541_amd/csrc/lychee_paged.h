@@ -13,9 +13,11 @@ constexpr int kTileScales = kTileTokens * kTokenBytes;  // where the scales begi
 constexpr int kScaleMin = 127 - 125, kScaleMax = 127 + 125;  // scale bytes of finite groups
 constexpr int kQ4Block = 64;               // tokens a wavefront takes at a time
 constexpr int kQ4MaxGroup = 16;
+constexpr int kSplits = 16;                // sizes of a piece that an attention launch weighs
+constexpr int kPieceCost = 12;             // what a piece costs whatever its length, in blocks
 constexpr int kQ4WgPerCu = 2;
-constexpr int kQ4MaxWg = 512;             // upper bound of an attention launch's grid
-constexpr int64_t kMaxTiles = 1 << 27;    // of a cache (292 GB)
+constexpr int kQ4MaxWg = 512;              // upper bound of an attention launch's grid
+constexpr int64_t kMaxTiles = 1 << 27;     // of a cache (292 GB)
 constexpr int kMaxContext = 1 << 24;       // tokens a request can hold
 
 // Sizes of a paged cache, as the kernels need them.
@@ -69,7 +71,8 @@ struct Q4AttnArgs {
     int64_t score_stride;
     float *part_o;        // [slot][group][128] un-normalised partial outputs
     float *part_ml;       // [slot][group][2]   running maximum (log2 units) and sum
-    uint32_t *seg_count;  // [B * H_kv * 2][kLineWords] blocks of a segment done so far; zero between launches
+    uint32_t *seg_count;  // [B * H_kv * 2][kLineWords] pieces of a segment done so far; zero between launches
+    uint32_t *claims;     // pieces claimed beyond the first of every workgroup; zero between launches
     int32_t n_wg, n_rseg, n_gseg;
     float scale, scale_log2e;
     uint16_t rmask[kMaxKvHeads];  // per KV head: bit i = query head g*group + i is a retrieval head
@@ -86,8 +89,8 @@ struct SelectArgs {
     uint64_t selects;  // bit g: KV head g's set is selected, else copied
 };
 
-// Partial slots of an attention launch: a workgroup's run of blocks crosses segments ((request, KV head, kind of
-// head)), and every piece has the slot run + segment.
+// Partial slots of an attention launch, one a piece: pieces are at least an equal share of the blocks long, but for the
+// last one of every segment ((request, KV head, kind of head)).
 inline int64_t q4_slots(int32_t batch, int32_t n_segs, int32_t n_wg) { return (int64_t)batch * n_segs + n_wg; }
 
 hipError_t launch_release(const ReleaseArgs &a, hipStream_t stream);

@@ -210,7 +210,7 @@ int lychee_q4_decode_attn(lychee_ctx *ctx, const lychee_paged *paged, const void
     const int64_t seg_blocks = (a.d.max_len + kQ4Block - 1) / kQ4Block;
     const int64_t set_blocks = ((paged->k < a.d.max_len ? paged->k : a.d.max_len) + kQ4Block - 1) / kQ4Block;
     const int64_t most = (int64_t)paged->batch * (a.n_rseg * seg_blocks + a.n_gseg * set_blocks);
-    if (most > INT32_MAX) return LYCHEE_EUNSUPPORTED;
+    if (most >= INT32_MAX / 2) return LYCHEE_EUNSUPPORTED;
     const OnDevice dev(ctx);
     if (!dev.ok) return LYCHEE_EHIP;
     a.q = static_cast<const uint16_t *>(q);
@@ -224,9 +224,12 @@ int lychee_q4_decode_attn(lychee_ctx *ctx, const lychee_paged *paged, const void
     a.part_o = reinterpret_cast<float *>(static_cast<char *>(workspace) + w.part_o);
     a.part_ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + w.part_ml);
     a.seg_count = reinterpret_cast<uint32_t *>(ctx->sync_dev + kSyncSeg);
+    a.claims = reinterpret_cast<uint32_t *>(ctx->sync_dev + kSyncClaims);
     a.n_wg = ctx->n_cu * kQ4WgPerCu;
     if (a.n_wg > kQ4MaxWg) a.n_wg = kQ4MaxWg;
-    if (a.n_wg > (most + kWaves - 1) / kWaves) a.n_wg = (int32_t)((most + kWaves - 1) / kWaves);  // (a run is four blocks at least)
+    // (a piece is four blocks at least, or a whole segment)
+    const int64_t pieces = (int64_t)paged->batch * (a.n_rseg * ((seg_blocks + kWaves - 1) / kWaves) + a.n_gseg * ((set_blocks + kWaves - 1) / kWaves));
+    if (a.n_wg > pieces) a.n_wg = (int32_t)pieces;
     a.scale = (float)(1.0 / sqrt((double)kHeadDim));
     a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)kHeadDim));
     return done(launch_q4_attn(a, static_cast<hipStream_t>(hip_stream)));

@@ -10,8 +10,15 @@ namespace {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 
+// Orders what the lanes of a wavefront hand to one another through LDS (whose accesses a wavefront makes in order).
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+// The cache is read once a step: nontemporal loads.
+__device__ __forceinline__ uint4 load16(const uint8_t *p) { return load_stream16(reinterpret_cast<const uint16_t *>(p)); }
 __device__ __forceinline__ int clamp_tokens(int L, int most) { return L < 0 ? 0 : (L > most ? most : L); }
-__device__ __forceinline__ int64_t tile_at(int32_t tile) { return (int64_t)tile * kTileBytes; }
 
 // ------------------------------------------------------------------------------ append
 // Magnitudes of two bf16 numbers, ordered as 16-bit integers (a NaN's is the largest).
@@ -68,7 +75,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a)
     const int page = slot >> a.d.page_shift, off = slot & ((1 << a.d.page_shift) - 1);
     if (slot < 0 || page >= a.d.n_pages) return;
     const int sub = off & (kTileTokens - 1);
-    uint8_t *tile = a.cache + tile_at(0) +
+    uint8_t *tile = a.cache +
                     ((int64_t)page * a.d.page_tiles + (int64_t)g * ((1 << a.d.page_shift) / kTileTokens) + off / kTileTokens) * kTileBytes;
     uint32_t *to = reinterpret_cast<uint32_t *>(tile + sub * kTokenBytes);
     gstore(to + lane, codes8(k, ks));
@@ -81,11 +88,17 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a)
 }
 
 // ------------------------------------------------------------------------------ read
+// Byte i as the scale of a conversion, which reads a float's exponent field alone (what the neighbouring bytes leave in
+// the sign and the mantissa is ignored).
+__device__ __forceinline__ float scale_of(uint32_t bytes, int i)
+{
+    return __builtin_bit_cast(float, i == 0 ? bytes << 23 : i == 1 ? bytes << 15 : i == 2 ? bytes << 7 : bytes >> 1);
+}
+
 // Eight codes as bf16 numbers, exactly: e2m1 times a power of two, within bf16's normal range for every scale byte that
 // append writes; 255 makes them NaN.
-__device__ __forceinline__ uint4 decode8(uint32_t c, uint32_t s)
+__device__ __forceinline__ uint4 decode8(uint32_t c, float scale)
 {
-    const float scale = __builtin_bit_cast(float, s << 23);
     return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0)),
                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1)),
                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2)),
@@ -115,8 +128,8 @@ __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a)
                                              off / kTileTokens) * kTileBytes;
             const uint32_t *row = reinterpret_cast<const uint32_t *>(tile + sub * kTokenBytes);
             const uint8_t *sc = tile + kTileScales + (lane >> 2) * kTileTokens + sub;
-            k = decode8(gload(row + lane), gload(sc));
-            v = decode8(gload(row + 16 + lane), gload(sc + 4 * kTileTokens));
+            k = decode8(gload(row + lane), scale_of(gload(sc), 0));
+            v = decode8(gload(row + 16 + lane), scale_of(gload(sc + 4 * kTileTokens), 0));
         }
         const int64_t to = (int64_t)b * a.stride_b + (int64_t)g * a.stride_h + (int64_t)r * a.stride_t + 8 * lane;
         gstore_u4(a.k_out + to, k);
@@ -135,43 +148,48 @@ __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a)
 // They are merged in LDS when the piece ends; a piece that is a whole segment writes the output, others leave a partial,
 // and the workgroup that completes a segment merges its partials.
 //
-// A wavefront's block: lane (g, n) = (lane / 16, lane % 16).
-//   scores  v_mfma_f32_16x16x32_bf16, A = queries (16 rows), B = keys (16 tokens), 4 times along the dimensions, for 4
-//           groups of 16 tokens: group a's column n is token 4n + a.  Head number i of the segment is row 4(i%4) + i/4,
-//           so that lane (g, n) has the scores of heads g, g+4, .. in its registers 0, 1, ..: with the usual four heads
-//           every lane works on one number in the softmax.  A lane loads 16 bytes of a key, its dimensions 32g .. 32g+31
-//           under one scale byte, straight from the cache, and converts them (two numbers an instruction, exactly);
-//           which dimension is which in the sum does not matter as long as the queries are laid out alike.
-//   weights go to LDS as bf16, hi + lo (rows that the heads leave free hold lo: the two products cost one), and come
-//           back as the A operand of the second product: lane (g, row) gets tokens 16g + 8s .. + 7 in step s of 2.
-//   values  lane (g, n) loads dword n (dimensions 8n .. 8n+7) of the values of tokens 16g .. 16g+15 and their scale bytes
-//           as one 16-byte load, converts them and pairs neighbouring tokens (v_perm): the B operands of eight products,
-//           product d giving dimension 8n + d.  So values are never transposed through LDS, and a scale is applied
-//           where it belongs, to the numbers of its token and group.
-struct Tile4 {
-    uint4 k[4];       // rows of tokens 4n .. 4n+3, dimensions 32g ..
-    uint32_t v[16];   // dword n of the values of tokens 16g .. 16g+15
-    uint32_t ks;      // scale bytes of the keys
-    uint4 vs;         // and of the values
-    int bad;          // not 0: some token of the block does not count
+// A wavefront's block of 64 tokens is four tiles (of a set: four times 16 rows of it), which go from the cache to registers in
+// whole lines, 16 bytes a lane (loaded in the pieces that the lanes need instead, 16 and 4 bytes of many rows, a 128K layer
+// took 37 us without any arithmetic), one block ahead, and through LDS to the lanes that need them.  Rows lie 144 bytes
+// apart there and tiles 2624, so that 16 lanes read 16 rows, and four rows of lanes four tokens, from banks of their own.
+// Lane (g, n) = (lane / 16, lane % 16); position 4n + a of the block is token 16a + n:
+//   scores  v_mfma_f32_16x16x32_bf16, A = queries (16 rows), B = the keys of tile a (column n: row n), 4 times along the
+//           dimensions.  Head number i of the segment is row 4(i%4) + i/4, so that lane (g, n) has the scores of heads g,
+//           g+4, .. in its registers 0, 1, ..: with the usual four heads every lane works on one number in the softmax.
+//           A lane takes 16 bytes of a key, its dimensions 32g .. 32g+31 under one scale byte, and converts them (two
+//           numbers an instruction, exactly); which dimension is which in the sum does not matter as long as the
+//           queries are laid out alike.
+//   weights go to LDS in order of position as bf16, hi + lo (rows that the heads leave free hold lo: the two products
+//           cost one), and come back as the A operand of the second product: lane (g, row) gets positions 16g + 8s .. + 7
+//           in step s of 2.
+//   values  lane (g, n) takes dword n (dimensions 8n .. 8n+7) of the values of those tokens, converts them and pairs
+//           neighbouring positions (v_perm): the B operands of eight products, product d giving dimension 8n + d.  A
+//           scale is applied where it belongs, to the numbers of its token and group.
+constexpr int kRowPad = kTokenBytes + 16;            // from one row to the next in LDS
+constexpr int kTilePad = 2624;                       // and from one tile to the next: 16 rows, 128 bytes of scales, 192 unused
+constexpr int kScalesAt = kTileTokens * kRowPad;
+static_assert(kScalesAt + 128 <= kTilePad && kTilePad % 256 == 64, "four tiles' rows of one number in banks of their own");
+
+struct Block {
+    uint4 row[8];    // lane: 16 bytes, number lane % 8, of rows 8j + lane / 8
+    uint4 scale;     // streaming: 16 bytes, number lane % 8, of the scales of tile lane / 8
+    uint8_t sc[8];   // gathering: the scale bytes of token `lane`
+    uint64_t bad;    // tokens that are not there, one bit each
 };
 
 constexpr int kPRow = 144;  // bytes from one row of weights in LDS to the next (64 x 2, and off the same banks)
 template <int R>
 struct SharedQ4 {
-    int32_t pre[kMaxBatch + 1];      // blocks of the requests before
     int32_t len[kMaxBatch];
-    uint32_t scan[kWaves + 1];
+    float pieces[kWaves][kSplits];   // of the sizes of a piece that are weighed
     uint16_t rmask[kMaxKvHeads];
     uint8_t rhead[kMaxKvHeads], ghead[kMaxKvHeads];
     int32_t heads[kQ4MaxGroup];      // query heads of the piece's segment
-    int32_t last;
+    int32_t last, next;
+    __align__(16) uint8_t p[kWaves][(R == 4 ? 2 : 1) * 16 * kPRow];  // weights; rows that no head writes stay zero
+    __align__(16) uint32_t row[kWaves][kQ4Block];                    // gathered tokens: tile * 16 + place
     union {
-        struct {
-            __align__(16) uint8_t p[kWaves][(R == 4 ? 2 : 1) * 16 * kPRow];
-            __align__(16) uint32_t row[kWaves][kQ4Block];       // gathered tokens: tile * 16 + place, ~0 = none
-            __align__(16) uint8_t scale[kWaves][8 * kQ4Block];  // and their scale bytes
-        };
+        __align__(16) uint8_t tile[kWaves][4 * kTilePad];
         struct {
             __align__(16) float o[kWaves][4 * R][kHeadDim];
             float ml[kWaves][4 * R][2];
@@ -179,6 +197,7 @@ struct SharedQ4 {
         struct {
             float w[4 * R][kQ4MaxWg];
             float l[4 * R];
+            __align__(16) float o[kThreads / 32][4][kHeadDim];
         } comb;
     };
 };
@@ -204,12 +223,6 @@ __device__ __forceinline__ bf16x8_t as_frag(uint32_t a, uint32_t b, uint32_t c, 
 {
     return __builtin_bit_cast(bf16x8_t, u32x4_t{a, b, c, d});
 }
-__device__ __forceinline__ float scale_of(uint32_t bytes, int i)
-{
-    const uint32_t s = i == 0 ? bytes << 23 : i == 1 ? bytes << 15 : i == 2 ? bytes << 7 : bytes >> 1;
-    return __builtin_bit_cast(float, s & 0x7F800000u);
-}
-
 // The part of a segment a wavefront works on, and where its tokens are.
 struct Seq {
     const int32_t *table;  // the request's row of the block table
@@ -217,108 +230,134 @@ struct Seq {
     const uint8_t *cache;
     int32_t len;           // tokens of the request
     int32_t n;             // tokens (entries) of the segment
+    int32_t last;          // the set's last entry
     int32_t head_tile;     // first tile of the KV head within a page
 };
 
 template <int R, bool GATHER, bool SCORES>
 struct Piece {
-    // Loads a block's tokens.  Addresses of tokens that do not count are those of some that are there.
-    static __device__ __forceinline__ void fetch(const Q4AttnArgs &a, const Seq &s, int blk, Tile4 &t, uint32_t *rows, uint8_t *scales)
+    // Streaming: page entries of 16 of the wavefront's blocks, four tiles each, one a lane (block i's tile x in lane 4i + x).
+    static __device__ __forceinline__ int fetch_entries(const Q4AttnArgs &a, const Seq &s, int lane, int blk, int end)
     {
-        const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-        const int ps = a.d.page_shift, tiles = 1 << (ps - 4);
-        if (!GATHER) {
-            const int most = max(0, (s.n - 1) / kTileTokens);  // the last tile
-            const int kt = min(blk * 4 + (n >> 2), most), vt = min(blk * 4 + g, most);
-            int kp = gload(s.table + (kt >> (ps - 4))), vp = gload(s.table + (vt >> (ps - 4)));
-            const bool k_bad = (uint32_t)kp >= (uint32_t)a.d.n_pages, v_bad = (uint32_t)vp >= (uint32_t)a.d.n_pages;
-            t.bad = (k_bad ? 1 : 0) | (v_bad ? 2 : 0);
-            kp = k_bad ? 0 : kp;
-            vp = v_bad ? 0 : vp;
-            const uint8_t *kb = s.cache + ((int64_t)kp * a.d.page_tiles + s.head_tile + (kt & (tiles - 1))) * kTileBytes;
-            const uint8_t *vb = s.cache + ((int64_t)vp * a.d.page_tiles + s.head_tile + (vt & (tiles - 1))) * kTileBytes;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) t.k[i] = gload_u4(kb + (4 * (n & 3) + i) * kTokenBytes + 16 * g);
-            t.ks = gload(reinterpret_cast<const uint32_t *>(kb + kTileScales + g * kTileTokens + 4 * (n & 3)));
-#pragma unroll
-            for (int j = 0; j < 16; ++j) t.v[j] = gload(reinterpret_cast<const uint32_t *>(vb + j * kTokenBytes + 64 + 4 * n));
-            t.vs = gload_u4(vb + kTileScales + (4 + (n >> 2)) * kTileTokens);
-        } else {
-            const int e = blk * kQ4Block + lane;
-            const int at = e < s.n ? gload(s.set + e) : -1;
-            const bool in = (uint32_t)at < (uint32_t)s.len;
-            const int tok = in ? at : 0;
-            int page = gload(s.table + (tok >> ps));
-            const bool ok = in && (uint32_t)page < (uint32_t)a.d.n_pages;
-            page = ok ? page : 0;
-            const int off = tok & ((1 << ps) - 1);
-            const uint32_t row = ((uint32_t)page * (uint32_t)a.d.page_tiles + (uint32_t)s.head_tile + (uint32_t)(off >> 4)) * 16u + (off & 15);
-            t.bad = !ok;
-            rows[lane] = row;
-            const uint8_t *sc = s.cache + (int64_t)(row >> 4) * kTileBytes + kTileScales + (row & 15);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) scales[i * kQ4Block + lane] = ok ? gload(sc + i * kTileTokens) : (uint8_t)127;
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            const uint4 kr = *reinterpret_cast<const uint4 *>(rows + 4 * n);
-            const uint32_t krow[4] = {kr.x, kr.y, kr.z, kr.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) t.k[i] = gload_u4(s.cache + (int64_t)(krow[i] + (krow[i] >> 4)) * 128 + 16 * g);
-            t.ks = *reinterpret_cast<const uint32_t *>(scales + g * kQ4Block + 4 * n);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint4 vr = *reinterpret_cast<const uint4 *>(rows + 16 * g + 4 * q);
-                const uint32_t vrow[4] = {vr.x, vr.y, vr.z, vr.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    t.v[4 * q + i] = gload(reinterpret_cast<const uint32_t *>(s.cache + (int64_t)(vrow[i] + (vrow[i] >> 4)) * 128 + 64 + 4 * n));
-            }
-            t.vs = *reinterpret_cast<const uint4 *>(scales + (4 + (n >> 2)) * kQ4Block + 16 * g);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-        }
+        const int most = max(0, (s.n - 1) / kTileTokens);
+        const int tile = min(min(blk + kWaves * (lane >> 2), end - 1) * 4 + (lane & 3), most);
+        return gload(s.table + (tile >> (a.d.page_shift - 4)));
+    }
+    static __device__ __forceinline__ int fetch_index(const Seq &s, int lane, int blk)
+    {
+        const int e = blk * kQ4Block + lane;
+        const int at = gload(s.set + min(e, s.last));
+        return e < s.n && (uint32_t)at < (uint32_t)s.len ? at : -1;
+    }
+    static __device__ __forceinline__ int fetch_page(const Q4AttnArgs &a, const Seq &s, int at)
+    {
+        return gload(s.table + (max(at, 0) >> a.d.page_shift));
     }
 
-    // Scores, weights and weighted values of a block.
-    static __device__ __forceinline__ void consume(const Q4AttnArgs &a, const Seq &s, int blk, Tile4 &t, const bf16x8_t (&qf)[4],
-                                                   float (&m)[R], float (&l)[R], f32x4_t (&o)[8], uint8_t *p, float *scores,
-                                                   float pool_scale)
+    // Loads a streamed block; entries: of fetch_entries, i: which of its blocks.  Tiles that are not there are read as some
+    // tile that is.
+    static __device__ __forceinline__ void stream(const Q4AttnArgs &a, const Seq &s, int lane, int blk, int entries, int i, Block &t)
     {
-        const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+        const int ps = a.d.page_shift, tiles = 1 << (ps - 4);
+        const uint8_t *base[4];
+        t.bad = 0;
+        if (ps >= 6) {  // (the same for the launch) a block lies in one page, all of it addressable
+            const int page = __builtin_amdgcn_readlane(entries, 4 * i);
+            const bool bad = (uint32_t)page >= (uint32_t)a.d.n_pages;
+            t.bad = bad ? ~0ull : 0ull;
+            base[0] = s.cache + ((int64_t)(bad ? 0 : page) * a.d.page_tiles + s.head_tile + ((blk * 4) & (tiles - 1))) * kTileBytes;
+#pragma unroll
+            for (int x = 1; x < 4; ++x) base[x] = base[0] + x * kTileBytes;
+        } else {
+            const int most = max(0, (s.n - 1) / kTileTokens);  // the last tile
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int page = __builtin_amdgcn_readlane(entries, 4 * i + x);
+                const bool bad = (uint32_t)page >= (uint32_t)a.d.n_pages;
+                t.bad |= bad ? 0xFFFFull << (16 * x) : 0ull;
+                base[x] = s.cache + ((int64_t)(bad ? 0 : page) * a.d.page_tiles + s.head_tile + (min(blk * 4 + x, most) & (tiles - 1))) * kTileBytes;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t.row[j] = load16(base[j >> 1] + (uint32_t)((j & 1) * 1024 + 16 * lane));
+        const int x = (lane >> 3) & 3;
+        const uint8_t *sb = x < 2 ? (x == 0 ? base[0] : base[1]) : (x == 2 ? base[2] : base[3]);
+        t.scale = load16(sb + kTileScales + 16 * (lane & 7));
+    }
+
+    // The same for a block of a set: `at` and `page` are this lane's token and its page.
+    static __device__ __forceinline__ void gather(const Q4AttnArgs &a, const Seq &s, int lane, int at, int page, Block &t, uint32_t *rows)
+    {
+        const int ps = a.d.page_shift;
+        const bool ok = at >= 0 && (uint32_t)page < (uint32_t)a.d.n_pages;
+        const int off = max(at, 0) & ((1 << ps) - 1);
+        const uint32_t row = ((uint32_t)(ok ? page : 0) * (uint32_t)a.d.page_tiles + (uint32_t)s.head_tile + (uint32_t)(off >> 4)) * 16u + (off & 15);
+        t.bad = __ballot(!ok);
+        rows[lane] = row;
+        wave_sync();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t r = rows[8 * j + (lane >> 3)];
+            t.row[j] = load16(s.cache + (int64_t)(r + (r >> 4)) * kTokenBytes + 16 * (lane & 7));
+        }
+        const uint8_t *sc = s.cache + (int64_t)(row >> 4) * kTileBytes + kTileScales + (row & 15);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t.sc[i] = gload(sc + i * kTileTokens);
+        wave_sync();
+    }
+
+    // A loaded block into the wavefront's tiles in LDS.
+    static __device__ __forceinline__ void stage(const Block &t, int lane, uint8_t *tile)
+    {
+        uint8_t *to = tile + (lane >> 3) * kRowPad + 16 * (lane & 7);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4 *>(to + (j >> 1) * kTilePad + (j & 1) * 8 * kRowPad) = t.row[j];
+        if (GATHER) {
+            uint8_t *sc = tile + (lane >> 4) * kTilePad + kScalesAt + (lane & 15);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sc[i * kTileTokens] = t.sc[i];
+        } else if (lane < 32) {
+            *reinterpret_cast<uint4 *>(tile + (lane >> 3) * kTilePad + kScalesAt + 16 * (lane & 7)) = t.scale;
+        }
+        wave_sync();
+    }
+
+    // Scores, weights and weighted values of a staged block; bad: of its Block.
+    static __device__ __forceinline__ void consume(const Q4AttnArgs &a, const Seq &s, int lane, int blk, uint64_t bad, const uint8_t *tile,
+                                                   const bf16x8_t (&qf)[4], float (&m)[R], float (&l)[R], f32x4_t (&o)[8], uint8_t *p,
+                                                   float *scores, float pool_scale)
+    {
+        const int n = lane & 15, g = lane >> 4;
         f32x4_t z[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             z[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-            const float sc = scale_of(t.ks, i);
-            const uint32_t kd[4] = {t.k[i].x, t.k[i].y, t.k[i].z, t.k[i].w};
+            const float sc = scale_of(tile[i * kTilePad + kScalesAt + g * kTileTokens + n], 0);
+            const uint4 k = *reinterpret_cast<const uint4 *>(tile + i * kTilePad + n * kRowPad + 16 * g);
+            const uint32_t kd[4] = {k.x, k.y, k.z, k.w};
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                bf16x8_t kf;
-                const auto k0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(kd[c], sc, 0);
-                const auto k1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(kd[c], sc, 1);
-                const auto k2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(kd[c], sc, 2);
-                const auto k3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(kd[c], sc, 3);
-                kf = as_frag(__builtin_bit_cast(uint32_t, k0), __builtin_bit_cast(uint32_t, k1), __builtin_bit_cast(uint32_t, k2),
-                             __builtin_bit_cast(uint32_t, k3));
-                z[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[c], kf, z[i], 0, 0, 0);
+                const uint4 x = decode8(kd[c], sc);
+                z[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[c], as_frag(x.x, x.y, x.z, x.w), z[i], 0, 0, 0);
             }
+            if (i & 1) __builtin_amdgcn_sched_barrier(0);  // (else all four tiles' conversions are made at once, and spilled)
         }
-        // which of the lane's four tokens count (all but in a segment's last block, and where pages are missing)
-        const bool part = !GATHER && (blk + 1) * kQ4Block > s.n;
-        uint32_t out_of = 0;  // bit i: token 4n + i does not count
-        uint32_t v_out = 0;   // bit j: value 16g + j does not
-        const unsigned long long any = __ballot(t.bad != 0);
-        const bool ragged = part || any != 0;
-        if (ragged) {
-            if (GATHER) {
-                out_of = (uint32_t)(any >> (4 * n)) & 15u;
-                v_out = (uint32_t)(any >> (16 * g)) & 0xFFFFu;
-            } else {
-                const int k0 = blk * kQ4Block + 4 * n, v0 = blk * kQ4Block + 16 * g;
+        uint32_t vs[4];  // scale bytes of values: tile i, tokens 4g .. 4g+3
 #pragma unroll
-                for (int i = 0; i < 4; ++i) out_of |= (k0 + i >= s.n || (t.bad & 1)) ? 1u << i : 0u;
+        for (int i = 0; i < 4; ++i)
+            vs[i] = *reinterpret_cast<const uint32_t *>(tile + i * kTilePad + kScalesAt + (4 + (n >> 2)) * kTileTokens + 4 * g);
+        // Tokens that do not count (behind a segment's last, or without a page): their scores are -infinity, and the scales
+        // of their values 2^-127, a number, since a weight of 0 times NaN is NaN.
+        if (!GATHER && (blk + 1) * kQ4Block > s.n) bad |= s.n <= blk * kQ4Block ? ~0ull : ~0ull << (s.n - blk * kQ4Block);
+        if (bad != 0) {
+            asm volatile("");  // (a branch: these are many instructions, and rare)
 #pragma unroll
-                for (int j = 0; j < 16; ++j) v_out |= (v0 + j >= s.n || (t.bad & 2)) ? 1u << j : 0u;
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t b = (uint32_t)(bad >> (16 * i)) & 0xFFFFu;
+#pragma unroll
+                for (int r = 0; r < R; ++r) z[i][r] = (b >> n) & 1u ? -__builtin_inff() : z[i][r];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) vs[i] &= (b >> (4 * g + j)) & 1u ? ~(0xFFu << (8 * j)) : ~0u;
             }
         }
         if (SCORES) {
@@ -328,11 +367,10 @@ struct Piece {
                 sum[i] = z[i][0];
 #pragma unroll
                 for (int r = 1; r < R; ++r) sum[i] += z[i][r];
-                if (ragged && ((out_of >> i) & 1u)) sum[i] = -__builtin_inff();
             }
-            // (over the four rows of lanes: row g ends with the sums of tokens 4n + g)
+            // (over the four rows of lanes: row g ends with the sums of tile g, lane by lane)
             const float x = sum_halves32_pair(sum_rows16_pair(sum[0], sum[1]), sum_rows16_pair(sum[2], sum[3]));
-            const int at = blk * kQ4Block + 4 * n + g;
+            const int at = blk * kQ4Block + lane;
             if (at < s.n) gstore(scores + at, x * pool_scale);
         }
         float w[4][R];
@@ -343,7 +381,6 @@ struct Piece {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 w[i][r] = z[i][r] * a.scale_log2e;
-                if (ragged && ((out_of >> i) & 1u)) w[i][r] = -__builtin_inff();
             }
             top[r] = max16(fmaxf(fmaxf(w[0][r], w[1][r]), fmaxf(w[2][r], w[3][r])));
             raise |= top[r] > m[r];
@@ -382,28 +419,25 @@ struct Piece {
             *reinterpret_cast<uint2 *>(p + (R <= 2 ? 4 * g + R + r : 16 + 4 * g + r) * kPRow + 8 * n) =
                 make_uint2(pk_bf16(lo[0], lo[1]), pk_bf16(lo[2], lo[3]));
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        uint32_t vs[4] = {t.vs.x, t.vs.y, t.vs.z, t.vs.w};
-        if (ragged) {  // a value that does not count has weight 0: make its scale a number
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if ((v_out >> j) & 1u) vs[j >> 2] &= ~(0xFFu << (8 * (j & 3)));
-        }
+        wave_sync();
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
             const bf16x8_t pf = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t *>(p + n * kPRow + 32 * g + 16 * st));
             bf16x8_t pl;
             if (R == 4) pl = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t *>(p + (16 + n) * kPRow + 32 * g + 16 * st));
             float sc[8];
+            uint32_t v[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sc[j] = scale_of(vs[2 * st + (j >> 2)], j & 3);
+            for (int j = 0; j < 8; ++j) {  // position 16g + 8st + j: tile j % 4, row 4g + 2st + j / 4
+                sc[j] = scale_of(vs[j & 3], 2 * st + (j >> 2));
+                v[j] = *reinterpret_cast<const uint32_t *>(tile + (j & 3) * kTilePad + (4 * g + 2 * st + (j >> 2)) * kRowPad + 64 + 4 * n);
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 uint32_t c[8], even[4], odd[4];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const uint32_t x = t.v[8 * st + j];
+                    const uint32_t x = v[j];
                     c[j] = __builtin_bit_cast(uint32_t, i == 0   ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, sc[j], 0)
                                                         : i == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, sc[j], 1)
                                                         : i == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, sc[j], 2)
@@ -421,10 +455,10 @@ struct Piece {
                     o[2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pl, ve, o[2 * i], 0, 0, 0);
                     o[2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pl, vo, o[2 * i + 1], 0, 0, 0);
                 }
+                if (i & 1) __builtin_amdgcn_sched_barrier(0);
             }
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        wave_sync();
     }
 
     // Blocks [b0, b0 + nb) of a segment with `heads` heads (sh.heads).  slot < 0: the piece is the whole segment and writes the
@@ -433,6 +467,15 @@ struct Piece {
                                                SharedQ4<R> &sh)
     {
         const int tid = fresh_tid(), lane = tid & 63, wave = uni(tid >> 6), n = lane & 15, g = lane >> 4;
+        const int end = b0 + nb;
+        int blk = b0 + wave;
+        int entries = 0, at = 0, at2 = 0, page = 0;
+        if (GATHER) {
+            at = fetch_index(s, lane, min(blk, end - 1));
+            at2 = fetch_index(s, lane, min(blk + kWaves, end - 1));
+        } else {
+            entries = fetch_entries(a, s, lane, min(blk, end - 1), end);
+        }
         bf16x8_t qf[4];
         {
             // head number i is row 4 (i % 4) + i / 4: row n is head number (n / 4) + 4 (n % 4)
@@ -452,26 +495,40 @@ struct Piece {
 #pragma unroll
         for (int d = 0; d < 8; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         uint8_t *p = sh.p[wave];
-        // (rows of weights that no head writes stay zero)
-        for (int i = lane; i < (int)sizeof sh.p[0] / 16; i += 64) reinterpret_cast<uint4 *>(p)[i] = make_uint4(0, 0, 0, 0);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
         float *scores = SCORES ? a.scores + ((int64_t)b * a.d.n_kv_heads + g0) * a.score_stride : nullptr;
         const float pool_scale = a.scale / (float)heads;
-        const int end = b0 + nb;
-        int blk = b0 + wave;
         if (blk < end) {
-            Tile4 t0, t1;
-            fetch(a, s, blk, t0, sh.row[wave], sh.scale[wave]);
-            for (;;) {
-                fetch(a, s, min(blk + kWaves, end - 1), t1, sh.row[wave], sh.scale[wave]);
-                consume(a, s, blk, t0, qf, m, l, o, p, scores, pool_scale);
+            // One block is in flight while another is worked on; what its addresses need is loaded earlier: 16 blocks' page
+            // entries at a time, or a set's entries two blocks and their pages one block before the rows.
+            Block t;
+            uint32_t *rows = sh.row[wave];
+            uint8_t *tile = sh.tile[wave];
+            int next_entries = entries, done = 0;
+            if (GATHER) page = fetch_page(a, s, at);
+            auto fetch = [&](Block &t, int blk) {  // (blocks in order; behind the last one again and again)
+                if (GATHER) {
+                    const int at_now = at, page_now = page;
+                    at = at2;
+                    page = fetch_page(a, s, at);
+                    at2 = fetch_index(s, lane, min(blk + 2 * kWaves, end - 1));
+                    gather(a, s, lane, at_now, page_now, t, rows);
+                } else {
+                    stream(a, s, lane, min(blk, end - 1), entries, done & 15, t);
+                    ++done;
+                    if ((done & 15) == 8) next_entries = fetch_entries(a, s, lane, blk + 9 * kWaves, end);  // (of blocks 16, 17, ..)
+                    if ((done & 15) == 0) entries = next_entries;
+                }
+            };
+            auto step = [&]() {
+                stage(t, lane, tile);
+                const uint64_t bad = t.bad;
+                fetch(t, blk + kWaves);
+                consume(a, s, lane, blk, bad, tile, qf, m, l, o, p, scores, pool_scale);
                 blk += kWaves;
-                if (blk >= end) break;
-                fetch(a, s, min(blk + kWaves, end - 1), t0, sh.row[wave], sh.scale[wave]);
-                consume(a, s, blk, t1, qf, m, l, o, p, scores, pool_scale);
-                blk += kWaves;
-                if (blk >= end) break;
+                return blk < end;
+            };
+            fetch(t, blk);
+            while (step()) {
             }
         }
         __syncthreads();  // (the weights' rows become the sums')
@@ -526,117 +583,248 @@ struct Piece {
     }
 };
 
-// Merges the partials of a segment, slots s0 .. s0 + count - 1, into the output.
+// Merges the partials of a segment, slots s0 .. s0 + count - 1, into the output.  The weights of a head's slots are one
+// wavefront's; 32 lanes have the columns of a head, four each, and eight groups of them share its slots, of four heads at a
+// time.  The partials come from memory, 2 us away: the first ones are asked for before the weights are known, and up to 64
+// slots of up to four heads all at once.
 template <int R>
 __device__ __forceinline__ void merge(const Q4AttnArgs &a, int b, int g0, int heads, int64_t s0, int count, SharedQ4<R> &sh)
 {
-    const int tid = fresh_tid(), lane = tid & 63, wave = tid >> 6;
-    for (int h = wave; h < heads; h += kWaves) {
-        float M = -__builtin_inff();
-        for (int i = lane; i < count; i += 64) {
-            const float m = gload_f2(a.part_ml + ((s0 + i) * a.d.group + h) * 2).x;
-            sh.comb.w[h][i] = m;
-            M = fmaxf(M, m);
+    const int tid = fresh_tid(), lane = tid & 63, wave = tid >> 6, c4 = tid & 31, grp = tid >> 5;
+    constexpr int kGroups = kThreads / 32;
+    const char *po = reinterpret_cast<const char *>(uni(a.part_o + s0 * a.d.group * kHeadDim));  // (32-bit offsets from here)
+    const char *pm = reinterpret_cast<const char *>(uni(a.part_ml + s0 * a.d.group * 2));
+    auto part = [&](int i, int h) {
+        return gload_f4(reinterpret_cast<const float *>(po + (uint32_t)((min(i, count - 1) * a.d.group + min(h, heads - 1)) * kHeadDim * 4 + 16 * c4)));
+    };
+    auto weigh = [&]() {
+        for (int h = wave; h < heads; h += kWaves) {
+            float M = -__builtin_inff(), l = 0.0f;
+            for (int i = lane; i < count; i += 64)
+                M = fmaxf(M, gload_f2(reinterpret_cast<const float *>(pm + (uint32_t)((i * a.d.group + h) * 8))).x);
+            M = wave_max_f(M);
+            const float base = M == -__builtin_inff() ? 0.0f : M;
+            for (int i = lane; i < count; i += 64) {
+                const float2 ml = gload_f2(reinterpret_cast<const float *>(pm + (uint32_t)((i * a.d.group + h) * 8)));
+                const float f = fast_exp2(ml.x - base);
+                sh.comb.w[h][i] = f;
+                l = fmaf(f, ml.y, l);
+            }
+            l = sum_halves32(sum_rows16(row16_sum(l)));
+            if (lane == 0) sh.comb.l[h] = l;
         }
-        M = wave_max_f(M);
-        const float base = M == -__builtin_inff() ? 0.0f : M;
-        float l = 0.0f;
-        for (int i = lane; i < count; i += 64) {
-            const float f = fast_exp2(sh.comb.w[h][i] - base);
-            l = fmaf(f, gload_f2(a.part_ml + ((s0 + i) * a.d.group + h) * 2).y, l);
-            sh.comb.w[h][i] = f;
+        __syncthreads();
+    };
+    float4 acc[4];
+    auto add = [&](int i, int h0, const float4 (&v)[4]) {
+        if (i >= count) return;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            const float w = sh.comb.w[min(h0 + h, heads - 1)][i];
+            acc[h].x = fmaf(w, v[h].x, acc[h].x);
+            acc[h].y = fmaf(w, v[h].y, acc[h].y);
+            acc[h].z = fmaf(w, v[h].z, acc[h].z);
+            acc[h].w = fmaf(w, v[h].w, acc[h].w);
         }
-        l = sum_halves32(sum_rows16(row16_sum(l)));
-        if (lane == 0) sh.comb.l[h] = l;
+    };
+    auto clear = [&]() {
+#pragma unroll
+        for (int h = 0; h < 4; ++h) acc[h] = make_float4(0.f, 0.f, 0.f, 0.f);
+    };
+    auto finish = [&](int h0) {
+#pragma unroll
+        for (int h = 0; h < 4; ++h) reinterpret_cast<float4 *>(sh.comb.o[grp][h])[c4] = acc[h];
+        __syncthreads();
+        for (int e = tid; e < min(4, heads - h0) * kHeadDim; e += kThreads) {
+            const int h = e / kHeadDim, d = e % kHeadDim;
+            float x = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) x += sh.comb.o[i][h][d];
+            const float l = sh.comb.l[h0 + h];
+            const int64_t row = ((int64_t)b * a.d.n_kv_heads + g0) * a.d.group + sh.heads[h0 + h];
+            gstore(a.out + row * kHeadDim + d, __builtin_bit_cast(uint16_t, (__bf16)(l == 0.0f ? 0.0f : x / l)));
+        }
+        __syncthreads();
+    };
+    if (count <= 8 * kGroups && heads <= 4) {
+        float4 v[8][4];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+#pragma unroll
+            for (int h = 0; h < 4; ++h) v[u][h] = part(grp + u * kGroups, h);
+        weigh();
+        clear();
+#pragma unroll
+        for (int u = 0; u < 8; ++u) add(grp + u * kGroups, 0, v[u]);
+        finish(0);
+        return;
     }
-    __syncthreads();
-    for (int e = tid; e < heads * kHeadDim; e += kThreads) {
-        const int h = e / kHeadDim, d = e % kHeadDim;
-        const float *from = a.part_o + (s0 * a.d.group + h) * kHeadDim + d;
-        float x = 0.0f;
-#pragma unroll 16
-        for (int i = 0; i < count; ++i) x = fmaf(sh.comb.w[h][i], gload(from + (int64_t)i * a.d.group * kHeadDim), x);
-        const float l = sh.comb.l[h];
-        const int64_t row = ((int64_t)b * a.d.n_kv_heads + g0) * a.d.group + sh.heads[h];
-        gstore(a.out + row * kHeadDim + d, __builtin_bit_cast(uint16_t, (__bf16)(l == 0.0f ? 0.0f : x / l)));
+    weigh();
+#pragma unroll 1
+    for (int h0 = 0; h0 < heads; h0 += 4) {
+        clear();
+#pragma unroll 1
+        for (int i0 = grp; i0 < count; i0 += 4 * kGroups) {
+            float4 v[4][4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int h = 0; h < 4; ++h) v[u][h] = part(i0 + u * kGroups, h0 + h);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) add(i0 + u * kGroups, h0, v[u]);
+        }
+        finish(h0);
     }
-    __syncthreads();
+}
+
+// How a launch is cut into pieces.  A piece costs as much as kPieceCost blocks whatever its length (its chain of loads, its
+// merge in LDS, its partial: 4 us; a block of a wavefront's is 1.3 us, and four wavefronts work side by side), and one that
+// is not a whole segment makes another workgroup merge partials.  So segments are cut into pieces of at most `size` blocks, for
+// the size of kSplits candidates that is cheapest: where all pieces have a workgroup of their own the longest one counts,
+// else the mean and half a piece, since workgroups that are done claim the next.  Sizes start at an equal share of all
+// blocks, four at least, and are multiples of four, a block for each wavefront.
+__device__ __forceinline__ int split_size(int share, int c)  // candidate c: 1, 9/8, .. 15/8, 2, 3, 4, 6, 8, 16, 64 shares, whole segments
+{
+    if (c == kSplits - 1) return 1 << 28;
+    const int eighths = c < 8 ? 8 + c : c == 8 ? 16 : c == 9 ? 24 : c == 10 ? 32 : c == 11 ? 48 : c == 12 ? 64 : c == 13 ? 128 : 512;
+    return (int)((((int64_t)share * eighths + 31) / 32) * 4);
+}
+// Pieces of a segment of n blocks, and how many blocks each has (the last may have fewer).
+__device__ __forceinline__ int piece_blocks(int n, int size)
+{
+    if (size >= n) return n;
+    const int pieces = quot(n + size - 1, size);
+    return quot(n + pieces - 1, pieces);
+}
+__device__ __forceinline__ int piece_count(int n, int size)
+{
+    const int each = piece_blocks(n, size);
+    return quot(n + each - 1, each);
+}
+
+__device__ __forceinline__ int wave_sum(int x)
+{
+    return (int)__builtin_amdgcn_readlane((int)wave_scan((uint32_t)x), 63);
 }
 
 template <int R, bool SETS, bool SCORES>
 __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(Q4AttnArgs a)
 {
     __shared__ SharedQ4<R> sh;
-    const int tid = threadIdx.x, B = a.d.batch, H = a.d.n_kv_heads;
-    if (tid < kMaxKvHeads) {
-        sh.rmask[tid] = a.rmask[tid];
-        sh.rhead[tid] = a.rhead[tid];
-        sh.ghead[tid] = a.ghead[tid];
-    }
+    const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), B = a.d.batch, H = a.d.n_kv_heads;
+    // Every wavefront works out the whole cut for itself: lane i has requests i * each .. i * each + each - 1.  (Loops that
+    // are not unrolled: a launch's instructions come from memory, and most have one request a lane.)
+    const int each = (B + 63) >> 6;
+    sh.rmask[lane] = a.rmask[lane];  // (here and below: every wavefront writes the same, and needs no barrier)
+    sh.rhead[lane] = a.rhead[lane];
+    sh.ghead[lane] = a.ghead[lane];
+    static_assert(kMaxKvHeads == 64, "a lane each");
+    for (int i = lane; i < (int)sizeof sh.p[0] / 16; i += 64) reinterpret_cast<uint4 *>(sh.p[wave])[i] = make_uint4(0, 0, 0, 0);
+    // (an empty segment is one block of tokens that do not count: its outputs are zero like any other's)
+    auto blocks_of = [&](int n) { return max(1, (n + kQ4Block - 1) / kQ4Block); };
+    auto set_blocks = [&](int n) { return blocks_of(min(n, a.d.k)); };
+    const int first = lane * each, last = min(first + each, B);
     int blocks = 0;
-    if (tid < B) {
-        const int L = clamp_tokens(gload(a.lengths + tid), a.d.max_len);
-        sh.len[tid] = L;
-        // (an empty segment is one block of tokens that do not count: its outputs are zero like any other's)
-        blocks = a.n_rseg * max(1, (L + kQ4Block - 1) / kQ4Block) + a.n_gseg * max(1, (min(L, a.d.k) + kQ4Block - 1) / kQ4Block);
+#pragma unroll 1
+    for (int r = first; r < last; ++r) {
+        const int L = clamp_tokens(gload(a.lengths + r), a.d.max_len);
+        sh.len[r] = L;  // (by every wavefront, the same)
+        blocks += a.n_rseg * blocks_of(L) + (SETS ? a.n_gseg * set_blocks(L) : 0);
     }
-    uint32_t total;
-    const uint32_t upto = block_scan((uint32_t)blocks, sh.scan, total);
-    if (tid < B) sh.pre[tid] = (int32_t)upto - blocks;
-    if (tid == 0) sh.pre[B] = (int32_t)total;
-    __syncthreads();
-    const int T = uni((int)total);
-    const int run = max(kWaves, (T + a.n_wg - 1) / a.n_wg);
-    const int n_segs = a.n_rseg + a.n_gseg;
-    int64_t x = (int64_t)blockIdx.x * run;
-    const int64_t end = min(x + run, (int64_t)T);
-    while (x < end) {
-        const int b = uni(find_item(sh.pre, B, (int)x));
-        const int L = uni(sh.len[b]);
-        const int rb = max(1, (L + kQ4Block - 1) / kQ4Block);
-        const int gb = max(1, (min(L, a.d.k) + kQ4Block - 1) / kQ4Block);
-        const int rel = (int)x - uni(sh.pre[b]);
-        const bool gather = SETS && rel >= a.n_rseg * rb;
-        const int in = gather ? rel - a.n_rseg * rb : rel;
-        const int per = gather ? gb : rb;
-        const int si = in / per, j = in - si * per;
-        const int nb = (int)min((int64_t)(per - j), end - x);
+    const int T = wave_sum(blocks);
+    const int share = max(kWaves, quot_uni(T + a.n_wg - 1, a.n_wg));
+    const float inv_wg = __builtin_amdgcn_rcpf((float)a.n_wg);
+    wave_sync();
+    // Lane (g, c): candidate c and every fourth request; in a large batch the wavefronts share the requests as well.
+    const bool shared = B > 16;
+    const int mine_of = split_size(share, lane & (kSplits - 1)), some = min(mine_of, 1 << 20);
+    const float inv = __builtin_amdgcn_rcpf((float)some);
+    int sum = 0;
+#pragma unroll 1
+    for (int r = shared ? 4 * wave + (lane >> 4) : lane >> 4; r < B; r += shared ? 4 * kWaves : 4) {
+        const int L = sh.len[r];
+        sum += a.n_rseg * quot_by(blocks_of(L) + some - 1, some, inv, [](uint32_t v) { return v; });
+        if (SETS) sum += a.n_gseg * quot_by(set_blocks(L) + some - 1, some, inv, [](uint32_t v) { return v; });
+    }
+    float pieces = sum_halves32(sum_rows16((float)sum));  // (far fewer than 2^24)
+    if (shared) {
+        sh.pieces[wave][lane & (kSplits - 1)] = pieces;
+        __syncthreads();
+        pieces = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) pieces += sh.pieces[w][lane & (kSplits - 1)];
+    }
+    const float longest = (float)min(some, T);
+    const float cost = pieces <= (float)a.n_wg ? kPieceCost + longest : (pieces * kPieceCost + (float)T) * inv_wg + 0.5f * (kPieceCost + longest);
+    const float least = -wave_max_f(-cost);
+    const int size = uni(split_size(share, (int)__builtin_ctzll(__ballot(cost == least))));
+    int mine = 0;  // pieces of the lane's requests
+#pragma unroll 1
+    for (int r = first; r < last; ++r)
+        mine += a.n_rseg * piece_count(blocks_of(sh.len[r]), size) + (SETS ? a.n_gseg * piece_count(set_blocks(sh.len[r]), size) : 0);
+    const int upto = (int)wave_scan((uint32_t)mine);
+    const int N = __builtin_amdgcn_readlane(upto, 63);
+    for (int at = blockIdx.x; at < N;) {
+        uint32_t claimed = 0;
+        if (N > a.n_wg && tid == 0)  // (asked for now, needed when the piece is done)
+            claimed = __hip_atomic_fetch_add((LYCHEE_GLOBAL uint32_t *)a.claims, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        // the request, kind of head, KV head and part that piece `at` is
+        const int who = (int)__builtin_popcountll(__ballot(upto <= at));
+        int rel = at - __builtin_amdgcn_readlane(upto - mine, who), b = who * each, L, rp, gp = 0;
+#pragma unroll 1
+        for (;; ++b) {
+            L = uni(sh.len[b]);
+            rp = uni(piece_count(blocks_of(L), size));
+            if (SETS) gp = uni(piece_count(set_blocks(L), size));
+            const int all = a.n_rseg * rp + a.n_gseg * gp;
+            if (rel < all) break;
+            rel -= all;
+        }
+        const bool gather = SETS && rel >= a.n_rseg * rp;
+        if (gather) rel -= a.n_rseg * rp;
+        const int parts = gather ? gp : rp, per = gather ? set_blocks(L) : blocks_of(L);
+        const int si = uni(quot(rel, parts)), part = rel - si * parts;
+        const int most = uni(piece_blocks(per, size));
+        const int j = part * most, nb = min(most, per - j);
         const int g = uni((int)(gather ? sh.ghead[si] : sh.rhead[si]));
         uint32_t heads_mask = uni((uint32_t)sh.rmask[g]);
         if (gather) heads_mask = ~heads_mask & ((1u << a.d.group) - 1u);
         const int heads = __builtin_popcount(heads_mask);
         if (tid < kQ4MaxGroup && ((heads_mask >> tid) & 1u)) sh.heads[__builtin_popcount(heads_mask & ((1u << tid) - 1u))] = tid;
         __syncthreads();
-        const int seg = b * n_segs + (gather ? a.n_rseg + si : si);
-        const bool whole = nb == per;
-        const int64_t slot = whole ? -1 : (int64_t)blockIdx.x + seg;
         Seq s;
         s.table = a.table + (int64_t)b * a.d.table_stride;
         s.set = SETS ? a.idx_in + ((int64_t)b * H + g) * a.d.k : nullptr;
         s.cache = a.cache;
         s.len = L;
         s.n = gather ? min(L, a.d.k) : L;
+        s.last = a.d.k - 1;
         s.head_tile = g << (a.d.page_shift - 4);
+        const int64_t slot = parts == 1 ? -1 : at;  // (a partial's slot is the piece's number)
         if (SETS && gather) Piece<R, true, false>::run(a, s, b, g, heads, j, nb, slot, sh);
         else Piece<R, false, SCORES>::run(a, s, b, g, heads, j, nb, slot, sh);
-        if (!whole) {
-            if (tid == 0) {
+        if (tid == 0) {
+            int last = 0;
+            if (parts > 1) {
                 uint32_t *counter = a.seg_count + (((int64_t)b * H + g) * 2 + (gather ? 1 : 0)) * kLineWords;
-                const uint32_t old = __hip_atomic_fetch_add((LYCHEE_GLOBAL uint32_t *)counter, (uint32_t)nb, __ATOMIC_RELAXED,
-                                                            __HIP_MEMORY_SCOPE_AGENT);
-                sh.last = old + (uint32_t)nb == (uint32_t)per;
-                if (sh.last) gstore_through(counter, 0u);  // as every launch finds it
+                const uint32_t old = __hip_atomic_fetch_add((LYCHEE_GLOBAL uint32_t *)counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                last = old + 1 == (uint32_t)parts;
+                if (last) gstore_through(counter, 0u);  // as every launch finds it
             }
-            __syncthreads();
-            if (sh.last) {
-                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-                const int64_t s0 = x - j;  // the segment's first block
-                const int w0 = (int)(s0 / run), w1 = (int)((s0 + per - 1) / run);
-                merge<R>(a, b, g, heads, (int64_t)w0 + seg, w1 - w0 + 1, sh);
+            sh.last = last;
+            sh.next = N;
+            if (N > a.n_wg) {
+                sh.next = (int)min((int64_t)N, (int64_t)a.n_wg + claimed);
+                if ((int)claimed == N - 1) gstore_through(a.claims, 0u);  // the launch's last claim (N - n_wg are met, n_wg are not)
             }
         }
         __syncthreads();
-        x += nb;
+        if (sh.last) {
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+            merge<R>(a, b, g, heads, at - part, parts, sh);
+        }
+        at = uni(sh.next);
+        __syncthreads();
     }
 }
 
