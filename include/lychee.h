@@ -359,7 +359,8 @@ int lychee_plan_pages(lychee_ctx *ctx, const lychee_paged *paged, const int32_t 
  *   k_new, v_new   bf16, element (i, g, d) of token i at base + i*stride_tok + g*stride_head + d; the
  *                  strides are in elements, multiples of 8, both operands share them
  *   slots          int32 [n_tokens]; a token whose slot is outside [0, n_pages * page_size) is not
- *                  written.  No slot may occur twice in a call. */
+ *                  written.  No slot may occur twice in a call
+ * EUNSUPPORTED for more than about 2^28 tokens times KV heads in a call. */
 int lychee_q4_append(lychee_ctx *ctx, const lychee_paged *paged, const void *k_new, const void *v_new,
                      int64_t stride_tok, int64_t stride_head, const int32_t *slots, int32_t n_tokens, void *cache,
                      void *hip_stream);

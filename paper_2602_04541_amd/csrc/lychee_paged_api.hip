@@ -149,6 +149,7 @@ int lychee_q4_append(lychee_ctx *ctx, const lychee_paged *paged, const void *k_n
     if (n_tokens == 0) return LYCHEE_OK;
     if (!k_new || !v_new || !slots || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(slots, 4)) return LYCHEE_EINVAL;
     if (stride_tok < 0 || stride_head < 0 || stride_tok % 8 || stride_head % 8) return LYCHEE_EINVAL;
+    if (((int64_t)n_tokens + 15) / 16 * paged->n_kv_heads >= 1 << 24) return LYCHEE_EUNSUPPORTED;  // (a launch's threads are 32 bits)
     const OnDevice dev(ctx);
     if (!dev.ok) return LYCHEE_EHIP;
     const AppendArgs a{dims_of(*paged), static_cast<const uint16_t *>(k_new), static_cast<const uint16_t *>(v_new), stride_tok,

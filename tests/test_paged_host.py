@@ -139,6 +139,7 @@ def test_sizes_that_are_refused(lb):
     assert refused(lb, "lychee_plan_pages", p, n_slots=-1) == lb.EINVAL
     assert refused(lb, "lychee_q4_append", p, n=-1) == lb.EINVAL
     assert refused(lb, "lychee_q4_append", p, n=0) == lb.OK   # nothing to do, and nothing launched
+    assert refused(lb, "lychee_q4_append", p, n=2 ** 31 - 1) == lb.EUNSUPPORTED
     for stride in (-8, 4, 129):
         assert refused(lb, "lychee_q4_append", p, stride_tok=stride) == lb.EINVAL
         assert refused(lb, "lychee_q4_append", p, stride_head=stride) == lb.EINVAL
