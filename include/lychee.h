@@ -321,8 +321,7 @@ typedef struct lychee_paged {
 
 /* Pure host functions.  lychee_check_paged: validates `paged` and, if `head_type_mask` (HOST, [H_q]) is
  * given, that sparse heads come with a set.  lychee_paged_workspace_bytes: scratch of
- * lychee_q4_decode_attn and lychee_select_scores (256-byte aligned, contents don't care); 0 if
- * `paged` is invalid. */
+ * lychee_q4_decode_attn (256-byte aligned, contents don't care); 0 if `paged` is invalid. */
 int    lychee_check_paged(const lychee_paged *paged, const uint8_t *head_type_mask, int has_idx_in);
 size_t lychee_paged_workspace_bytes(const lychee_paged *paged);
 
@@ -400,7 +399,7 @@ int lychee_q4_decode_attn(lychee_ctx *ctx, const lychee_paged *paged, const void
  * must not be idx_in; score_stride >= max_pages * page_size. */
 int lychee_select_scores(lychee_ctx *ctx, const lychee_paged *paged, const float *scores, int64_t score_stride,
                          const int32_t *lengths, const uint8_t *head_type_mask, const int32_t *idx_in,
-                         int32_t *idx_out, void *workspace, size_t workspace_bytes, void *hip_stream);
+                         int32_t *idx_out, void *hip_stream);
 
 const char *lychee_strerror(int code);
 

@@ -108,7 +108,7 @@ def _load() -> ctypes.CDLL:
     lib.lychee_q4_append.argtypes = [vp, pgd, vp, vp, i64, i64, vp, i32, vp, vp]
     lib.lychee_q4_read.argtypes = [vp, pgd, vp, vp, vp, vp, vp, vp, i64, i64, i64, i32, vp]
     lib.lychee_q4_decode_attn.argtypes = [vp, pgd, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp, sz, vp]
-    lib.lychee_select_scores.argtypes = [vp, pgd, vp, i64, vp, vp, vp, vp, vp, sz, vp]
+    lib.lychee_select_scores.argtypes = [vp, pgd, vp, i64, vp, vp, vp, vp, vp]
     lib.lychee_strerror.argtypes = [ctypes.c_int]
     lib.lychee_strerror.restype = ctypes.c_char_p
     for name in EXPORTS:
@@ -380,13 +380,12 @@ class Context:
                                           workspace.numel() * workspace.element_size(), self._on(stream)),
                "lychee_q4_decode_attn")
 
-    def select_scores(self, paged: Paged, scores, lengths, head_type_mask, idx_in, idx_out, workspace,
-                      stream=None) -> None:
+    def select_scores(self, paged: Paged, scores, lengths, head_type_mask, idx_in, idx_out, stream=None) -> None:
+        """lychee_select_scores; scores [B, H_kv, row] with contiguous (b, g) rows."""
         mask, at = _mask_ptr(head_type_mask, paged.n_q_heads)
         assert _is_rows(scores)
         _check(_lib.lychee_select_scores(self._h, ctypes.byref(paged), _at(scores), scores.stride(1), _at(lengths), at,
-                                         _at(idx_in), _at(idx_out), _at(workspace),
-                                         workspace.numel() * workspace.element_size(), self._on(stream)),
+                                         _at(idx_in), _at(idx_out), self._on(stream)),
                "lychee_select_scores")
 
     # -- helpers ------------------------------------------------------------------------

@@ -238,7 +238,7 @@ int lychee_q4_decode_attn(lychee_ctx *ctx, const lychee_paged *paged, const void
 
 int lychee_select_scores(lychee_ctx *ctx, const lychee_paged *paged, const float *scores, int64_t score_stride,
                          const int32_t *lengths, const uint8_t *head_type_mask, const int32_t *idx_in, int32_t *idx_out,
-                         void *workspace, size_t workspace_bytes, void *hip_stream)
+                         void *hip_stream)
 {
     if (ctx == nullptr) return LYCHEE_EINVAL;
     int rc = check_paged(paged);
@@ -246,7 +246,6 @@ int lychee_select_scores(lychee_ctx *ctx, const lychee_paged *paged, const float
     if (!scores || !lengths || !idx_out || !aligned(scores, 4) || !aligned(lengths, 4) || !aligned(idx_in, 4) || !aligned(idx_out, 4))
         return LYCHEE_EINVAL;
     if (idx_in == idx_out) return LYCHEE_EINVAL;
-    if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < carve(*paged).total) return LYCHEE_EWORKSPACE;
     SelectArgs a;
     memset(&a, 0, sizeof a);
     a.d = dims_of(*paged);

@@ -463,8 +463,7 @@ def check_select(ctx, x, lens, k, mask=None, heads_per=2, idx=None):
     p = lb.make_paged(B, H * heads_per, H, 1, page, max(1, n // page), k)
     t = torch.from_numpy(np.ascontiguousarray(x, np.float32)).to(DEV)
     out = ints(np.full((B, H, k), 55))
-    ws = lb.alloc_paged_workspace(p)
-    ctx.select_scores(p, t, ints(lens), mask, None if idx is None else ints(idx), out, ws)
+    ctx.select_scores(p, t, ints(lens), mask, None if idx is None else ints(idx), out)
     got = out.cpu().numpy()
     for b in range(B):
         L = int(np.clip(lens[b], 0, p.max_pages * page))
@@ -571,7 +570,7 @@ def test_a_serving_loop_of_two_layers(ctx):
             m.q = draw(rng, (B, H * G, 128))
             _, sc = check_attn(ctx, m, masks[layer], sets, scores=True)
             idx = torch.from_numpy(sc).to(DEV)
-            ctx.select_scores(p, idx, d["lens"], masks[layer], None if sets is None else ints(sets), d["sets"], ws)
+            ctx.select_scores(p, idx, d["lens"], masks[layer], None if sets is None else ints(sets), d["sets"])
             got = d["sets"].cpu().numpy()
             for b in range(B):
                 for g in range(H):
@@ -606,7 +605,7 @@ def test_a_captured_step_replays_as_the_eager_calls_run(ctx):
         c.plan_pages(m.p, s["lens"], s["new"], s["table"], s["free"], s["count"], None, None, s["slots"], s["start"], s["status"])
         c.q4_append(m.p, s["kv"][:, 0], s["kv"][:, 1], s["slots"], s["cache"])
         c.q4_decode_attn(m.p, s["q"], s["cache"], s["table"], s["lens"], mask, s["idx"], s["out"], s["scores"], s["ws"])
-        c.select_scores(m.p, s["scores"], s["lens"], mask, s["idx"], s["sets"], s["ws"])
+        c.select_scores(m.p, s["scores"], s["lens"], mask, s["idx"], s["sets"])
 
     eager, held_ctx = state(), lb.Context(0)
     try:
