@@ -441,7 +441,7 @@ def _own(s):
     if "paged" not in s:  # what a program keeps beside its cache: the shape, and the workspace of its calls
         size = s["cache"].shape[0] if "cache" in s else len(s["free"]) if "free" in s else 1
         s["paged"] = lb.make_paged(c["batch"], c["q_heads"], c["kv_heads"], size, c["page"], _max_pages(c), c["k"])
-        if c["op"] in ("attn", "select"):
+        if c["op"] == "attn":
             s["ws"] = lb.alloc_paged_workspace(s["paged"], DEV)
     p = s["paged"]
     if c["op"] == "plan":
@@ -459,7 +459,7 @@ def _own(s):
         ctx.q4_read(p, s["cache"], s["table"], None, s["lens"], s["rows"][0], s["rows"][1])
         return {"k": s["rows"][0], "v": s["rows"][1]}
     if c["op"] == "select":
-        ctx.select_scores(p, s["scores"], s["lens"], s["mask"], s["sets"], s["idx"], s["ws"])
+        ctx.select_scores(p, s["scores"], s["lens"], s["mask"], s["sets"], s["idx"])
         return {"idx": s["idx"]}
     ctx.q4_decode_attn(p, s["q"], s["cache"], s["table"], s["lens"], s["mask"], s["sets"], s["out"], s["scores"], s["ws"])
     return {"out": s["out"]} if s["scores"] is None else {"out": s["out"], "scores": s["scores"]}
