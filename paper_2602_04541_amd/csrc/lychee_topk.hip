@@ -90,9 +90,11 @@ __device__ __forceinline__ void find_bin(uint32_t want, SharedTopk &sh)
 
 // A row's scores: position i * 1024 + t of the row is number i of thread t.  A NaN is -infinity; behind the row's end there are
 // NaN, which no comparison takes.  Scores are compared as they are, an instruction each; keys are for those that count.
+// (A comparison: fmaxf is free to give a signaling NaN back.)
+__device__ __forceinline__ float number(float x) { return x == x ? x : -__builtin_inff(); }
 __device__ __forceinline__ float score_at(float x, int pos, int i, int L)
 {
-    x = fmaxf(x, -__builtin_inff());
+    x = number(x);
     if ((i + 1) * kSelThreads > L) x = pos < L ? x : __builtin_nanf("");  // (uniform: a thread's last)
     return x;
 }
@@ -146,7 +148,7 @@ struct Scores<0> {  // read again
 #pragma unroll
             for (int u = 0; u < kU; ++u) v[u] = gload(q + (uint32_t)(u * kSelThreads + tid));
 #pragma unroll
-            for (int u = 0; u < kU; ++u) f(i0 + u, fmaxf(v[u], -__builtin_inff()));
+            for (int u = 0; u < kU; ++u) f(i0 + u, number(v[u]));
         }
         for (; i0 < to; i0 += 8) {
             float v[8];
@@ -184,6 +186,9 @@ __device__ __forceinline__ float score_of(uint32_t key)
     return __builtin_bit_cast(float, (key & 0x80000000u) ? key & 0x7FFFFFFFu : ~key);
 }
 constexpr uint32_t kLeastKey = 0x007FFFFFu;  // of -infinity
+// The score that bounds the keys up to this one: the key behind the negative numbers' is no score's, and as a number it would
+// be the -0 that compares equal to the +0 above it.
+__device__ __forceinline__ float score_up_to(uint32_t key) { return score_of(key == 0x7FFFFFFFu ? key - 1u : key); }
 
 // Ranks the keys in sh.list (c of them) against one another and marks the positions of the `left` largest.
 __device__ __forceinline__ void rank_list(uint32_t c, uint32_t left, SharedTopk &sh)
@@ -251,7 +256,7 @@ __device__ __forceinline__ void select_scan(const float *x, int L, int n, uint32
     for (;;) {
         const uint32_t span = hi - lo;
         shift = span < (uint32_t)kTopBins ? 0 : 20 - __builtin_clz(span);
-        const float from = score_of(lo), to = score_of(hi);
+        const float from = score_of(lo), to = score_up_to(hi);
         __syncthreads();
         // (from +0 on a score orders like its bits, -0 aside)
         if (lo >= 0x80000000u) {
@@ -276,7 +281,7 @@ __device__ __forceinline__ void select_scan(const float *x, int L, int n, uint32
     // 3 and 4, a window of positions at a time
     uint32_t at = 0, ties = 0;  // places and ties of the windows before
     // (what lies above: from lo on, if the bin is taken whole, else from the key behind hi on)
-    const float bin_lo = score_of(lo), bin_hi = score_of(hi);
+    const float bin_lo = score_of(lo), bin_hi = score_up_to(hi);
     for (int w0 = 0; w0 < L; w0 += kWindow) {
         const int from = w0 / kSelThreads, to = min(row.n, from + kWindow / kSelThreads);
         uint32_t al = 0, ah = 0, tl = 0, th = 0;  // 64 numbers' words, one a lane

@@ -513,6 +513,31 @@ def test_selection_among_equals(ctx, what):
         check_select(ctx, x, [n - 7], kk)
 
 
+@pytest.mark.parametrize("zeros", [0, 5000, 14999, 15000, 15001])
+def test_selection_at_the_edge_below_zero(ctx, zeros):
+    """The last ones taken are the smallest negative numbers there are, or the zeros above them; too many for the list."""
+    rng = np.random.default_rng(zeros)
+    n = 40000
+    x = (-rng.integers(1, 1 << 23, (1, 2, n))).astype(np.float64) * 2.0 ** -149
+    x[0, 1] = -rng.integers(1, 300, n) * 2.0 ** -149
+    at = rng.permutation(n)[:zeros]
+    x[:, :, at] = np.where(rng.random(zeros) < 0.5, 0.0, -0.0)
+    check_select(ctx, x, [n - 9], 15000)
+    x[:, :, at[:100]] = 3.0
+    check_select(ctx, x, [n], 15000)
+
+
+def test_selection_passes_over_every_kind_of_nan(ctx):
+    rng = np.random.default_rng(17)
+    for n in (5000, 20000, 140000):
+        x = rng.standard_normal((1, 2, n)).astype(np.float32)
+        bits = x.view(np.uint32)
+        bits[rng.random(x.shape) < 0.4] = 0x7F800001   # signaling
+        bits[rng.random(x.shape) < 0.2] = 0xFFFFFFFF
+        for k in (40, n // 2, n - 32):
+            check_select(ctx, x, [n], k)
+
+
 def test_selection_of_a_batch_with_kept_sets_and_empty_requests(ctx):
     rng = np.random.default_rng(4)
     B, H, n, k = 40, 3, 2048, 100
