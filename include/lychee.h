@@ -328,7 +328,9 @@ size_t lychee_paged_workspace_bytes(const lychee_paged *paged);
 /* Gives the pages of finished requests back to the pool.  The free pages are a stack: entries
  * free_pages[0 .. *free_count-1], taken and given at its end.
  *   done           uint8 [B]: not 0 = the request's pages go back, in order of the request and of its
- *                  table, and its length becomes 0
+ *                  table, and its length becomes 0.  The table's entries go back as they are, whoever
+ *                  else holds them: a page shared with another request is the caller's to take out of the
+ *                  table (an entry outside [0, n_pages) that comes back into a table is no page there)
  *   lengths, lengths_out         int32 [B]; may be one array
  *   free_pages     int32 [n_pages]; pages that do not fit any more (given back twice) are dropped
  *   free_count, free_count_out   int32 [1]; may be one word

@@ -356,8 +356,9 @@ class Context:
                "lychee_plan_pages")
 
     def q4_append(self, paged: Paged, k_new, v_new, slots, cache, stream=None) -> None:
-        """lychee_q4_append; k_new and v_new are [n_tokens, H_kv, 128] with the same strides."""
+        """lychee_q4_append; k_new and v_new are [n_tokens, H_kv, 128] with the same strides, a token for every slot."""
         assert k_new.stride() == v_new.stride() and k_new.stride(2) == 1
+        assert len(k_new) >= slots.numel() <= len(v_new)
         _check(_lib.lychee_q4_append(self._h, ctypes.byref(paged), _at(k_new), _at(v_new), k_new.stride(0),
                                      k_new.stride(1), _at(slots), slots.numel(), _at(cache), self._on(stream)),
                "lychee_q4_append")

@@ -1120,7 +1120,7 @@ const char *lychee_strerror(int code)
     switch (code) {
     case LYCHEE_OK: return "ok";
     case LYCHEE_EINVAL: return "invalid argument";
-    case LYCHEE_EUNSUPPORTED: return "unsupported shape (head_dim must be 128, at most 4 query heads per KV head, at most 64 KV heads, batch at most 256, fewer than 128 layers per step)";
+    case LYCHEE_EUNSUPPORTED: return "unsupported shape (head_dim must be 128, at most 4 query heads per KV head (16 on the 4-bit cache), at most 64 KV heads, batch at most 256, fewer than 128 layers per step, pages of 16 to 256 tokens, at most 2^24 a request)";
     case LYCHEE_EWORKSPACE: return "workspace missing, misaligned or too small";
     case LYCHEE_EHIP: return "HIP runtime error";
     case LYCHEE_EARENA: return "the context's descriptor arena is full and a captured graph still uses it: use a new context";

@@ -212,6 +212,8 @@ int lychee_q4_decode_attn(lychee_ctx *ctx, const lychee_paged *paged, const void
     const int64_t set_blocks = ((paged->k < a.d.max_len ? paged->k : a.d.max_len) + kQ4Block - 1) / kQ4Block;
     const int64_t most = (int64_t)paged->batch * (a.n_rseg * seg_blocks + a.n_gseg * set_blocks);
     if (most >= INT32_MAX / 2) return LYCHEE_EUNSUPPORTED;
+    // a pending select still reads this workspace
+    if (ctx->pending.active && ctx->pending.workspace == workspace) return LYCHEE_EINVAL;
     const OnDevice dev(ctx);
     if (!dev.ok) return LYCHEE_EHIP;
     a.q = static_cast<const uint16_t *>(q);

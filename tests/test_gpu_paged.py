@@ -361,6 +361,51 @@ def test_many_short_requests(ctx):
     check_attn(ctx, m, np.array([1, 0, 1, 0], np.uint8), m.sets(9, "short"), scores=True)
 
 
+@pytest.mark.parametrize("batch,heads", [(256, 3), (65, 6), (40, 7)])
+def test_more_pieces_than_workgroups(ctx, batch, heads):
+    """Workgroups that are done claim the next piece; every launch finds the claims at zero, whatever the last one was."""
+    rng = np.random.default_rng(batch)
+    lens = rng.integers(0, 50, batch)
+    lens[[3, batch // 2]] = [4000, 1500]   # (cut into pieces among the others)
+    m = Made(batch, lens, 2 * heads, heads, 16, k=20)
+    mask, idx = np.tile(np.array([1, 0], np.uint8), heads), m.sets(20, "wild")
+    few = Made(5, [100, 20], 4, 2, 16)
+    first = check_attn(ctx, m, mask, idx, scores=True)
+    for _ in range(2):
+        check_attn(ctx, few)
+        again = check_attn(ctx, m, mask, idx, scores=True)
+        assert (again[0] == first[0]).all() and (again[1] == first[1]).all()
+
+
+@pytest.mark.parametrize("group", [1, 3, 6, 13])
+def test_segments_of_many_partials(ctx, group):
+    m = Made(20 + group, [30011], group, 1, 64, k=11003)
+    check_attn(ctx, m, scores=True)
+    if group > 1:
+        check_attn(ctx, m, (np.arange(group) % 3 == 0).astype(np.uint8), m.sets(11003, "wild"))
+
+
+def test_the_workspace_of_a_pending_selection_is_refused(ctx):
+    lb = binding()
+    m = Made(18, [70], 4, 2, 16)
+    rng = np.random.default_rng(0)
+    q, kv = bf16(draw(rng, (1, 4, 128))), [bf16(draw(rng, (1, 2, 96, 128))) for _ in range(2)]
+    shape = lb.make_shape(1, 4, 2, 96, 16, kv[0])
+    need = max(lb.step_workspace_bytes(shape, 2), lb.paged_workspace_bytes(m.p))
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    mask, lens = np.ones(4, np.uint8), ints([96])
+    plain, late, out, idx = ints(np.zeros((1, 2, 16))), ints(np.zeros((1, 2, 16))), torch.empty_like(q), ints(m.table)
+    ctx.decode_attn(shape, q, kv[0], kv[1], mask, None, out, plain, lens, ws)
+    ctx.decode_attn_deferred(shape, q, kv[0], kv[1], mask, None, out, late, lens, ws)
+    with pytest.raises(lb.LycheeError) as e:
+        ctx.q4_decode_attn(m.p, bf16(m.q), m.cache, idx, ints(m.lens), None, None, torch.empty_like(q), None, ws)
+    assert e.value.code == lb.EINVAL
+    check_attn(ctx, m)   # (on its own workspace it runs)
+    ctx.select_flush()
+    assert (late == plain).all()
+    ctx.q4_decode_attn(m.p, bf16(m.q), m.cache, idx, ints(m.lens), None, None, torch.empty_like(q), None, ws)
+
+
 @pytest.mark.parametrize("bad", [-1, 1 << 30, -(1 << 31)])
 def test_pages_that_are_not_there_are_left_out(ctx, bad):
     m = Made(6, [200, 64, 48], 4, 1, 16, k=40)
