@@ -68,8 +68,7 @@ constexpr size_t kSyncGen = 0, kSyncApart = 128, kSyncExit = 256;  // uint32 [1 
 constexpr size_t kSyncRows = (size_t)kMaxBatch * kMaxKvHeads;  // (sequence, KV head) pairs a shape can have
 constexpr size_t kSyncThr = 8192;                               // uint64 [kSyncRows][kLineWords / 2]
 constexpr size_t kSyncPages = kSyncExit + 4 * kLineWords * (1 + kExitGroups);  // uint32: workgroups that have read a plan's inputs
-constexpr size_t kSyncClaims = kSyncPages + 4 * kLineWords;  // uint32: pieces of an attention launch on the 4-bit cache claimed
-static_assert(kSyncClaims + 4 * kLineWords <= kSyncThr, "");
+static_assert(kSyncPages + 4 * kLineWords <= kSyncThr, "");
 constexpr size_t kSyncSet = kSyncThr + kSyncRows * kLineWords * 4;  // uint32 [kSetFlagWords]
 constexpr size_t kSyncSeg = kSyncSet + kSetFlagWords * 4;  // uint32 [kSyncRows][2][kLineWords]
 constexpr size_t kSyncCount = kSyncSeg + kSyncRows * 2 * kLineWords * 4;  // int32 [3][kSyncRows][kLineWords]

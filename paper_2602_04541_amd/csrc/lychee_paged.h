@@ -15,6 +15,7 @@ constexpr int kQ4Block = 64;               // tokens a wavefront takes at a time
 constexpr int kQ4MaxGroup = 16;
 constexpr int kSplits = 16;                // sizes of a piece that an attention launch weighs
 constexpr int kPieceCost = 12;             // what a piece costs whatever its length, in blocks
+constexpr int kCutCost = 100;              // and what a cut adds where there are more pieces than workgroups
 constexpr int kQ4WgPerCu = 2;
 constexpr int kQ4MaxWg = 512;              // upper bound of an attention launch's grid
 constexpr int64_t kMaxTiles = 1 << 27;     // of a cache (292 GB)
@@ -72,7 +73,6 @@ struct Q4AttnArgs {
     float *part_o;        // [slot][group][128] un-normalised partial outputs
     float *part_ml;       // [slot][group][2]   running maximum (log2 units) and sum
     uint32_t *seg_count;  // [B * H_kv * 2][kLineWords] pieces of a segment done so far; zero between launches
-    uint32_t *claims;     // pieces claimed beyond the first of every workgroup; zero between launches
     int32_t n_wg, n_rseg, n_gseg;
     float scale, scale_log2e;
     uint16_t rmask[kMaxKvHeads];  // per KV head: bit i = query head g*group + i is a retrieval head

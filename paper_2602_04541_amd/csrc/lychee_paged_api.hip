@@ -227,7 +227,6 @@ int lychee_q4_decode_attn(lychee_ctx *ctx, const lychee_paged *paged, const void
     a.part_o = reinterpret_cast<float *>(static_cast<char *>(workspace) + w.part_o);
     a.part_ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + w.part_ml);
     a.seg_count = reinterpret_cast<uint32_t *>(ctx->sync_dev + kSyncSeg);
-    a.claims = reinterpret_cast<uint32_t *>(ctx->sync_dev + kSyncClaims);
     a.n_wg = ctx->n_cu * kQ4WgPerCu;
     if (a.n_wg > kQ4MaxWg) a.n_wg = kQ4MaxWg;
     // (a piece is four blocks at least, or a whole segment)

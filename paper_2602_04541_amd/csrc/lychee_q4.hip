@@ -138,10 +138,16 @@ __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a)
 // in one pass over the tokens with a running m and l.
 //
 // The space of work is blocks of 64 tokens of a segment, a segment being a (request, KV head, kind of head): its whole
-// sequence for retrieval heads, its set for sparse ones.  A workgroup takes a contiguous run of blocks, cut into pieces
-// where segments end; in a piece each of its four wavefronts takes every fourth block with an (m, l, o) of its own.
+// sequence for retrieval heads, its set for sparse ones.  Segments are cut into pieces (split_size), and a workgroup takes
+// one piece after another; in a piece each of its four wavefronts takes every fourth block with an (m, l, o) of its own.
 // They are merged in LDS when the piece ends; a piece that is a whole segment writes the output, others leave a partial,
 // and the workgroup that completes a segment merges its partials.
+//
+// What bounds it: 131072 tokens of 8 KV heads (142.6 MB) take 33.5 us, of which the loop has 23 (loads alone 19, 7.1 TB/s;
+// arithmetic alone 12, for four query heads a KV head), the start 5 (the cut, page entries, the first lines 2 us away) and
+// the merge of the partials 5.  64 short requests (109 MB, 15 us of reading) take 31 us, which is their longest one's, in one piece:
+// a block a wavefront takes 2 to 2.7 us, being a chain through LDS and the matrix units that two wavefronts a SIMD hide only
+// in part.  Two workgroups a CU: three need 168 registers, and spill (a fifth slower).
 //
 // A wavefront's block of 64 tokens is four tiles (of a set: four times 16 rows of it), which go from the cache to registers in
 // whole lines, 16 bytes a lane (loaded in the pieces that the lanes need instead, 16 and 4 bytes of many rows, a 128K layer
@@ -175,12 +181,14 @@ struct Block {
 constexpr int kPRow = 144;  // bytes from one row of weights in LDS to the next (64 x 2, and off the same banks)
 template <int R>
 struct SharedQ4 {
-    int32_t len[kMaxBatch];
+    __align__(16) int32_t len[kMaxBatch];
     float pieces[kWaves][kSplits];   // of the sizes of a piece that are weighed
+    uint32_t classes[kWaves][kSplits];
+    uint8_t order[kMaxBatch];        // requests, the longest first
     uint16_t rmask[kMaxKvHeads];
     uint8_t rhead[kMaxKvHeads], ghead[kMaxKvHeads];
     int32_t heads[kQ4MaxGroup];      // query heads of the piece's segment
-    int32_t last, next;
+    int32_t last;
     __align__(16) uint8_t p[kWaves][(R == 4 ? 2 : 1) * 16 * kPRow];  // weights; rows that no head writes stay zero
     __align__(16) uint32_t row[kWaves][kQ4Block];                    // gathered tokens: tile * 16 + place
     union {
@@ -675,9 +683,13 @@ __device__ __forceinline__ void merge(const Q4AttnArgs &a, int b, int g0, int he
 // How a launch is cut into pieces.  A piece costs as much as kPieceCost blocks whatever its length (its chain of loads, its
 // merge in LDS, its partial: 4 us; a block of a wavefront's is 1.3 us, and four wavefronts work side by side), and one that
 // is not a whole segment makes another workgroup merge partials.  So segments are cut into pieces of at most `size` blocks, for
-// the size of kSplits candidates that is cheapest: where all pieces have a workgroup of their own the longest one counts,
-// else the mean and half a piece, since workgroups that are done claim the next.  Sizes start at an equal share of all
-// blocks, four at least, and are multiples of four, a block for each wavefront.
+// the size of kSplits candidates that is cheapest: the longest piece counts, or where there are more pieces than workgroups,
+// their sum and what cutting adds (kCutCost a piece), if that is more.  Sizes start at an equal share of all blocks, four at
+// least, and are multiples of four, a block for each wavefront.
+// Piece number i is workgroup i's; of more pieces than workgroups, the next ones go to the workgroups in turn, forwards and
+// backwards.  Requests are numbered from the longest to the shortest: a launch's workgroups begin over some 5 us, in order, and
+// two share a CU.  64 requests of 61 to 3001 tokens 37 -> 30 us, 256 of up to 2000 27 -> 25, 200 over sets 41 -> 37 (numbered as
+// they come; claiming the next piece from a counter took as long).
 __device__ __forceinline__ int split_size(int share, int c)  // candidate c: 1, 9/8, .. 15/8, 2, 3, 4, 6, 8, 16, 64 shares, whole segments
 {
     if (c == kSplits - 1) return 1 << 28;
@@ -750,24 +762,51 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(Q4AttnArgs a)
         for (int w = 0; w < kWaves; ++w) pieces += sh.pieces[w][lane & (kSplits - 1)];
     }
     const float longest = (float)min(some, T);
-    const float cost = pieces <= (float)a.n_wg ? kPieceCost + longest : (pieces * kPieceCost + (float)T) * inv_wg + 0.5f * (kPieceCost + longest);
+    const float cut = (pieces - (float)(B * (a.n_rseg + (SETS ? a.n_gseg : 0)))) * kCutCost;
+    const float cost = fmaxf(kPieceCost + longest, pieces <= (float)a.n_wg ? 0.0f : (pieces * kPieceCost + cut + (float)T) * inv_wg + 0.5f * kPieceCost);
     const float least = -wave_max_f(-cost);
     const int size = uni(split_size(share, (int)__builtin_ctzll(__ballot(cost == least))));
+    auto pieces_of = [&](int L) { return a.n_rseg * piece_count(blocks_of(L), size) + (SETS ? a.n_gseg * piece_count(set_blocks(L), size) : 0); };
     int mine = 0;  // pieces of the lane's requests
 #pragma unroll 1
-    for (int r = first; r < last; ++r)
-        mine += a.n_rseg * piece_count(blocks_of(sh.len[r]), size) + (SETS ? a.n_gseg * piece_count(set_blocks(sh.len[r]), size) : 0);
-    const int upto = (int)wave_scan((uint32_t)mine);
+    for (int r = first; r < last; ++r) mine += pieces_of(sh.len[r]);
+    int upto = (int)wave_scan((uint32_t)mine);
     const int N = __builtin_amdgcn_readlane(upto, 63);
-    for (int at = blockIdx.x; at < N;) {
-        uint32_t claimed = 0;
-        if (N > a.n_wg && tid == 0)  // (asked for now, needed when the piece is done)
-            claimed = __hip_atomic_fetch_add((LYCHEE_GLOBAL uint32_t *)a.claims, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    // The longest requests first (in 16 classes, else as they are numbered), so that what begins late is short: thread r finds
+    // the place of request r.
+    const bool ordered = B > 16 || N > a.n_wg;
+    if (ordered) {
+        int longest_len = 1;
+#pragma unroll 1
+        for (int r = first; r < last; ++r) longest_len = max(longest_len, sh.len[r]);
+        const float part = 15.99f * __builtin_amdgcn_rcpf((float)wave_max((uint32_t)longest_len));
+        const int cls = tid < B ? max(0, 15 - (int)((float)sh.len[tid] * part)) : kSplits;
+        unsigned long long same = 0;
+        uint32_t count = 0;
+#pragma unroll
+        for (int c = 0; c < kSplits; ++c) {
+            const unsigned long long m = __ballot(cls == c);
+            same = cls == c ? m : same;
+            count = lane == c ? (uint32_t)__builtin_popcountll(m) : count;
+        }
+        if (lane < kSplits) sh.classes[wave][lane] = count;
+        __syncthreads();
+        const uint32_t x = sh.classes[lane & 3][lane >> 2];
+        const int before = __shfl((int)(wave_scan(x) - x), (cls & (kSplits - 1)) * 4 + wave);
+        if (tid < B) sh.order[before + __builtin_popcountll(same & ((1ull << lane) - 1ull))] = (uint8_t)tid;
+        __syncthreads();
+        mine = 0;
+#pragma unroll 1
+        for (int r = first; r < last; ++r) mine += pieces_of(sh.len[sh.order[r]]);
+        upto = (int)wave_scan((uint32_t)mine);
+    }
+    for (int round = 0, at = blockIdx.x; at < N; ++round, at = round * a.n_wg + (round & 1 ? a.n_wg - 1 - (int)blockIdx.x : (int)blockIdx.x)) {
         // the request, kind of head, KV head and part that piece `at` is
         const int who = (int)__builtin_popcountll(__ballot(upto <= at));
-        int rel = at - __builtin_amdgcn_readlane(upto - mine, who), b = who * each, L, rp, gp = 0;
+        int rel = at - __builtin_amdgcn_readlane(upto - mine, who), nth = who * each, b, L, rp, gp = 0;
 #pragma unroll 1
-        for (;; ++b) {
+        for (;; ++nth) {
+            b = ordered ? uni((int)sh.order[nth]) : nth;
             L = uni(sh.len[b]);
             rp = uni(piece_count(blocks_of(L), size));
             if (SETS) gp = uni(piece_count(set_blocks(L), size));
@@ -807,18 +846,12 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(Q4AttnArgs a)
                 if (last) gstore_through(counter, 0u);  // as every launch finds it
             }
             sh.last = last;
-            sh.next = N;
-            if (N > a.n_wg) {
-                sh.next = (int)min((int64_t)N, (int64_t)a.n_wg + claimed);
-                if ((int)claimed == N - 1) gstore_through(a.claims, 0u);  // the launch's last claim (N - n_wg are met, n_wg are not)
-            }
         }
         __syncthreads();
         if (sh.last) {
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
             merge<R>(a, b, g, heads, at - part, parts, sh);
         }
-        at = uni(sh.next);
         __syncthreads();
     }
 }

@@ -363,7 +363,7 @@ def test_many_short_requests(ctx):
 
 @pytest.mark.parametrize("batch,heads", [(256, 3), (65, 6), (40, 7)])
 def test_more_pieces_than_workgroups(ctx, batch, heads):
-    """Workgroups that are done claim the next piece; every launch finds the claims at zero, whatever the last one was."""
+    """Workgroups take several pieces, whose requests are ordered by length; the same bits again after another launch."""
     rng = np.random.default_rng(batch)
     lens = rng.integers(0, 50, batch)
     lens[[3, batch // 2]] = [4000, 1500]   # (cut into pieces among the others)
