@@ -143,7 +143,7 @@ __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a)
 // They are merged in LDS when the piece ends; a piece that is a whole segment writes the output, others leave a partial,
 // and the workgroup that completes a segment merges its partials.
 //
-// What bounds it: 131072 tokens of 8 KV heads (142.6 MB) take 33.5 us, of which the loop has 23 (loads alone 19, 7.1 TB/s;
+// What bounds it: 131072 tokens of 8 KV heads (142.6 MB) take 34 us, of which the loop has 23 (loads alone 19, 7.1 TB/s;
 // arithmetic alone 12, for four query heads a KV head), the start 5 (the cut, page entries, the first lines 2 us away) and
 // the merge of the partials 5.  64 short requests (109 MB, 15 us of reading) take 31 us, which is their longest one's, in one piece:
 // a block a wavefront takes 2 to 2.7 us, being a chain through LDS and the matrix units that two wavefronts a SIMD hide only

@@ -18,7 +18,7 @@
 // candidates are more than the list holds (many equal scores, sets of more than 8000) or the row is longer than the bitmap,
 // 2 and 3 go over the row itself instead, a window of the bitmap at a time (select_scan).
 //
-// Bound by one CU's work on its row: 8 rows of 33K scores take 13.9 us, 64 of up to 98K 24.9, of which the passes over the
+// Bound by one CU's work on its row: a row of 32768 scores takes 13.9 us, 64 of up to 98304 25.4, of which the passes over the
 // row have half, and the chains of barriers, prefix sums and LDS atomics the rest; the bytes are 2 us of it.  Rows shared by up
 // to 8 workgroups, whose candidates the last one selected from, took 17.9 and 45 us: what is left to the last one is as long.
 #include "lychee_device.h"
