@@ -685,12 +685,13 @@ __device__ __forceinline__ void merge(const Q4AttnArgs &a, int b, int g0, int he
 // is not a whole segment makes another workgroup merge partials.  So segments are cut into pieces of at most `size` blocks, for
 // the size of kSplits candidates that is cheapest: the longest piece counts, or where there are more pieces than workgroups,
 // their sum and what cutting adds (kCutCost a piece), if that is more: uncut, 100 requests of 100 to 8000 tokens take 78.5 us,
-// cut at 112 of their 125 blocks 82.  Sizes start at an equal share of all blocks, four at
-// least, and are multiples of four, a block for each wavefront.
+// cut at 112 of their 125 blocks 82.  Sizes start at an equal share of all blocks, four at least, and are multiples of four, a
+// block for each wavefront.
 // Piece number i is workgroup i's; of more pieces than workgroups, the next ones go to the workgroups in turn, forwards and
-// backwards.  Requests are numbered from the longest to the shortest: a launch's workgroups begin over some 5 us, in order, and
-// two share a CU.  64 requests of 61 to 3001 tokens 37 -> 30 us, 256 of up to 2000 27 -> 25, 200 over sets 41 -> 37 (numbered as
-// they come; claiming the next piece from a counter took as long).
+// backwards (claimed from a counter they took as long).  Numbers go by the kind of head, retrieval first, since sets are
+// mostly the shorter segments, and within it from the longest to the shortest request: a launch's workgroups begin over some
+// 5 us, in order, and two share a CU.  64 requests of 61 to 3001 tokens 37 -> 30 us, 256 of up to 2000 27 -> 25, 200 over sets
+// 41 -> 36, and by the kind of head 8 of 16K to 96K over sets of 2048 55.7 -> 53.6, over 4096 44.4 -> 42.3.
 __device__ __forceinline__ int split_size(int share, int c)  // candidate c: 1, 9/8, .. 15/8, 2, 3, 4, 6, 8, 16, 64 shares, whole segments
 {
     if (c == kSplits - 1) return 1 << 28;
@@ -769,12 +770,21 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(Q4AttnArgs a)
     const float cost = fmaxf(kPieceCost + longest, pieces <= (float)a.n_wg ? 0.0f : (pieces * kPieceCost + cut + (float)T) * inv_wg + 0.5f * kPieceCost);
     const float least = -wave_max_f(-cost);
     const int size = uni(split_size(share, (int)__builtin_ctzll(__ballot(cost == least))));
-    auto pieces_of = [&](int L) { return a.n_rseg * piece_count(blocks_of(L), size) + (SETS ? a.n_gseg * piece_count(set_blocks(L), size) : 0); };
-    int mine = 0;  // pieces of the lane's requests
+    // Pieces of the lane's requests, of retrieval and of sparse heads, and with those of the lanes before.
+    int r_mine, g_mine, r_upto, g_upto;
+    auto count_pieces = [&](auto request) {
+        r_mine = g_mine = g_upto = 0;
 #pragma unroll 1
-    for (int r = first; r < last; ++r) mine += pieces_of(sh.len[r]);
-    int upto = (int)wave_scan((uint32_t)mine);
-    const int N = __builtin_amdgcn_readlane(upto, 63);
+        for (int r = first; r < last; ++r) {
+            const int L = sh.len[request(r)];
+            r_mine += a.n_rseg * piece_count(blocks_of(L), size);
+            if (SETS) g_mine += a.n_gseg * piece_count(set_blocks(L), size);
+        }
+        r_upto = (int)wave_scan((uint32_t)r_mine);
+        if (SETS) g_upto = (int)wave_scan((uint32_t)g_mine);
+    };
+    count_pieces([](int r) { return r; });
+    const int n_r = __builtin_amdgcn_readlane(r_upto, 63), N = n_r + __builtin_amdgcn_readlane(g_upto, 63);
     // The longest requests first (in 16 classes, else as they are numbered), so that what begins late is short: thread r finds
     // the place of request r.
     const bool ordered = B > 16 || N > a.n_wg;
@@ -795,28 +805,24 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(Q4AttnArgs a)
         const int before = __shfl((int)(wave_scan(x) - x), (cls & (kSplits - 1)) * 4 + wave);
         if (tid < B) sh.order[before + __builtin_popcountll(same & ((1ull << lane) - 1ull))] = (uint8_t)tid;
         __syncthreads();
-        mine = 0;
-#pragma unroll 1
-        for (int r = first; r < last; ++r) mine += pieces_of(sh.len[sh.order[r]]);
-        upto = (int)wave_scan((uint32_t)mine);
+        count_pieces([&](int r) { return (int)sh.order[r]; });
     }
     for (int round = 0, at = blockIdx.x; at < N; ++round, at = round * a.n_wg + (round & 1 ? a.n_wg - 1 - (int)blockIdx.x : (int)blockIdx.x)) {
-        // the request, kind of head, KV head and part that piece `at` is
-        const int who = (int)__builtin_popcountll(__ballot(upto <= at));
-        int rel = at - __builtin_amdgcn_readlane(upto - mine, who), nth = who * each, b, L, rp, gp = 0;
+        // the kind of head, request, KV head and part that piece `at` is
+        const bool gather = SETS && at >= n_r;
+        const int nth = gather ? at - n_r : at, upto = gather ? g_upto : r_upto;
+        const int who = (int)__builtin_popcountll(__ballot(upto <= nth));
+        int rel = nth - __builtin_amdgcn_readlane(upto - (gather ? g_mine : r_mine), who), place = who * each, b, L, per, parts;
 #pragma unroll 1
-        for (;; ++nth) {
-            b = ordered ? uni((int)sh.order[nth]) : nth;
+        for (;; ++place) {
+            b = ordered ? uni((int)sh.order[place]) : place;
             L = uni(sh.len[b]);
-            rp = uni(piece_count(blocks_of(L), size));
-            if (SETS) gp = uni(piece_count(set_blocks(L), size));
-            const int all = a.n_rseg * rp + a.n_gseg * gp;
+            per = gather ? set_blocks(L) : blocks_of(L);
+            parts = uni(piece_count(per, size));
+            const int all = parts * (gather ? a.n_gseg : a.n_rseg);
             if (rel < all) break;
             rel -= all;
         }
-        const bool gather = SETS && rel >= a.n_rseg * rp;
-        if (gather) rel -= a.n_rseg * rp;
-        const int parts = gather ? gp : rp, per = gather ? set_blocks(L) : blocks_of(L);
         const int si = uni(quot(rel, parts)), part = rel - si * parts;
         const int most = uni(piece_blocks(per, size));
         const int j = part * most, nb = min(most, per - j);
