@@ -716,3 +716,70 @@ def test_the_rows_that_were_read_serve_the_bf16_calls(ctx):
     mine = check_attn(ctx, m)[0]
     # (each is within half a bf16 step of the value and far less beside it)
     assert (np.abs(host(out) - mine) <= 2.0 ** -7 * np.abs(mine) + 1e-4).all()
+
+
+def attn_call(c, m, mask, idx):
+    """The tensors of a call on `m` and the call itself."""
+    d = dict(q=bf16(m.q), table=ints(m.table), lens=ints(m.lens), idx=ints(idx), out=torch.zeros((m.p.batch, m.p.n_q_heads, 128), dtype=torch.bfloat16, device=DEV),
+             sc=torch.zeros((m.p.batch, m.p.n_kv_heads, m.max_pages * m.p.page_size), device=DEV),
+             sets=torch.zeros((m.p.batch, m.p.n_kv_heads, m.p.k), dtype=torch.int32, device=DEV))
+
+    def run(ws):
+        c.q4_decode_attn(m.p, d["q"], m.cache, d["table"], d["lens"], mask, d["idx"], d["out"], d["sc"], ws)
+        c.select_scores(m.p, d["sc"], d["lens"], mask, d["idx"], d["sets"])
+
+    def take():
+        got = [d[n].cpu().clone() for n in ("out", "sc", "sets")]
+        for n in ("out", "sc", "sets"):
+            d[n].zero_()
+        return got
+
+    return run, take
+
+
+def two_calls(c0, c1):
+    mask = np.array([1, 0, 0, 0, 0, 0, 1, 1], np.uint8)
+    big, wide = Made(31, [2500, 900], 8, 2, 64, k=200), Made(32, np.arange(20, 90, 3), 8, 2, 16, k=33)
+    pairs = [attn_call(c, m, mask, m.sets(m.p.k)) for c, m in ((c0, big), (c1, wide))]
+    want = []
+    for (run, take), m in zip(pairs, (big, wide)):
+        run(m.ws)
+        want.append(take())
+    torch.cuda.synchronize()
+    return (big, wide), pairs, want
+
+
+def test_two_contexts_on_two_streams(ctx):
+    other = binding().Context(0)
+    made, pairs, want = two_calls(ctx, other)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        for _ in range(4):
+            for (run, _), m, s in zip(pairs, made, streams):
+                with torch.cuda.stream(s):
+                    run(m.ws)
+        torch.cuda.synchronize()
+        for (_, take), w in zip(pairs, want):
+            assert all(torch.equal(a, b) for a, b in zip(take(), w))
+        torch.cuda.synchronize()
+    other.close()
+
+
+def test_two_captured_graphs_share_a_context_and_a_workspace(ctx):
+    made, pairs, want = two_calls(ctx, ctx)
+    ws = max((m.ws for m in made), key=lambda t: t.numel())
+    graphs = []
+    for run, _ in pairs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            run(ws)
+        graphs.append(g)
+    for turn in range(4):
+        for i in (0, 1, 1, 0):
+            graphs[i].replay()
+            if turn & 1:
+                pairs[1 - i][0](ws)   # (an eager call of the other between them)
+        torch.cuda.synchronize()
+        for (_, take), w in zip(pairs, want):
+            assert all(torch.equal(a, b) for a, b in zip(take(), w))
+        torch.cuda.synchronize()
