@@ -253,9 +253,9 @@ int lychee_select_scores(lychee_ctx *ctx, const lychee_paged *paged, const float
     if (score_stride < a.d.max_len) return LYCHEE_EINVAL;
     for (int g = 0; g < paged->n_kv_heads; ++g) {
         bool any = head_type_mask == nullptr;
-        for (int i = 0; i < a.d.group && !any; ++i) {
+        for (int i = 0; i < a.d.group && head_type_mask != nullptr; ++i) {
             if (head_type_mask[g * a.d.group + i] > 1) return LYCHEE_EINVAL;
-            any = head_type_mask[g * a.d.group + i] != 0;
+            any |= head_type_mask[g * a.d.group + i] != 0;
         }
         if (any) a.selects |= 1ull << g;
         else if (idx_in == nullptr) return LYCHEE_EINVAL;

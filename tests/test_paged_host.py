@@ -134,6 +134,17 @@ def test_workspace_and_scores_are_checked(lb, name):
     assert refused(lb, name, p, mask=bad.ctypes.data) == lb.EINVAL
 
 
+@pytest.mark.parametrize("name", ["lychee_q4_decode_attn", "lychee_select_scores"])
+@pytest.mark.parametrize("at", range(1, 8))
+def test_every_head_type_is_checked(lb, name, at):
+    """A value that is no head type is refused wherever it stands, behind a retrieval head of its group as well."""
+    mask = np.array([1, 0, 0, 0, 1, 1, 1, 1], np.uint8)
+    mask[at] = 7
+    p = shape(lb)
+    assert lb.check_paged(p, mask) == lb.EINVAL
+    assert refused(lb, name, p, mask=mask.ctypes.data) == lb.EINVAL
+
+
 def test_sizes_that_are_refused(lb):
     p = shape(lb)
     assert refused(lb, "lychee_plan_pages", p, n_slots=-1) == lb.EINVAL
