@@ -119,7 +119,9 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PlanArgs a)
         const int b = find_item(sh.page0, B, i);
         gstore(a.table + (int64_t)b * a.d.table_stride + sh.held[b] + (i - sh.page0[b]), gload(a.free_pages + count - 1 - i));
     }
-    for (int i = blockIdx.x * kThreads + tid; i < a.n_slots; i += step) {
+    // (n_slots may be 2^31 - 1, and a step goes past that)
+    for (uint32_t at = blockIdx.x * kThreads + tid; at < (uint32_t)a.n_slots; at += step) {
+        const int i = (int)at;
         int slot = -1;
         if (i < n_tokens) {
             const int b = find_item(sh.start, B, i);

@@ -446,16 +446,16 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a)
     const int g = blockIdx.x % a.d.n_kv_heads, b = blockIdx.x / a.d.n_kv_heads;
     const int64_t r = (int64_t)b * a.d.n_kv_heads + g;
     int32_t *out = a.idx_out + r * a.d.k;
-    const int k = a.d.k;
+    const int k = a.d.k;  // (up to 2^31 - 1: loops up to it step past an int's range)
     if (!((a.selects >> g) & 1ull)) {
         const int32_t *in = a.idx_in + r * k;
-        for (int i = tid; i < k; i += kSelThreads) gstore(out + i, gload(in + i));
+        for (uint32_t i = tid; i < (uint32_t)k; i += kSelThreads) gstore(out + i, gload(in + i));
         return;
     }
     int L = uni(gload(a.lengths + b));
     L = L < 0 ? 0 : (L > a.d.max_len ? a.d.max_len : L);
     const int n = min(k, L);
-    for (int i = n + tid; i < k; i += kSelThreads) gstore(out + i, -1);
+    for (uint32_t i = n + tid; i < (uint32_t)k; i += kSelThreads) gstore(out + i, -1);
     if (n == L) {
         for (int i = tid; i < n; i += kSelThreads) gstore(out + i, i);
         return;

@@ -594,6 +594,39 @@ def test_selection_of_a_batch_with_kept_sets_and_empty_requests(ctx):
     check_select(ctx, x, lens, k, mask, idx=rng.integers(-5, 5000, (B, H, k)))
 
 
+# ------------------------------------------------------------------ counts that an int just holds
+
+
+def test_a_set_and_a_copied_set_of_the_most_entries(ctx):
+    lb = binding()
+    k = 2 ** 31 - 1
+    p = lb.make_paged(1, 1, 1, 1, 16, 2, k)
+    room = torch.full((k + 2048,), 7, dtype=torch.int32, device=DEV)
+    x = torch.arange(32, dtype=torch.float32, device=DEV).view(1, 1, 32)
+    ctx.select_scores(p, x, ints([20]), None, None, room[1024:1024 + k].view(1, 1, k))
+    assert room[1024:1044].tolist() == list(range(20)) and bool((room[1044:1024 + k] == -1).all())
+    assert bool((room[:1024] == 7).all()) and bool((room[1024 + k:] == 7).all())
+    out = torch.full((k + 2048,), 9, dtype=torch.int32, device=DEV)
+    ctx.select_scores(p, x, ints([20]), np.zeros(1, np.uint8), room[1024:1024 + k].view(1, 1, k), out[1024:1024 + k].view(1, 1, k))
+    assert torch.equal(out[1024:1024 + k], room[1024:1024 + k])
+    assert bool((out[:1024] == 9).all()) and bool((out[1024 + k:] == 9).all())
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+def test_a_plan_with_room_for_the_most_slots(ctx, in_place):
+    lb = binding()
+    n, ends = 2 ** 31 - 1, 1 << 18
+    p = lb.make_paged(2, 1, 1, 8, 16, 4)
+    room = torch.full((n + 2 * ends,), 7, dtype=torch.int32, device=DEV)
+    slots = room[ends:ends + n]
+    d = [ints([0, 0]), ints([3, 1]), ints(np.full((2, 4), -1)), ints(np.arange(8)), ints([8])]
+    lo, co = (None, None) if in_place else (ints([0, 0]), ints([0]))
+    start, status = ints([7] * 3), ints([7])
+    ctx.plan_pages(p, *d, lo, co, slots, start, status)
+    assert status.tolist() == [0] and start.tolist() == [0, 3, 4] and slots[:4].tolist() == [112, 113, 114, 96]
+    assert bool((slots[4:] == -1).all()) and bool((room[:ends] == 7).all()) and bool((room[ends + n:] == 7).all())
+
+
 # ------------------------------------------------------------------ together
 
 
