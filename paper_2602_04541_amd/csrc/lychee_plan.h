@@ -205,4 +205,17 @@ LYCHEE_HD inline uint32_t merge_heads(int32_t split, int32_t part, uint32_t rmas
     return all;
 }
 
+// How the selection from scores (Eq. 2 on rows of L scores, n < L of them taken) cuts a row into groups.  Position
+// i * kTopkThreads + t of the row is number i of thread t, and a group is so many consecutive numbers of one thread: as
+// many as leave ceil(2n / kTopkThreads) groups a thread, one at least.  At least n groups hold a position, so that the n-th
+// largest of the groups' largest bounds the row's n-th: groups of one number are L > n; with more numbers in each a
+// thread has ceil(2n / kTopkThreads) groups or more, all of them but its last one whole, which are 1024 >= 2n groups if that
+// is one, 1024 + 1 > n if it is two, and else at least 2n - 1024 >= n.
+constexpr int32_t kTopkThreads = 1024;
+LYCHEE_HD inline int32_t topk_group(int32_t n, int32_t L)
+{
+    const int32_t numbers = (L + kTopkThreads - 1) / kTopkThreads, each = numbers / ((2 * n + kTopkThreads - 1) / kTopkThreads);
+    return each > 1 ? each : 1;
+}
+
 }  // namespace lychee

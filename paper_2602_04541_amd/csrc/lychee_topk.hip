@@ -2,7 +2,8 @@
 //
 // A score's key is an unsigned integer that orders like it (NaN as -infinity, -0 as 0).  One workgroup a row; thread t has
 // positions t, t + 1024, ..
-//   1  The row is cut into groups, each thread's consecutive positions, at least 2n of them where the row is long enough.
+//   1  The row is cut into groups, each thread's consecutive positions, about 2n of them where the row is long enough
+//      (topk_group).
 //      The n-th largest of the groups' largest keys is a bound that n keys at least reach, whatever the scores are, and for
 //      scores without order about 1.4 n (G groups of which n reach it hold -G ln(1 - n/G) keys above).  So only the groups'
 //      largest are counted, an eighth of an octave a bin, and the rest of the row meets one comparison a key.
@@ -18,7 +19,8 @@
 // candidates are more than the list holds (many equal scores, sets of more than 8000) or the row is longer than the bitmap,
 // 2 and 3 go over the row itself instead, a window of the bitmap at a time (select_scan).
 //
-// Bound by one CU's work on its row: a row of 32768 scores takes 13.9 us, 64 of up to 98304 25.4, of which the passes over the
+// Bound by one CU's work on its row: a row of 32768 scores takes 13.9 us for 2048 of them and 11.5 for 256 (32 without
+// step 1's bound), 64 rows of up to 98304 25.4 for 4096, of which the passes over the
 // row have half, and the chains of barriers, prefix sums and LDS atomics the rest; the bytes are 2 us of it.  Rows shared by up
 // to 8 workgroups, whose candidates the last one selected from, took 17.9 and 45 us: what is left to the last one is as long.
 #include "lychee_device.h"
@@ -27,7 +29,7 @@
 namespace lychee {
 namespace {
 
-constexpr int kSelThreads = 1024;
+constexpr int kSelThreads = kTopkThreads;
 constexpr int kSelWaves = kSelThreads / 64;
 constexpr int kTopBins = 4096;
 constexpr int kBinsEach = kTopBins / kSelThreads;  // bins a thread adds up
@@ -326,8 +328,7 @@ __device__ __forceinline__ void select_row(const float *x, int L, int n, int32_t
     const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
     const Scores<E> row(x, L, tid);
     // 1: groups of `each` scores
-    const int want = (2 * n + kSelThreads - 1) / kSelThreads;
-    const int each = max(1, row.n / want);
+    const int each = topk_group(n, L);
     {
         float m = __builtin_nanf(""), most = m;
         int left = each;
@@ -344,15 +345,9 @@ __device__ __forceinline__ void select_row(const float *x, int L, int n, int32_t
         if (lane == 0) sh.top[wave] = top;
     }
     __syncthreads();
-    // (empty groups: of a row's last positions.  Where the others may be fewer than n, they bound nothing.)
-    const int groups = ((row.n + each - 1) / each) * kSelThreads;
-    uint32_t lo = kLeastKey, hi = wave_max(sh.top[lane & (kSelWaves - 1)]);
-    if (groups - kSelThreads >= n) {
-        find_bin((uint32_t)n, sh);
-        lo = max(kLeastKey, sh.bin << 20);
-    } else {
-        for (int i = tid; i < kTopBins; i += kSelThreads) sh.hist[i] = 0;
-    }
+    uint32_t hi = wave_max(sh.top[lane & (kSelWaves - 1)]);
+    find_bin((uint32_t)n, sh);  // (at least n groups have been counted: topk_group)
+    uint32_t lo = max(kLeastKey, sh.bin << 20);
     // 2: the candidates.  A thread marks its own in a word, 32 positions at a time, and the wavefront's go into its list at a
     // prefix sum of their numbers; then they are dealt to its lanes.  (With a branch for every 64 scores that hold a candidate,
     // and nearly all do, a row of 98K took 17 us here.)  A bound of -infinity leaves out nothing.

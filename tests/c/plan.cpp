@@ -53,6 +53,8 @@ extern "C" int32_t threshold_alone(int32_t n, int32_t L, int32_t r_blocks, int32
     return lychee::threshold_alone(n, L, r_blocks, n_wg, margin, fits);
 }
 
+extern "C" int32_t topk_group(int32_t n, int32_t L) { return lychee::topk_group(n, L); }
+
 extern "C" int32_t merge_split(int32_t kv_heads, int32_t group, int32_t any_sparse, int32_t others, int32_t slots, int32_t n_wg)
 {
     return lychee::merge_split(kv_heads, group, any_sparse != 0, others, slots, n_wg);

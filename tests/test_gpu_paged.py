@@ -530,6 +530,22 @@ def test_selection_by_size(ctx, L, k):
     check_select(ctx, x, [L, max(0, L - 13)], k)
 
 
+@pytest.mark.parametrize("L", [1025, 2049, 8192, 8195, 33000, 131072, 140000])
+@pytest.mark.parametrize("k", [1, 2, 16, 255, 256, 512, 513, 1024])
+def test_selection_of_few(ctx, L, k):
+    """Sets of up to one entry a thread: rows without order, rows whose high scores are all one thread's (a stride of 1024), or
+    one wavefront's, more of them than are taken and than its list holds; and fewer positions than the rows are long."""
+    rng = np.random.default_rng(L + k)
+    n = -(-L // 16) * 16
+    x = rng.standard_normal((1, 4, n))
+    x[0, 1, 37::1024] += 30.0
+    x[0, 2, np.arange(n) % 1024 < 64] += 30.0
+    x[0, 3] = -np.abs(x[0, 3])
+    x[0, 3, rng.permutation(n)[:3 * k]] = 0.0
+    check_select(ctx, x, [L], k)
+    check_select(ctx, x, [k + 1], k)
+
+
 @pytest.mark.parametrize("what", ["equal", "two values", "duplicates", "steps", "extremes", "sorted", "reversed", "tiny", "planted"])
 def test_selection_among_equals(ctx, what):
     rng = np.random.default_rng(3)

@@ -227,6 +227,26 @@ def test_merges_of_a_phased_step_are_dealt_evenly(plan):
     assert splits == {0, 1, 2}
 
 
+def test_a_selection_has_a_group_for_every_entry_of_its_set(plan):
+    """At least n groups of a row of L > n scores hold a position (their largest bound the n-th largest score), whatever n and L;
+    and of longer rows about 2n do: 2n - 1024 at least, or 1024; 4n + 2048 at most."""
+    rng = random.Random(4)
+    cases = [(n, L) for n in list(range(1, 1100, 7)) + [512, 513, 1024, 1025, 2048, 4096, 8192]
+             for L in (n + 1, n + 2, 2 * n + 1, 1023, 1024, 1025, 2047, 2048, 2049, 3333, 32768, 98304, 131073, 1 << 24)]
+    cases += [(n, int(n * 2 ** rng.uniform(0, 12)) + 1) for n in (int(2 ** rng.uniform(0, 23)) for _ in range(2000))]
+    for n, L in cases:
+        if not n < L <= 1 << 24:
+            continue
+        each = plan.topk_group(n, L)
+        whole, rest = divmod(L, 1024 * each)   # groups that every thread has whole; positions of the others
+        groups = 1024 * whole + min(1024, rest)
+        assert each >= 1 and groups >= n, (n, L, each, groups)
+        if L >= max(2 * n, 2048):
+            assert groups >= min(2 * n, max(n, 2 * n - 1024)) and (each == 1 or groups >= 1024), (n, L, groups)
+        if L >= 4 * n and L >= 4096:
+            assert groups <= max(4 * n, 2048) + 2048, (n, L, groups)
+
+
 def test_no_launch_has_the_generation_of_flags_that_nobody_has_written(plan):
     """Flags start at 0 and a threshold word that was not asked for is 0: across the wrap of the 32 bits too no
     generation is, and it differs from the one before it."""
