@@ -187,40 +187,136 @@ def make_paged(batch: int, n_q_heads: int, n_kv_heads: int, n_pages: int, page_s
 
 def check_paged(paged: Paged, head_type_mask: Optional[np.ndarray] = None, has_idx_in: bool = True) -> int:
     """lychee_check_paged: returns the status code (pure host)."""
-    m = None if head_type_mask is None else np.ascontiguousarray(head_type_mask, dtype=np.uint8)
-    return _lib.lychee_check_paged(ctypes.byref(paged), None if m is None else m.ctypes.data, int(has_idx_in))
+    try:
+        m, at = _mask_ptr(head_type_mask, paged.n_q_heads, "lychee_check_paged")
+    except LycheeError as e:
+        return _lib.lychee_check_paged(ctypes.byref(paged), None, int(has_idx_in)) or e.code
+    return _lib.lychee_check_paged(ctypes.byref(paged), at, int(has_idx_in))
 
 
 def paged_workspace_bytes(paged: Paged) -> int:
     return int(_lib.lychee_paged_workspace_bytes(ctypes.byref(paged)))
 
 
-def _mask_ptr(head_type_mask, n_q_heads: int):
+# The calls of the paged 4-bit cache look at what they are given: the library sees addresses alone, and would misread a view
+# or another type, and write past a buffer that is too short.  That costs about 0.15 us a tensor (release and plan
+# together 12.3 us, 10.3 without, 14 with a function's call for every tensor), so what a call is mostly given is looked at
+# first, and what is not that gets a second look, and its message, from the functions below.
+_I32, _BF16, _F32 = torch.int32, torch.bfloat16, torch.float32
+
+
+def _refuse(call: str, name: str, t, want: str):
+    have = "%s %s strides %s on %s" % (t.dtype, list(t.shape), list(t.stride()), t.device) if isinstance(t, torch.Tensor) else type(t).__name__
+    raise LycheeError(EINVAL, "%s: %s is %s, not %s; it" % (call, name, have, want))
+
+
+def _mask_ptr(head_type_mask, n_q_heads: int, call: str):
     """The host array of head types and its address (None: every head is a retrieval head)."""
     if head_type_mask is None:
         return None, None
-    m = np.ascontiguousarray(head_type_mask, dtype=np.uint8)
-    assert m.shape == (n_q_heads,)
+    given = np.asarray(head_type_mask)
+    m = np.ascontiguousarray(given, dtype=np.uint8)
+    if m.shape != (n_q_heads,) or (m is not given and not np.array_equal(m, given)):
+        raise LycheeError(EINVAL, "%s: head_type_mask is %s %s, not %d zeros and ones; it" % (call, given.dtype, list(given.shape), n_q_heads))
     return m, m.ctypes.data
 
 
-def _at(t) -> Optional[int]:
-    return None if t is None else t.data_ptr()
+def _arrays(call: str, device: int, *wanted):
+    """The addresses of (name, tensor, type, n): n entries or more that lie one behind the other.  None stays None, which the
+    library refuses where it has to."""
+    at = []
+    for name, t, dtype, n in wanted:
+        if t is None:
+            at.append(None)
+            continue
+        try:
+            if not (t.dtype is dtype and t.numel() >= n and t.is_contiguous() and t.get_device() == device):
+                _refuse(call, name, t, "a contiguous %s of %d entries on device %d" % (dtype, n, device))
+        except AttributeError:
+            _refuse(call, name, t, "a tensor")
+        at.append(t.data_ptr())
+    return at
 
 
-def _raw_stream(device: int) -> Optional[int]:
-    """torch's current stream of a device as a hipStream_t."""
-    return _current_raw_stream(device) or None
+def _on_device(t, device: int, itemsize: int) -> bool:
+    return isinstance(t, torch.Tensor) and t.element_size() == itemsize and t.get_device() == device
+
+
+def _strided(t, *row: int) -> bool:
+    """Whether the last dimensions are at least so large, and the last of them contiguous."""
+    return t.dim() >= len(row) and t.stride(-1) == 1 and all(a >= b for a, b in zip(t.shape[t.dim() - len(row):], row))
+
+
+def _table_at(call: str, t, paged: Paged, device: int) -> Optional[int]:
+    """The address of a block table: [B, >= max_pages] with rows table_stride apart, or as many entries in a row."""
+    if t is None:
+        return None
+    B, stride = paged.batch, paged.table_stride
+    if not (isinstance(t, torch.Tensor) and t.dtype is _I32 and t.shape == (B, stride) and t.is_contiguous() and t.get_device() == device):
+        n = paged.max_pages
+        ok = _on_device(t, device, 4) and t.dtype is _I32
+        if ok and t.dim() == 2:
+            ok = _strided(t, B, n) and (t.stride(0) == stride or B == 1)
+        elif ok:
+            ok = t.is_contiguous() and t.numel() >= (B - 1) * stride + n
+        if not ok:
+            _refuse(call, "block_table", t, "a torch.int32 [%d, %d] with rows %d apart on device %d" % (B, n, stride, device))
+    return t.data_ptr()
+
+
+def _cache_at(call: str, t, paged: Paged, device: int) -> Optional[int]:
+    """The address of a layer's pages: bytes in a row, or [n_pages, bytes of a page] with pages page_tiles tiles apart."""
+    if t is None:
+        return None
+    pages, apart = paged.n_pages, paged.page_tiles * Q4_TILE_BYTES
+    if not (_on_device(t, device, 1) and t.is_contiguous() and t.numel() >= pages * apart):
+        page = paged.n_kv_heads * (paged.page_size // Q4_TILE_TOKENS) * Q4_TILE_BYTES
+        ok = _on_device(t, device, 1)
+        if ok and t.is_contiguous():  # (the last of several interleaved layers ends before its last page does)
+            ok = t.numel() >= (pages - 1) * apart + page
+        elif ok:
+            ok = t.dim() == 2 and _strided(t, pages, page) and t.stride(0) == apart
+        if not ok:
+            _refuse(call, "cache", t, "%d pages of %d bytes, %d apart, on device %d" % (pages, page, apart, device))
+    return t.data_ptr()
+
+
+def _scores_at(call: str, t, paged: Paged, device: int):
+    """The address of score rows [B, H_kv, row] and their distance: row (b, g) lies (b * H_kv + g) strides behind the first, and
+    the last of them too has room for max_pages * page_size."""
+    if t is None:
+        return None, 0
+    B, H, n = paged.batch, paged.n_kv_heads, paged.max_pages * paged.page_size
+    ok = _on_device(t, device, 4) and t.dtype is _F32 and t.dim() == 3
+    if not (ok and t.is_contiguous() and t.shape[0] >= B and t.shape[1] == H and t.shape[2] >= n):
+        ok = ok and _strided(t, B, H, 0) and (B == 1 or (t.shape[1] == H and t.stride(0) == H * t.stride(1)))
+        if ok and t.shape[2] < n:  # (a view of the first positions)
+            ok = t.untyped_storage().nbytes() // 4 - t.storage_offset() >= (B * H - 1) * t.stride(1) + n
+        if not ok:
+            _refuse(call, "scores", t, "a torch.float32 [%d, %d, %d], evenly spaced rows, on device %d" % (B, H, n, device))
+    return t.data_ptr(), t.stride(1)
+
+
+def _rows_at(call: str, names, k, v, shape, device: int):
+    """The addresses of two bf16 tensors of a shape at least, with the same strides and contiguous rows, and the strides."""
+    if k is None or v is None:
+        return None, None, (0,) * len(shape)
+    ok = False
+    if _on_device(k, device, 2) and _on_device(v, device, 2):
+        strides = k.stride()
+        ok = k.dtype is _BF16 and v.dtype is _BF16 and k.shape == shape and v.shape == shape and strides[-1] == 1 and v.stride() == strides
+    if not ok:
+        for name, t in zip(names, (k, v)):
+            if not (_on_device(t, device, 2) and t.dtype is _BF16 and t.dim() == len(shape) and _strided(t, *shape)
+                    and t.stride() == k.stride()):
+                _refuse(call, name, t, "a torch.bfloat16 %s, strided like %s, on device %d" % (list(shape), names[0], device))
+        strides = k.stride()
+    return k.data_ptr(), v.data_ptr(), strides
 
 
 # (torch.cuda.current_stream builds a Stream object, 2.9 us of a call; the getter behind it takes 0.07)
 _current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
                               lambda device: torch.cuda.current_stream(device).cuda_stream)
-
-
-def _is_rows(scores) -> bool:
-    """Whether row (b, g) of [B, H_kv, n] lies (b * H_kv + g) strides behind the first."""
-    return scores.stride(2) == 1 and (scores.shape[0] == 1 or scores.stride(0) == scores.shape[1] * scores.stride(1))
 
 
 class Context:
@@ -332,62 +428,112 @@ class Context:
     # (calls of a few microseconds: what marshals their arguments is kept short)
     def _on(self, stream):
         """The stream of a call: the given one, or the current one of the context's device (not of the current device)."""
-        if stream is None:
-            return _raw_stream(self.device)
-        return _stream(stream)
+        return _current_raw_stream(self.device) if stream is None else _stream(stream)
 
     def release_pages(self, paged: Paged, done, lengths, block_table, free_pages, free_count, lengths_out=None,
                       free_count_out=None, stream=None) -> None:
-        """lychee_release_pages; lengths and count are updated in place unless outputs are given."""
-        _check(_lib.lychee_release_pages(self._h, ctypes.byref(paged), _at(done), _at(lengths), _at(block_table),
-                                         _at(free_pages), _at(free_count),
-                                         _at(lengths if lengths_out is None else lengths_out),
-                                         _at(free_count if free_count_out is None else free_count_out),
-                                         self._on(stream)), "lychee_release_pages")
+        """lychee_release_pages; lengths and count are updated in place unless outputs are given.  done: bytes or bool."""
+        B, pages, device = paged.batch, paged.n_pages, self.device
+        lengths_out = lengths if lengths_out is None else lengths_out
+        free_count_out = free_count if free_count_out is None else free_count_out
+        try:
+            fine = (done.element_size() == 1 and lengths.dtype is block_table.dtype is free_pages.dtype is free_count.dtype
+                    is lengths_out.dtype is free_count_out.dtype is _I32
+                    and done.get_device() == lengths.get_device() == block_table.get_device() == free_pages.get_device()
+                    == free_count.get_device() == lengths_out.get_device() == free_count_out.get_device() == device
+                    and done.is_contiguous() and lengths.is_contiguous() and block_table.is_contiguous()
+                    and free_pages.is_contiguous() and lengths_out.is_contiguous()
+                    and block_table.shape == (B, paged.table_stride) and lengths.numel() >= B <= lengths_out.numel()
+                    and free_pages.numel() >= pages and free_count.numel() >= 1 <= free_count_out.numel() and done.numel() >= B)
+        except AttributeError:  # (None, say)
+            fine = False
+        if fine:
+            at = (done.data_ptr(), lengths.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
+                  lengths_out.data_ptr(), free_count_out.data_ptr())
+        else:
+            call, byte = "lychee_release_pages", isinstance(done, torch.Tensor) and done.element_size() == 1
+            at = _arrays(call, device, ("done", done, done.dtype if byte else torch.uint8, B), ("lengths", lengths, _I32, B),
+                         ("free_pages", free_pages, _I32, pages), ("free_count", free_count, _I32, 1),
+                         ("lengths_out", lengths_out, _I32, B), ("free_count_out", free_count_out, _I32, 1))
+            at.insert(2, _table_at(call, block_table, paged, device))
+        _check(_lib.lychee_release_pages(self._h, paged, *at, self._on(stream)), "lychee_release_pages")
 
     def plan_pages(self, paged: Paged, lengths, new_tokens, block_table, free_pages, free_count, lengths_out,
                    free_count_out, slots, token_start, status, stream=None) -> None:
         """lychee_plan_pages; lengths_out / free_count_out None: in place."""
-        _check(_lib.lychee_plan_pages(self._h, ctypes.byref(paged), _at(lengths), _at(new_tokens), _at(block_table),
-                                      _at(free_pages), _at(free_count),
-                                      _at(lengths if lengths_out is None else lengths_out),
-                                      _at(free_count if free_count_out is None else free_count_out), _at(slots),
-                                      slots.numel(), _at(token_start), _at(status), self._on(stream)),
-               "lychee_plan_pages")
+        B, pages, device = paged.batch, paged.n_pages, self.device
+        lengths_out = lengths if lengths_out is None else lengths_out
+        free_count_out = free_count if free_count_out is None else free_count_out
+        try:
+            fine = (lengths.dtype is new_tokens.dtype is block_table.dtype is free_pages.dtype is free_count.dtype is lengths_out.dtype
+                    is free_count_out.dtype is slots.dtype is token_start.dtype is status.dtype is _I32
+                    and lengths.get_device() == new_tokens.get_device() == block_table.get_device() == free_pages.get_device()
+                    == free_count.get_device() == lengths_out.get_device() == free_count_out.get_device() == slots.get_device()
+                    == token_start.get_device() == status.get_device() == device
+                    and lengths.is_contiguous() and new_tokens.is_contiguous() and block_table.is_contiguous()
+                    and free_pages.is_contiguous() and lengths_out.is_contiguous() and slots.is_contiguous()
+                    and token_start.is_contiguous()
+                    and block_table.shape == (B, paged.table_stride) and lengths.numel() >= B <= new_tokens.numel()
+                    and lengths_out.numel() >= B < token_start.numel() and free_pages.numel() >= pages
+                    and free_count.numel() >= 1 <= free_count_out.numel() and status.numel() >= 1)
+        except AttributeError:
+            fine = False
+        if fine:
+            at = (lengths.data_ptr(), new_tokens.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
+                  lengths_out.data_ptr(), free_count_out.data_ptr(), slots.data_ptr(), slots.numel(), token_start.data_ptr(),
+                  status.data_ptr())
+        else:
+            call = "lychee_plan_pages"
+            at = _arrays(call, device, ("lengths", lengths, _I32, B), ("new_tokens", new_tokens, _I32, B),
+                         ("free_pages", free_pages, _I32, pages), ("free_count", free_count, _I32, 1),
+                         ("lengths_out", lengths_out, _I32, B), ("free_count_out", free_count_out, _I32, 1),
+                         ("slots", slots, _I32, 0), ("token_start", token_start, _I32, B + 1), ("status", status, _I32, 1))
+            at.insert(2, _table_at(call, block_table, paged, device))
+            at.insert(8, 0 if slots is None else slots.numel())
+        _check(_lib.lychee_plan_pages(self._h, paged, *at, self._on(stream)), "lychee_plan_pages")
 
     def q4_append(self, paged: Paged, k_new, v_new, slots, cache, stream=None) -> None:
         """lychee_q4_append; k_new and v_new are [n_tokens, H_kv, 128] with the same strides, a token for every slot."""
-        assert k_new.stride() == v_new.stride() and k_new.stride(2) == 1
-        assert len(k_new) >= slots.numel() <= len(v_new)
-        _check(_lib.lychee_q4_append(self._h, ctypes.byref(paged), _at(k_new), _at(v_new), k_new.stride(0),
-                                     k_new.stride(1), _at(slots), slots.numel(), _at(cache), self._on(stream)),
-               "lychee_q4_append")
+        call, device = "lychee_q4_append", self.device
+        (slot,) = _arrays(call, device, ("slots", slots, _I32, 0))
+        n = 0 if slots is None else slots.numel()
+        k, v, strides = _rows_at(call, ("k_new", "v_new"), k_new, v_new, (n, paged.n_kv_heads, paged.head_dim), device)
+        _check(_lib.lychee_q4_append(self._h, paged, k, v, strides[0], strides[1], slot, n, _cache_at(call, cache, paged, device),
+                                     self._on(stream)), call)
 
     def q4_read(self, paged: Paged, cache, block_table, first, last, k_out, v_out, stream=None) -> None:
         """lychee_q4_read; k_out and v_out are [B, H_kv, rows, 128] with the same strides."""
-        assert k_out.stride() == v_out.stride() and k_out.stride(3) == 1
-        _check(_lib.lychee_q4_read(self._h, ctypes.byref(paged), _at(cache), _at(block_table), _at(first), _at(last),
-                                   _at(k_out), _at(v_out), k_out.stride(0), k_out.stride(1), k_out.stride(2),
-                                   k_out.shape[2], self._on(stream)), "lychee_q4_read")
+        call, device, B = "lychee_q4_read", self.device, paged.batch
+        begin, end = _arrays(call, device, ("first", first, _I32, B), ("last", last, _I32, B))
+        n = k_out.shape[2] if isinstance(k_out, torch.Tensor) and k_out.dim() == 4 else 0
+        k, v, strides = _rows_at(call, ("k_out", "v_out"), k_out, v_out, (B, paged.n_kv_heads, n, paged.head_dim), device)
+        _check(_lib.lychee_q4_read(self._h, paged, _cache_at(call, cache, paged, device), _table_at(call, block_table, paged, device),
+                                   begin, end, k, v, strides[0], strides[1], strides[2], n, self._on(stream)), call)
 
     def q4_decode_attn(self, paged: Paged, q, cache, block_table, lengths, head_type_mask, idx_in, out, scores, workspace,
                        stream=None) -> None:
-        """lychee_q4_decode_attn; scores None or [B, H_kv, row] with contiguous (b, g) rows."""
-        mask, at = _mask_ptr(head_type_mask, paged.n_q_heads)
-        assert scores is None or _is_rows(scores)
-        _check(_lib.lychee_q4_decode_attn(self._h, ctypes.byref(paged), _at(q), _at(cache), _at(block_table),
-                                          _at(lengths), at, _at(idx_in), _at(out), _at(scores),
-                                          0 if scores is None else scores.stride(1), _at(workspace),
-                                          workspace.numel() * workspace.element_size(), self._on(stream)),
-               "lychee_q4_decode_attn")
+        """lychee_q4_decode_attn; q, out [B, H_q, 128]; scores None or [B, H_kv, row] with evenly spaced (b, g) rows."""
+        call, device, B, heads = "lychee_q4_decode_attn", self.device, paged.batch, paged.n_q_heads
+        mask, types = _mask_ptr(head_type_mask, heads, call)
+        n = B * heads * paged.head_dim
+        kind = workspace.dtype if isinstance(workspace, torch.Tensor) else torch.uint8
+        at_q, length, idx, at_out, ws = _arrays(
+            call, device, ("q", q, _BF16, n), ("lengths", lengths, _I32, B),
+            ("idx_in", idx_in, _I32, B * paged.n_kv_heads * paged.k), ("out", out, _BF16, n), ("workspace", workspace, kind, 0))
+        score, stride = _scores_at(call, scores, paged, device)
+        _check(_lib.lychee_q4_decode_attn(self._h, paged, at_q, _cache_at(call, cache, paged, device),
+                                          _table_at(call, block_table, paged, device), length, types, idx, at_out, score, stride, ws,
+                                          0 if ws is None else workspace.nbytes, self._on(stream)), call)
 
     def select_scores(self, paged: Paged, scores, lengths, head_type_mask, idx_in, idx_out, stream=None) -> None:
-        """lychee_select_scores; scores [B, H_kv, row] with contiguous (b, g) rows."""
-        mask, at = _mask_ptr(head_type_mask, paged.n_q_heads)
-        assert _is_rows(scores)
-        _check(_lib.lychee_select_scores(self._h, ctypes.byref(paged), _at(scores), scores.stride(1), _at(lengths), at,
-                                         _at(idx_in), _at(idx_out), self._on(stream)),
-               "lychee_select_scores")
+        """lychee_select_scores; scores [B, H_kv, row] with evenly spaced (b, g) rows."""
+        call, B = "lychee_select_scores", paged.batch
+        mask, types = _mask_ptr(head_type_mask, paged.n_q_heads, call)
+        n = B * paged.n_kv_heads * paged.k
+        length, idx, new = _arrays(call, self.device, ("lengths", lengths, _I32, B), ("idx_in", idx_in, _I32, n),
+                                   ("idx_out", idx_out, _I32, n))
+        score, stride = _scores_at(call, scores, paged, self.device)
+        _check(_lib.lychee_select_scores(self._h, paged, score, stride, length, types, idx, new, self._on(stream)), call)
 
     # -- helpers ------------------------------------------------------------------------
     def select_stats(self, stream=None):

@@ -4,6 +4,7 @@ import ctypes
 
 import numpy as np
 import pytest
+import torch
 
 from tests import paged_reference as R
 
@@ -165,6 +166,151 @@ def test_sizes_that_are_refused(lb):
     wide = shape(lb, batch=256, n_q_heads=64, n_kv_heads=64, max_pages=1 << 20)
     assert refused(lb, "lychee_q4_decode_attn", wide, stride=1 << 24) == lb.EUNSUPPORTED          # 2^32 blocks
     assert refused(lb, "lychee_select_scores", p, idx_out=A, idx_in=A) == lb.EINVAL
+
+
+# ------------------------------------------------------------------ what the binding refuses
+
+
+def bound(lb, device=-1):
+    """The binding's methods without a context: tensors of the CPU pass for the device's, and what is passed on the library
+    refuses (EINVAL, since there is no context)."""
+    c = object.__new__(lb.Context)
+    c._h, c.device = None, device
+    return c
+
+
+def ints(*size):
+    return torch.zeros(size, dtype=torch.int32)
+
+
+def half(*size):
+    return torch.zeros(size, dtype=torch.bfloat16)
+
+
+def arguments(lb, p):
+    """Tensors just large enough, by method and argument (shape(lb): 2 requests, 8 heads on 2, 10 pages of 16 tokens, 4 a
+    request, sets of 5)."""
+    pages = dict(lengths=ints(2), block_table=ints(2, 4), free_pages=ints(10), free_count=ints(1), lengths_out=ints(2),
+                 free_count_out=ints(1))
+    cache = torch.zeros((10, 2 * 2176), dtype=torch.uint8)
+    mask = np.array([1, 0, 0, 0, 1, 1, 1, 1], np.uint8)
+    kv, rows = half(7, 2, 2, 128), half(2, 2, 2, 9, 136)
+    return {
+        "release_pages": dict(done=torch.zeros(2, dtype=torch.uint8), **pages),
+        "plan_pages": dict(pages, new_tokens=ints(2), slots=ints(7), token_start=ints(3), status=ints(1)),
+        "q4_append": dict(k_new=kv[:, 0], v_new=kv[:, 1], slots=ints(7), cache=cache),
+        "q4_read": dict(cache=cache, block_table=ints(2, 4), first=ints(2), last=ints(2), k_out=rows[0, ..., :128],
+                        v_out=rows[1, ..., :128]),
+        "q4_decode_attn": dict(q=half(2, 8, 128), cache=cache, block_table=ints(2, 4), lengths=ints(2), head_type_mask=mask,
+                               idx_in=ints(2, 2, 5), out=half(2, 8, 128), scores=torch.zeros(2, 2, 64),
+                               workspace=lb.alloc_paged_workspace(p, "cpu")),
+        "select_scores": dict(scores=torch.zeros(2, 2, 64), lengths=ints(2), head_type_mask=mask, idx_in=ints(2, 2, 5),
+                              idx_out=ints(2, 2, 5)),
+    }
+
+
+METHODS = ["release_pages", "plan_pages", "q4_append", "q4_read", "q4_decode_attn", "select_scores"]
+
+
+def says(lb, p, method, args, device=-1):
+    """What the call's error says: that the library refused it (there is no context), or which argument the binding did."""
+    with pytest.raises(lb.LycheeError) as e:
+        getattr(bound(lb, device), method)(p, stream=0, **args)
+    assert e.value.code == lb.EINVAL
+    return str(e.value)
+
+
+@pytest.mark.parametrize("method", METHODS)
+def test_the_binding_looks_at_types_sizes_layout_and_device(lb, method):
+    p = shape(lb)
+    passed = "lychee_%s failed" % method
+    args = arguments(lb, p)[method]
+    assert says(lb, p, method, args).startswith(passed)
+    for name, t in args.items():
+        if name == "head_type_mask":
+            continue
+        bad = [t.to(torch.int64) if t.element_size() == 4 or name == "done" else t.to(torch.float32)]
+        if t.dim() == 1:
+            bad.append(torch.stack((t, t), 1)[:, 0] if len(t) > 1 else None)    # every other entry
+            bad.append(t[:-1] if name not in ("slots", "workspace") else None)
+        else:
+            bad.append(t.transpose(-1, -2).contiguous().transpose(-1, -2))         # rows that are columns
+            bad += [t[:-1], t.narrow(t.dim() - 1, 0, t.shape[-1] - 1).contiguous()]
+            if t.dim() == 3:
+                bad.append(t[:, :-1].contiguous())
+            if t.dim() > 2 and name not in ("k_new", "v_new", "k_out", "v_out", "scores"):
+                bad.append(torch.stack((t, t), 1)[:, 0])                           # a view of a fused tensor
+        bad = [b for b in bad if b is not None]
+        assert bad
+        if name == "workspace":
+            bad = [torch.stack((t, t), 1)[:, 0]]
+        for b in bad:
+            assert "lychee_%s: %s is" % (method, name) in says(lb, p, method, dict(args, **{name: b})), (name, b.dtype, b.shape, b.stride())
+    # a tensor of another device than the context's
+    assert says(lb, p, method, args, device=0).startswith("lychee_%s: " % method)
+    if "head_type_mask" in args:
+        for m in (np.ones(7, np.uint8), np.ones((2, 4), np.uint8), np.full(8, 256), np.full(8, 0.5), np.full(8, -1)):
+            assert "head_type_mask" in says(lb, p, method, dict(args, head_type_mask=m))
+        for m in (np.ones(8, bool), np.ones(8), [1, 0, 0, 0, 1, 1, 1, 1], None):
+            assert says(lb, p, method, dict(args, head_type_mask=m)).startswith(passed)
+
+
+def test_layouts_that_the_binding_takes(lb):
+    """Views that the calls read right: wide tables, interleaved layers, outputs of a larger batch, scores' first positions."""
+    p = shape(lb, table_stride=6, page_tiles=6)
+    a = arguments(lb, p)
+    wide, pool = ints(2, 6), torch.zeros((10, 3, 2 * 2176), dtype=torch.uint8)
+    for table in (wide, wide[:, :5], wide.view(-1), ints(3, 12)[:, :6], ints(3, 6), ints(10)):
+        ok = table.dim() == 1 or table.stride(0) == 6
+        said = says(lb, p, "q4_read", dict(a["q4_read"], block_table=table, cache=pool[:, 0]))
+        assert said.startswith("lychee_q4_read failed") if ok else "block_table is" in said, (table.shape, table.stride())
+    assert "block_table is" in says(lb, p, "q4_read", dict(a["q4_read"], block_table=ints(9), cache=pool[:, 0]))
+    for cache, ok in ((pool[:, 2], True), (pool, True), (pool.view(-1)[2 * 4352:], True), (pool.view(-1)[2 * 4352 + 1:], False),
+                      (torch.zeros((10, 2, 4352), dtype=torch.uint8)[:, 0], False), (pool.view(torch.int8)[:, 1], True)):
+        said = says(lb, p, "q4_append", dict(a["q4_append"], cache=cache))
+        assert said.startswith("lychee_q4_append failed") if ok else "cache is" in said, (cache.shape, cache.stride())
+    p, a = shape(lb), arguments(lb, shape(lb))
+    room = torch.zeros(2, 2, 80)
+    tail = torch.zeros(4 * 80 - 17)                                              # 63 positions of the last row
+    for x, ok in ((room, True), (room[..., :50], True), (torch.zeros(5, 2, 64), True), (torch.zeros(2, 3, 64), False),
+                  (torch.zeros(2, 3, 64)[:, :2], False), (tail.as_strided((2, 2, 50), (160, 80, 1)), False),
+                  (torch.zeros(2, 64), False)):
+        for method in ("q4_decode_attn", "select_scores"):
+            said = says(lb, p, method, dict(a[method], scores=x))
+            assert said.startswith("lychee_%s failed" % method) if ok else "scores is" in said, (x.shape, x.stride())
+    for method, names in (("release_pages", ("lengths_out", "free_count_out")), ("plan_pages", ("lengths_out", "free_count_out"))):
+        assert says(lb, p, method, dict(a[method], **{n: None for n in names})).startswith("lychee_%s failed" % method)
+    assert says(lb, p, "release_pages", dict(a["release_pages"], done=torch.zeros(2, dtype=torch.bool))).startswith("lychee_release_pages failed")
+    assert says(lb, p, "q4_append", dict(a["q4_append"], slots=ints(8))).startswith("lychee_q4_append: k_new is")
+    assert lb.check_paged(p, np.ones(7, np.uint8)) == lb.check_paged(p, np.full(8, 256)) == lb.EINVAL
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("method", ["release_pages", "plan_pages"])
+def test_what_the_usual_and_the_other_way_pass_on(lb, method, in_place, monkeypatch):
+    """A table that is not looked at first (a flat one) brings the call to the same arguments in the same places."""
+    passed = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: passed.append((name, args)) or 0
+
+    p = shape(lb)
+    a = arguments(lb, p)[method]
+    if in_place:
+        a.update(lengths_out=None, free_count_out=None)
+    monkeypatch.setattr(lb, "_lib", Library())
+    for table in (a["block_table"], a["block_table"].view(-1)):
+        getattr(bound(lb), method)(p, stream=0, **dict(a, block_table=table))
+    assert passed[0] == passed[1] and passed[0][0] == "lychee_" + method
+    at = {k: None if t is None else t.data_ptr() for k, t in a.items()}
+    at.update(lengths_out=at["lengths_out"] or at["lengths"], free_count_out=at["free_count_out"] or at["free_count"], n_slots=7)
+    order = {"release_pages": "done lengths block_table free_pages free_count lengths_out free_count_out",
+             "plan_pages": "lengths new_tokens block_table free_pages free_count lengths_out free_count_out slots n_slots token_start status"}
+    assert list(passed[0][1][2:-1]) == [at[n] for n in order[method].split()]
+    missing = dict(a, lengths=None, lengths_out=None)
+    getattr(bound(lb), method)(p, stream=0, **missing)   # (None goes on to the library, which refuses it)
+    assert passed[2][1][2:].count(None) == 3
 
 
 # ------------------------------------------------------------------ the reference against hand-made values
