@@ -339,7 +339,8 @@ int lychee_release_pages(lychee_ctx *ctx, const lychee_paged *paged, const uint8
                          const int32_t *block_table, int32_t *free_pages, const int32_t *free_count,
                          int32_t *lengths_out, int32_t *free_count_out, void *hip_stream);
 
-/* Block table, slots and lengths of a step in which request b gets new_tokens[b] >= 0 more tokens.
+/* Block table, slots and lengths of a step in which request b gets new_tokens[b] >= 0 more tokens (free_pages and free_count:
+ * the stack of lychee_release_pages).
  *   block_table    entries of the pages taken are written: requests in order take pages off the end of
  *                  free_pages; other entries are left as they are
  *   lengths_out    lengths[b] + new_tokens[b]; may be `lengths`.  free_count_out may be `free_count`

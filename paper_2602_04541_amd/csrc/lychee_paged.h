@@ -15,7 +15,7 @@ constexpr int kQ4Block = 64;               // tokens a wavefront takes at a time
 constexpr int kQ4MaxGroup = 16;
 constexpr int kSplits = 16;                // sizes of a piece that an attention launch weighs
 constexpr int kPieceCost = 12;             // what a piece costs whatever its length, in blocks
-constexpr int kCutCost = 160;              // and what a cut adds where there are more pieces than workgroups
+constexpr int kCutCost = 160;              // and the weight of a cut where there are more pieces than workgroups (fitted)
 constexpr int kQ4WgPerCu = 2;
 constexpr int kQ4MaxWg = 512;              // upper bound of an attention launch's grid
 constexpr int64_t kMaxTiles = 1 << 27;     // of a cache (292 GB)

@@ -143,11 +143,13 @@ __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a)
 // They are merged in LDS when the piece ends; a piece that is a whole segment writes the output, others leave a partial,
 // and the workgroup that completes a segment merges its partials.
 //
-// What bounds it: 131072 tokens of 8 KV heads (142.6 MB) take 34 us, of which the loop has 23 (loads alone 19, 7.1 TB/s;
-// arithmetic alone 12, for four query heads a KV head), the start 5 (the cut, page entries, the first lines 2 us away) and
-// the merge of the partials 5.  64 short requests (109 MB, 15 us of reading) take 31 us, which is their longest one's, in one piece:
-// a block a wavefront takes 2 to 2.7 us, being a chain through LDS and the matrix units that two wavefronts a SIMD hide only
-// in part.  Two workgroups a CU: three need 168 registers, and spill (a fifth slower).
+// What bounds it: 131072 tokens of 8 KV heads (142.6 MB) take 33.6 us (35.2 over several caches in turn, none of which the
+// last-level cache holds), of which the loop has 23 (loads alone 19, 7.1 TB/s; arithmetic alone 12, for four query heads a KV
+// head), the start 5 (the cut, page entries, the first lines 2 us away) and the merge of the partials 5.  64 short requests
+// (109 MB, 15 us of reading) take 29.3 us, which is their longest one's, in one piece: a wavefront takes 2 to 2.7 us for each
+// block of 64 tokens, being a chain through LDS and the matrix units that two wavefronts a SIMD hide only in part.  Groups of
+// 9 to 16 query heads have twice the products, and up to 16 heads' partials that one workgroup merges: 32768 tokens of two such
+// KV heads (8.9 MB) take 33 us.  Two workgroups a CU: three need 168 registers, and spill (a fifth slower).
 //
 // A wavefront's block of 64 tokens is four tiles (of a set: four times 16 rows of it), which go from the cache to registers in
 // whole lines, 16 bytes a lane (loaded in the pieces that the lanes need instead, 16 and 4 bytes of many rows, a 128K layer
@@ -160,8 +162,11 @@ __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a)
 //           A lane takes 16 bytes of a key, its dimensions 32g .. 32g+31 under one scale byte, and converts them (two
 //           numbers an instruction, exactly); which dimension is which in the sum does not matter as long as the
 //           queries are laid out alike.
-//   weights go to LDS in order of position as bf16, hi + lo (rows that the heads leave free hold lo: the two products
-//           cost one), and come back as the A operand of the second product: lane (g, row) gets positions 16g + 8s .. + 7
+//   weights go to LDS in order of position as bf16, hi + lo, off by 2^-17 of a weight at most: of one in [2^e, 2^(e+1))
+//           hi leaves up to 2^(e-8), and half a place of that in bf16 is 2^(e-17).  One bf16 number would be off by 2^-8, as
+//           much as the output's own rounding, and the matrix units' fp32 products run at a sixteenth of bf16's rate.  The
+//           sum l has the weights unrounded.  Rows that the heads leave free hold lo, so that with up to 8 heads the two
+//           products cost one.  They come back as the A operand of the second product: lane (g, row) gets positions 16g + 8s .. + 7
 //           in step s of 2.
 //   values  lane (g, n) takes dword n (dimensions 8n .. 8n+7) of the values of those tokens, converts them and pairs
 //           neighbouring positions (v_perm): the B operands of eight products, product d giving dimension 8n + d.  A
@@ -681,17 +686,25 @@ __device__ __forceinline__ void merge(const Q4AttnArgs &a, int b, int g0, int he
 }
 
 // How a launch is cut into pieces.  A piece costs as much as kPieceCost blocks whatever its length (its chain of loads, its
-// merge in LDS, its partial: 4 us; a block of a wavefront's is 1.3 us, and four wavefronts work side by side), and one that
-// is not a whole segment makes another workgroup merge partials.  So segments are cut into pieces of at most `size` blocks, for
-// the size of kSplits candidates that is cheapest: the longest piece counts, or where there are more pieces than workgroups,
-// their sum and what cutting adds (kCutCost a piece), if that is more: uncut, 100 requests of 100 to 8000 tokens take 78.5 us,
-// cut at 112 of their 125 blocks 82.  Sizes start at an equal share of all blocks, four at least, and are multiples of four, a
-// block for each wavefront.
+// merge in LDS, its partial: 5 us, in which four wavefronts take 8 to 10 blocks; 6, 9, 12 and 16 blocks give the same times
+// within their noise on the 16 shapes below), and one that is not a whole segment makes another workgroup merge partials.  So
+// segments are cut into pieces of at most `size` blocks, for the size of kSplits candidates that is cheapest: the longest piece
+// counts, or where there are more pieces than workgroups, the mean of what a workgroup has and what cutting adds, if that is
+// more.  What it adds (kCutCost a piece) is no cost that was measured but a weight that was fitted: 160 against 12 takes 64
+// requests of 61 to 3001 tokens from 36 to 31 us, 48 of 1000 to 6000 from 52 to 48, 100 of 100 to 8000 from 82 to 79, 128 of
+// 100 to 4000 from 62 to 63, and changes nothing on 12 shapes more.  The mean does not see that workgroups take whole
+// pieces, and no size is below an equal share: 65 requests of 20000 tokens of 8 KV heads are 520 segments, which are not cut, and
+// take 315 us where 64 take 216 (of 3000 tokens 57 and 40).  Sizes start at an equal share of all blocks, four at least, and
+// are multiples of four, a block for each wavefront.
 // Piece number i is workgroup i's; of more pieces than workgroups, the next ones go to the workgroups in turn, forwards and
 // backwards (claimed from a counter they took as long).  Numbers go by the kind of head, retrieval first, since sets are
 // mostly the shorter segments, and within it from the longest to the shortest request: a launch's workgroups begin over some
-// 5 us, in order, and two share a CU.  64 requests of 61 to 3001 tokens 37 -> 30 us, 256 of up to 2000 27 -> 25, 200 over sets
+// 5 us, in order, and two share a CU.  64 requests of 61 to 3001 tokens 37 -> 31 us, 256 of up to 2000 27 -> 25, 200 over sets
 // 41 -> 36, and by the kind of head 8 of 16K to 96K over sets of 2048 55.7 -> 53.6, over 4096 44.4 -> 42.3.
+// Requests are ordered by length where workgroups take several pieces or the batch is larger than 16.  Finding the order costs
+// 0.5 to 1 us (2 to 16 requests whose pieces all fit: 16.3 -> 17.1, 12.5 -> 13.3, 19.3 -> 20.2 with it); without it 60 requests
+// of 61 to 3001 tokens in 480 pieces take 36 us instead of 29.  Large batches of few pieces, which need it least, pay for that:
+// 40 requests on 2 KV heads 17 -> 18 us, 200 of up to 2000 tokens 23 -> 26.
 __device__ __forceinline__ int split_size(int share, int c)  // candidate c: 1, 9/8, .. 15/8, 2, 3, 4, 6, 8, 16, 64 shares, whole segments
 {
     if (c == kSplits - 1) return 1 << 28;
@@ -891,6 +904,9 @@ hipError_t launch_read(const ReadArgs &a, hipStream_t stream)
     return hipGetLastError();
 }
 
+// A launch is one build, by the shape's group, whatever the head types divide it into: R numbers of every lane's softmax are
+// 4R heads.  Wider than needed costs: a group of 4 at 128K takes 32.1 us with R = 1, 33.0 with 2, 36.1 with 4; a group of 8 (64
+// short requests) 31.3 with 2, 36 with 4.
 hipError_t launch_q4_attn(const Q4AttnArgs &a, hipStream_t stream)
 {
     return a.d.group <= 4 ? launch_r<1>(a, stream) : a.d.group <= 8 ? launch_r<2>(a, stream) : launch_r<4>(a, stream);

@@ -14,15 +14,15 @@
 //      of them are taken, treated like those above; or, if they are one key, they have a bitmap of their own, whose first so
 //      many count.
 //   4  A prefix sum over the bitmap's words gives every word its place in the set.
-// Rows of up to 8 positions a thread stay in registers between 1 and 2; longer ones are read again, from the L2 (with 32
-// positions a thread in registers a row of 32K took 14.3 us, read again 13.7).  Where the
-// candidates are more than the list holds (many equal scores, sets of more than 8000) or the row is longer than the bitmap,
-// 2 and 3 go over the row itself instead, a window of the bitmap at a time (select_scan).
+// Rows of up to 8 positions a thread stay in registers between 1 and 2; longer ones are read again, from the L2 (32 positions a
+// thread in registers are 0.6 us slower for a row of 32K).  Where the candidates are more than the list holds (many equal
+// scores, sets of more than 8000) or the row is longer than the bitmap, 2 and 3 go over the row itself instead, a window of the
+// bitmap at a time (select_scan): 10000 of a row of 32768 take 27 us, 16384 of 131072 68, 4096 of 262144 105.
 //
-// Bound by one CU's work on its row: a row of 32768 scores takes 13.9 us for 2048 of them and 11.5 for 256 (32 without
-// step 1's bound), 64 rows of up to 98304 25.4 for 4096, of which the passes over the
-// row have half, and the chains of barriers, prefix sums and LDS atomics the rest; the bytes are 2 us of it.  Rows shared by up
-// to 8 workgroups, whose candidates the last one selected from, took 17.9 and 45 us: what is left to the last one is as long.
+// Bound by one CU's work on its row: a row of 32768 scores takes 14.1 us for 2048 of them and 11.5 for 256 (32 without
+// step 1's bound), 64 rows of up to 98304 25.3 for 4096, of which the passes over the row have half, and the chains of barriers,
+// prefix sums and LDS atomics the rest; the bytes are 2 us of it.  One way to share a row was tried: up to 8 workgroups list
+// candidates, the last one selects from the lists; 17.9 and 45 us, since that one's chain is as long as a row's of its own.
 #include "lychee_device.h"
 #include "lychee_paged.h"
 
