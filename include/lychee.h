@@ -404,6 +404,72 @@ int lychee_select_scores(lychee_ctx *ctx, const lychee_paged *paged, const float
                          const int32_t *lengths, const uint8_t *head_type_mask, const int32_t *idx_in,
                          int32_t *idx_out, void *hip_stream);
 
+/* ==========================================================================================
+ * Attention over whole prompts: several query tokens a request, each attending to the positions up to its own
+ * (Eq. 1 with a causal mask, every head dense: what fills the caches that the decode calls read, rewrites the last
+ * tokens of a long generation, and, with its gradient, trains head types on full attention).
+ *
+ *   - Query tokens are packed: those of request b are rows token_start[b] .. token_start[b+1]-1 of q and out, as
+ *     lychee_plan_pages numbers them.  token_start is int32 [batch + 1], in ascending order; values are clamped to
+ *     [0, n_tokens].  A request may have no tokens.  Rows that belong to no request are left as they were.
+ *   - Its keys are L_b in number, and its n_b query tokens are the last n_b of them: query i sits at position
+ *     p = L_b - n_b + i and attends to the positions 0 .. p.  A query with p < 0 has nothing to attend to: its output
+ *     is zero, its lse -infinity.
+ *   - Query head h uses KV head h / (n_q_heads / n_kv_heads), up to LYCHEE_PROMPT_MAX_GROUP query heads a KV head.
+ *   - What a query does not see has no influence on its results, infinities and NaN included.
+ *   - Softmax statistics and sums are fp32; weights, and dS in the backward pass, are rounded to bf16 for the matrix units.
+ *   - Each call enqueues one or two kernel launches (none for n_tokens = 0), may be captured, and leaves the caller's
+ *     current device as it was; launches of these calls are not timed by lychee_timing_enable.  The workspace is scratch
+ *     (256-byte aligned, contents don't care).
+ * ========================================================================================== */
+#define LYCHEE_PROMPT_MAX_GROUP 16
+
+typedef struct lychee_prompt {
+    int32_t batch;        /* requests, in [1, LYCHEE_MAX_BATCH]                                   */
+    int32_t n_q_heads;    /* a multiple of n_kv_heads                                            */
+    int32_t n_kv_heads;   /* in [1, LYCHEE_MAX_KV_HEADS]                                         */
+    int32_t head_dim;     /* must be LYCHEE_HEAD_DIM                                             */
+    int32_t n_tokens;     /* packed rows; n_tokens * n_q_heads / n_kv_heads < 2^28                */
+    int32_t max_len;      /* upper bound of lengths[] (keys in a cache), <= 2^24; lengths are clamped to it */
+    int64_t q_stride_tok, q_stride_head; /* of q and dq: element (i, h, d) at base + i*stride_tok + h*stride_head + d */
+    int64_t kv_stride_batch, kv_stride_head, kv_stride_tok; /* of k, v, dk and dv; elements, multiples of 8 as those
+                             of q; those of tokens in [128, 2^24], of query heads <= 2^24.  kv_stride_batch counts where
+                             `lengths` are given                                                    */
+} lychee_prompt;
+
+/* Pure host functions.  lychee_prompt_workspace_bytes serves both calls below; 0 if `prompt` is invalid. */
+int    lychee_check_prompt(const lychee_prompt *prompt);
+size_t lychee_prompt_workspace_bytes(const lychee_prompt *prompt);
+
+/* out = softmax(q K^T / sqrt(128)) V under the causal mask.
+ *   q              bf16, strided, 16-byte aligned (as k, v and out)
+ *   k, v           lengths NULL: packed like q, (i, g, d) at base + i*kv_stride_tok + g*kv_stride_head + d, L_b = n_b.
+ *                  Else a cache as the decode calls have it, (b, g, t, d) at base + b*kv_stride_batch +
+ *                  g*kv_stride_head + t*kv_stride_tok + d, that holds the new tokens' rows already
+ *   lengths        NULL, or int32 [B]: L_b, clamped to [0, max_len]
+ *   out            bf16 [n_tokens][H_q][128]
+ *   lse            NULL, or float [H_q][n_tokens]: log of the sum of exp of a row's scores */
+int lychee_prompt_attn(lychee_ctx *ctx, const lychee_prompt *prompt, const void *q, const void *k, const void *v,
+                       const int32_t *token_start, const int32_t *lengths, void *out, float *lse, void *workspace,
+                       size_t workspace_bytes, void *hip_stream);
+
+/* Its gradient for packed sequences: d_out and out bf16 [n_tokens][H_q][128], out and lse as the call above wrote them; dq
+ * strided like q, dk and dv like k and v, summed over the query heads of a KV head.  Heads must not share rows
+ * (strides of heads >= 128).  Gradients are written, not added to; rows of no request are left as they were. */
+int lychee_prompt_attn_backward(lychee_ctx *ctx, const lychee_prompt *prompt, const void *d_out, const void *q,
+                                const void *k, const void *v, const void *out, const float *lse,
+                                const int32_t *token_start, void *dq, void *dk, void *dv, void *workspace,
+                                size_t workspace_bytes, void *hip_stream);
+
+/* The same attention over the paged 4-bit cache, for the pieces of prompts (and single tokens) that lychee_plan_pages
+ * gave slots to and lychee_q4_append has written: lengths as after the step (lengths_out), token_start as planned.
+ * Tokens whose table entry is no page are left out.  q strided like above, out bf16 [n_tokens][H_q][128]. */
+size_t lychee_q4_prompt_workspace_bytes(const lychee_paged *paged, int32_t n_tokens);
+int lychee_q4_prompt_attn(lychee_ctx *ctx, const lychee_paged *paged, const void *q, int64_t q_stride_tok,
+                          int64_t q_stride_head, int32_t n_tokens, const void *cache, const int32_t *block_table,
+                          const int32_t *lengths, const int32_t *token_start, void *out, void *workspace,
+                          size_t workspace_bytes, void *hip_stream);
+
 const char *lychee_strerror(int code);
 
 /* ==========================================================================================

@@ -40,6 +40,8 @@ EXPORTS = [
     "lychee_timing_read", "lychee_probe_read", "lychee_probe_copy", "lychee_strerror",
     "lychee_check_paged", "lychee_paged_workspace_bytes", "lychee_release_pages", "lychee_plan_pages",
     "lychee_q4_append", "lychee_q4_read", "lychee_q4_decode_attn", "lychee_select_scores",
+    "lychee_check_prompt", "lychee_prompt_workspace_bytes", "lychee_prompt_attn", "lychee_prompt_attn_backward",
+    "lychee_q4_prompt_workspace_bytes", "lychee_q4_prompt_attn",
 ]
 
 
@@ -60,6 +62,14 @@ class Paged(ctypes.Structure):
                 ("head_dim", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
                 ("max_pages", ctypes.c_int32), ("table_stride", ctypes.c_int32), ("page_tiles", ctypes.c_int32),
                 ("k", ctypes.c_int32)]
+
+
+class Prompt(ctypes.Structure):
+    """Mirror of `lychee_prompt`."""
+    _fields_ = [("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("n_tokens", ctypes.c_int32), ("max_len", ctypes.c_int32),
+                ("q_stride_tok", ctypes.c_int64), ("q_stride_head", ctypes.c_int64), ("kv_stride_batch", ctypes.c_int64),
+                ("kv_stride_head", ctypes.c_int64), ("kv_stride_tok", ctypes.c_int64)]
 
 
 class LycheeError(RuntimeError):
@@ -109,11 +119,20 @@ def _load() -> ctypes.CDLL:
     lib.lychee_q4_read.argtypes = [vp, pgd, vp, vp, vp, vp, vp, vp, i64, i64, i64, i32, vp]
     lib.lychee_q4_decode_attn.argtypes = [vp, pgd, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp, sz, vp]
     lib.lychee_select_scores.argtypes = [vp, pgd, vp, i64, vp, vp, vp, vp, vp]
+    pmt = ctypes.POINTER(Prompt)
+    lib.lychee_check_prompt.argtypes = [pmt]
+    lib.lychee_prompt_workspace_bytes.argtypes = [pmt]
+    lib.lychee_prompt_workspace_bytes.restype = sz
+    lib.lychee_prompt_attn.argtypes = [vp, pmt, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.lychee_prompt_attn_backward.argtypes = [vp, pmt, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.lychee_q4_prompt_workspace_bytes.argtypes = [pgd, i32]
+    lib.lychee_q4_prompt_workspace_bytes.restype = sz
+    lib.lychee_q4_prompt_attn.argtypes = [vp, pgd, vp, i64, i64, i32, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.lychee_strerror.argtypes = [ctypes.c_int]
     lib.lychee_strerror.restype = ctypes.c_char_p
     for name in EXPORTS:
         if name not in ("lychee_workspace_bytes", "lychee_step_workspace_bytes", "lychee_paged_workspace_bytes",
-                        "lychee_strerror"):
+                        "lychee_prompt_workspace_bytes", "lychee_q4_prompt_workspace_bytes", "lychee_strerror"):
             getattr(lib, name).restype = ctypes.c_int
     return lib
 
@@ -196,6 +215,29 @@ def check_paged(paged: Paged, head_type_mask: Optional[np.ndarray] = None, has_i
 
 def paged_workspace_bytes(paged: Paged) -> int:
     return int(_lib.lychee_paged_workspace_bytes(ctypes.byref(paged)))
+
+
+def make_prompt(batch: int, q: torch.Tensor, kv: torch.Tensor) -> Prompt:
+    """A `lychee_prompt` for q [n_tokens, H_q, 128] and keys (and values) like kv: [n_tokens, H_kv, 128], packed like q, or a cache
+    [B, H_kv, L_cap, 128]; sizes and strides are theirs."""
+    if kv.dim() == 4:
+        n_kv, max_len, strides = kv.shape[1], kv.shape[2], (kv.stride(0), kv.stride(1), kv.stride(2))
+    else:
+        n_kv, max_len, strides = kv.shape[1], 0, (0, kv.stride(1), kv.stride(0))
+    return Prompt(batch, q.shape[1], n_kv, q.shape[2], q.shape[0], max_len, q.stride(0), q.stride(1), *strides)
+
+
+def check_prompt(prompt: Prompt) -> int:
+    """lychee_check_prompt: returns the status code (pure host)."""
+    return _lib.lychee_check_prompt(ctypes.byref(prompt))
+
+
+def prompt_workspace_bytes(prompt: Prompt) -> int:
+    return int(_lib.lychee_prompt_workspace_bytes(ctypes.byref(prompt)))
+
+
+def q4_prompt_workspace_bytes(paged: Paged, n_tokens: int) -> int:
+    return int(_lib.lychee_q4_prompt_workspace_bytes(ctypes.byref(paged), n_tokens))
 
 
 # The calls of the paged 4-bit cache look at what they are given: the library sees addresses alone, and would misread a view
@@ -312,6 +354,20 @@ def _rows_at(call: str, names, k, v, shape, device: int):
                 _refuse(call, name, t, "a torch.bfloat16 %s, strided like %s, on device %d" % (list(shape), names[0], device))
         strides = k.stride()
     return k.data_ptr(), v.data_ptr(), strides
+
+
+def _strided_at(call: str, name: str, t, shape, strides, device: int) -> Optional[int]:
+    """The address of a bf16 tensor of this shape with these strides (those of dimensions of one entry do not count)."""
+    if t is None:
+        return None
+    if not (_on_device(t, device, 2) and t.dtype is _BF16 and t.shape == shape
+            and (t.stride() == strides or all(n <= 1 or a == b for n, a, b in zip(shape, t.stride(), strides)) or 0 in shape)):
+        _refuse(call, name, t, "a torch.bfloat16 %s with strides %s on device %d" % (list(shape), list(strides), device))
+    return t.data_ptr()
+
+
+def _dtype_of(t):
+    return t.dtype if isinstance(t, torch.Tensor) else torch.uint8
 
 
 # (torch.cuda.current_stream builds a Stream object, 2.9 us of a call; the getter behind it takes 0.07)
@@ -535,6 +591,56 @@ class Context:
         score, stride = _scores_at(call, scores, paged, self.device)
         _check(_lib.lychee_select_scores(self._h, paged, score, stride, length, types, idx, new, self._on(stream)), call)
 
+    # -- whole prompts ------------------------------------------------------------------
+    def _rows_like(self, call: str, prompt: Prompt, *named):
+        """The addresses of (name, tensor) like q: [n_tokens, H_q, 128], strided as in the prompt."""
+        n, heads, d = prompt.n_tokens, prompt.n_q_heads, prompt.head_dim
+        return [_strided_at(call, name, t, (n, heads, d), (prompt.q_stride_tok, prompt.q_stride_head, 1), self.device) for name, t in named]
+
+    def _keys_like(self, call: str, prompt: Prompt, cached: bool, *named):
+        """The same of (name, tensor) like k: packed rows [n_tokens, H_kv, 128] or a cache [B, H_kv, max_len, 128]."""
+        tok, head, d = prompt.kv_stride_tok, prompt.kv_stride_head, prompt.head_dim
+        shape, strides = (prompt.n_tokens, prompt.n_kv_heads, d), (tok, head, 1)
+        if cached:
+            shape, strides = (prompt.batch, prompt.n_kv_heads, prompt.max_len, d), (prompt.kv_stride_batch, head, tok, 1)
+        return [_strided_at(call, name, t, shape, strides, self.device) for name, t in named]
+
+    def prompt_attn(self, prompt: Prompt, q, k, v, token_start, lengths, out, lse, workspace, stream=None) -> None:
+        """lychee_prompt_attn; q [n_tokens, H_q, 128]; k and v [n_tokens, H_kv, 128], or with lengths [B, H_kv, max_len, 128]; out
+        [n_tokens, H_q, 128]; lse None or [H_q, n_tokens]."""
+        call, device, B, n = "lychee_prompt_attn", self.device, prompt.batch, prompt.n_tokens * prompt.n_q_heads
+        (at_q,) = self._rows_like(call, prompt, ("q", q))
+        at_k, at_v = self._keys_like(call, prompt, lengths is not None, ("k", k), ("v", v))
+        start, length, at_out, at_lse, ws = _arrays(
+            call, device, ("token_start", token_start, _I32, B + 1), ("lengths", lengths, _I32, B),
+            ("out", out, _BF16, n * prompt.head_dim), ("lse", lse, _F32, n), ("workspace", workspace, _dtype_of(workspace), 0))
+        _check(_lib.lychee_prompt_attn(self._h, prompt, at_q, at_k, at_v, start, length, at_out, at_lse, ws,
+                                       0 if ws is None else workspace.nbytes, self._on(stream)), call)
+
+    def prompt_attn_backward(self, prompt: Prompt, d_out, q, k, v, out, lse, token_start, dq, dk, dv, workspace, stream=None) -> None:
+        """lychee_prompt_attn_backward; dq strided like q, dk and dv like k and v."""
+        call, device, B, n = "lychee_prompt_attn_backward", self.device, prompt.batch, prompt.n_tokens * prompt.n_q_heads
+        at_q, at_dq = self._rows_like(call, prompt, ("q", q), ("dq", dq))
+        at_k, at_v, at_dk, at_dv = self._keys_like(call, prompt, False, ("k", k), ("v", v), ("dk", dk), ("dv", dv))
+        at_g, at_out, at_lse, start, ws = _arrays(
+            call, device, ("d_out", d_out, _BF16, n * prompt.head_dim), ("out", out, _BF16, n * prompt.head_dim), ("lse", lse, _F32, n),
+            ("token_start", token_start, _I32, B + 1), ("workspace", workspace, _dtype_of(workspace), 0))
+        _check(_lib.lychee_prompt_attn_backward(self._h, prompt, at_g, at_q, at_k, at_v, at_out, at_lse, start, at_dq, at_dk, at_dv, ws,
+                                                0 if ws is None else workspace.nbytes, self._on(stream)), call)
+
+    def q4_prompt_attn(self, paged: Paged, q, cache, block_table, lengths, token_start, out, workspace, stream=None) -> None:
+        """lychee_q4_prompt_attn; q [n_tokens, H_q, 128], strided; out [n_tokens, H_q, 128]."""
+        call, device, B = "lychee_q4_prompt_attn", self.device, paged.batch
+        n = q.shape[0] if isinstance(q, torch.Tensor) and q.dim() == 3 else 0
+        strides = (q.stride(0), q.stride(1), 1) if n else (paged.head_dim, 0, 1)
+        at_q = _strided_at(call, "q", q, (n, paged.n_q_heads, paged.head_dim), strides, device)
+        length, start, at_out, ws = _arrays(
+            call, device, ("lengths", lengths, _I32, B), ("token_start", token_start, _I32, B + 1),
+            ("out", out, _BF16, n * paged.n_q_heads * paged.head_dim), ("workspace", workspace, _dtype_of(workspace), 0))
+        _check(_lib.lychee_q4_prompt_attn(self._h, paged, at_q, strides[0], strides[1], n, _cache_at(call, cache, paged, device),
+                                          _table_at(call, block_table, paged, device), length, start, at_out, ws,
+                                          0 if ws is None else workspace.nbytes, self._on(stream)), call)
+
     # -- helpers ------------------------------------------------------------------------
     def select_stats(self, stream=None):
         """(too_few, too_many): score rows the select ranked whole since the context was created."""
@@ -590,6 +696,22 @@ def alloc_paged_workspace(paged: Paged, device="cuda") -> torch.Tensor:
     n = paged_workspace_bytes(paged)
     if n == 0:
         raise LycheeError(check_paged(paged), "lychee_paged_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def alloc_prompt_workspace(prompt: Prompt, device="cuda") -> torch.Tensor:
+    """A device buffer of lychee_prompt_workspace_bytes(prompt) bytes."""
+    n = prompt_workspace_bytes(prompt)
+    if n == 0:
+        raise LycheeError(check_prompt(prompt), "lychee_prompt_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def alloc_q4_prompt_workspace(paged: Paged, n_tokens: int, device="cuda") -> torch.Tensor:
+    """A device buffer of lychee_q4_prompt_workspace_bytes(paged, n_tokens) bytes."""
+    n = q4_prompt_workspace_bytes(paged, n_tokens)
+    if n == 0:
+        raise LycheeError(check_paged(paged) or EUNSUPPORTED, "lychee_q4_prompt_workspace_bytes")
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 

@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblychee.so")
 SOURCES = ["lychee_api.hip", "lychee_units.hip", "lychee_layer.hip", "lychee_paged_api.hip", "lychee_pages.hip", "lychee_q4.hip",
-           "lychee_topk.hip"]
+           "lychee_topk.hip", "lychee_prompt_api.hip", "lychee_prompt.hip", "lychee_prompt_grad.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-command-line-argument"]

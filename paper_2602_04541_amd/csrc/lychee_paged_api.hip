@@ -1,5 +1,6 @@
 // Host side of the paged 4-bit cache: argument checks and launches of the calls that lychee.h declares for it.
 #include "lychee_context.h"
+#include "lychee_host.h"
 #include "lychee_paged.h"
 
 #include <math.h>
@@ -33,22 +34,6 @@ int check_heads(const lychee_paged *p, const uint8_t *mask, bool has_idx_in)
     return LYCHEE_OK;
 }
 
-PagedDims dims_of(const lychee_paged &p)
-{
-    PagedDims d;
-    d.batch = p.batch;
-    d.n_kv_heads = p.n_kv_heads;
-    d.group = p.n_q_heads / p.n_kv_heads;
-    d.n_pages = p.n_pages;
-    d.page_shift = 0;
-    while ((1 << d.page_shift) < p.page_size) ++d.page_shift;
-    d.max_len = p.max_pages * p.page_size;
-    d.table_stride = p.table_stride;
-    d.page_tiles = p.page_tiles;
-    d.k = p.k;
-    return d;
-}
-
 struct Carved {
     size_t part_o, part_ml, total;
 };
@@ -61,25 +46,6 @@ Carved carve(const lychee_paged &p)
     c.total = c.part_ml + (size_t)round_up(heads * 2 * (int64_t)sizeof(float), 256);
     return c;
 }
-
-// The context's device while a call launches, then the caller's again.
-struct OnDevice {
-    int before = -1;
-    bool ok = false;
-    explicit OnDevice(const lychee_ctx *ctx)
-    {
-        ok = hipGetDevice(&before) == hipSuccess && (before == ctx->device || hipSetDevice(ctx->device) == hipSuccess);
-        if (before == ctx->device) before = -1;
-    }
-    ~OnDevice()
-    {
-        if (before >= 0) (void)hipSetDevice(before);
-    }
-    OnDevice(const OnDevice &) = delete;
-    OnDevice &operator=(const OnDevice &) = delete;
-};
-
-int done(hipError_t e) { return e == hipSuccess ? LYCHEE_OK : LYCHEE_EHIP; }
 
 uint32_t *arrived_word(lychee_ctx *ctx) { return reinterpret_cast<uint32_t *>(ctx->sync_dev + kSyncPages); }
 

@@ -1,0 +1,56 @@
+// What the host side and the kernels of attention over whole prompts share: the kernels' arguments, the sizes of
+// their launches.
+#pragma once
+
+#include "lychee_paged.h"
+
+namespace lychee {
+
+constexpr int kPromptMaxGroup = 16;
+constexpr int kPromptRows = 128;          // query rows of a tile, a row being a (token, query head of the KV head)
+constexpr int kPromptKeys = 64;           // keys a workgroup takes at a time
+constexpr int kPromptMinPiece = 4;        // blocks of keys in a piece of a split tile, at least
+constexpr int64_t kPromptMaxRows = 1 << 28;  // query tokens times heads of a group (row numbers are divided with a multiplication)
+constexpr int64_t kPromptMaxStride = 1 << 24;  // elements from a token's row to the next (offsets within 64 rows fit 32 bits)
+
+// A batch of packed query rows.
+struct PromptRows {
+    const int32_t *start;    // [batch + 1]
+    const int32_t *lengths;  // [batch] keys of a request, or nullptr: as many as it has query tokens
+    int32_t batch, n_kv_heads, group;
+    int32_t n_tokens, max_len;
+    uint32_t group_magic;    // ceil(2^32 / group): r / group = umulhi(r, magic) for group > 1 and r < kPromptMaxRows
+    int64_t q_tok, q_head;   // strides of q, elements
+};
+
+struct PromptArgs {
+    PromptRows r;
+    const uint16_t *q, *k, *v;
+    int64_t kv_batch, kv_head, kv_tok;  // strides of k and v; kv_batch counts where there are lengths
+    const uint8_t *cache;               // the paged cache, or nullptr
+    const int32_t *table;
+    PagedDims d;
+    uint16_t *out;      // [n_tokens][n_q_heads][128]
+    float *lse;         // [n_q_heads][n_tokens] or nullptr
+    float *part_o;      // [piece][kPromptRows][128] un-normalised partial outputs
+    float *part_ml;     // [piece][kPromptRows][2]   maximum (log2 units) and sum
+    int32_t slots;      // 0: tiles are not split; else the pieces that fill the device
+    int32_t n_items, n_tiles;  // pieces and tiles of a KV head that the launch has room for
+    float scale_log2e;
+};
+
+struct PromptGradArgs {
+    PromptRows r;
+    const uint16_t *g, *q, *k, *v, *out;
+    const float *lse;
+    int64_t kv_head, kv_tok;
+    uint16_t *dq, *dk, *dv;  // strided like q, k and v
+    float *stat;             // [n_q_heads][n_tokens][2] lse in log2 units, g . out
+    float scale, scale_log2e;
+    int32_t n_row_tiles, n_key_tiles;  // of a KV head, at most
+};
+
+hipError_t launch_prompt(const PromptArgs &a, hipStream_t stream);
+hipError_t launch_prompt_grad(const PromptGradArgs &a, hipStream_t stream);
+
+}  // namespace lychee

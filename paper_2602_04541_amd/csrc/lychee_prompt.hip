@@ -1,0 +1,273 @@
+// Causal attention over whole prompts: packed rows of queries against keys that are packed alike, lie in a bf16 cache, or in
+// the paged 4-bit cache.
+//
+// For row r of a (request, KV head) - query token t = r / G, query head r % G of the head's group - at position
+// p = L - n + t:
+//     s_j = q . k_j log2(e) / sqrt(128),  m = max s,  l = sum 2^(s_j - m),  o = sum 2^(s_j - m) v_j / l    over j <= p
+// in one pass over blocks of 64 keys with a running m and l.
+//
+// A workgroup has 128 rows, 32 a wavefront, so that a KV head's keys are read once for all of its query heads and a single
+// token's group shares a tile.  Scores are made turned, S^T = K Q^T: a lane has one row (column) and half of a
+// block's keys, the running maximum and sum need one exchange between two lanes, and the weights are the B operand of the second
+// product O^T = V^T P^T as they stand.
+#include "lychee_prompt_device.h"
+
+namespace lychee {
+namespace {
+
+struct SharedPrompt {
+    __align__(16) uint8_t k[2][kBlockBytes];
+    __align__(16) uint8_t v[2][kBlockBytes];
+    __align__(8) uint16_t bad[2][kWaves];  // of a block's keys those whose page is not there, a bit each
+    SharedPlan plan;
+};
+
+template <bool Q4>
+__global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
+{
+    __shared__ SharedPrompt sh;
+    const PromptRows &p = a.r;
+    const int g = blockIdx.x % p.n_kv_heads;
+    const Tile w = find_tile<false>(p, blockIdx.x / p.n_kv_heads, a.slots, sh.plan);
+    if (!w.found || (w.piece > 0 && w.first >= w.last)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hi = lane >> 5;
+    const int rows = w.n * p.group, row = w.tile * kPromptRows + wave * 32 + (lane & 31);
+    const int row_in = min(row, rows - 1), token = token_of(p, row_in), head = g * p.group + row_in - token * p.group;
+    const int pos = w.len - w.n + token;  // keys 0 .. pos are seen
+    const int lowest = w.len - w.n + token_of(p, min(w.tile * kPromptRows + wave * 32, rows - 1));  // of the wavefront's rows
+    const int highest = w.len - w.n + token_of(p, min(w.tile * kPromptRows + wave * 32 + 31, rows - 1));
+
+    bf16x8_t qf[8];
+    {
+        const uint16_t *q = a.q + (int64_t)(w.start + token) * p.q_tok + (int64_t)head * p.q_head + 8 * hi;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) qf[ks] = *(const LYCHEE_GLOBAL bf16x8_t *)(q + 16 * ks);
+    }
+    const uint32_t row_at = row_place(lane), turn_at = turn_place(lane);
+
+    // bf16: copies go to LDS as they are, 16 rows of either operand a step, four a wavefront.
+    const int64_t base = p.lengths ? (int64_t)w.b * a.kv_batch : (int64_t)w.start * a.kv_tok;
+    const uint16_t *kb = a.k + base + (int64_t)g * a.kv_head, *vb = a.v + base + (int64_t)g * a.kv_head;
+    const uint32_t to_k = lds_address(sh.k) + wave * 4 * kRowBytes, to_v = lds_address(sh.v) + wave * 4 * kRowBytes;
+    const int fetch_row = 4 * wave + (lane >> 4);
+    const uint32_t fetch_chunk = (uint32_t)((lane & 15) ^ swizzle(fetch_row)) << 4;  // (the same for rows 16 apart)
+    const uint32_t fetch_at = (uint32_t)fetch_row * (uint32_t)(2 * a.kv_tok) + fetch_chunk;
+    // 4 bits: a thread takes a quarter (one scale's dimensions) of a token's key and of its value, and writes their bf16 numbers.
+    const int token4 = threadIdx.x >> 2, part4 = threadIdx.x & 3;
+    uint4 code_k = make_uint4(0, 0, 0, 0), code_v = code_k;
+    uint32_t scale_kv = 0;  // bytes: key, value
+    int entry = -1;         // of the block table, for the block after the one that is loaded
+    const auto fetch_entry = [&](int blk) {
+        const int t = min(blk * kPromptKeys + token4, w.len - 1);
+        entry = gload(a.table + (int64_t)w.b * a.d.table_stride + (t >> a.d.page_shift));
+    };
+    const auto fetch = [&](int blk, int buf) {
+        const int j0 = blk * kPromptKeys;
+        if constexpr (Q4) {
+            const int t = j0 + token4, off = t & ((1 << a.d.page_shift) - 1);
+            const bool ok = t < w.len && (uint32_t)entry < (uint32_t)a.d.n_pages;
+            const uint8_t *tile = a.cache + ((int64_t)(ok ? entry : 0) * a.d.page_tiles + (int64_t)g * ((1 << a.d.page_shift) / kTileTokens) +
+                                             off / kTileTokens) * kTileBytes;
+            const int sub = off & (kTileTokens - 1);
+            const u32x4_t k4 = *(const LYCHEE_GLOBAL u32x4_t *)(tile + sub * kTokenBytes + 16 * part4);
+            const u32x4_t v4 = *(const LYCHEE_GLOBAL u32x4_t *)(tile + sub * kTokenBytes + 64 + 16 * part4);
+            code_k = make_uint4(k4[0], k4[1], k4[2], k4[3]);
+            code_v = make_uint4(v4[0], v4[1], v4[2], v4[3]);
+            const uint32_t ks = gload(tile + kTileScales + part4 * kTileTokens + sub), vs = gload(tile + kTileScales + (4 + part4) * kTileTokens + sub);
+            scale_kv = ok ? ks | vs << 8 : 0u;  // (a scale of 0 makes numbers that are no NaN: a weight of 0 times NaN is NaN)
+            const uint64_t there = __ballot(ok);
+            if (lane == 0) {
+                uint32_t bad = 0;  // (four lanes a token)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) bad |= (uint32_t)(~there >> (4 * i) & 1) << i;
+                sh.bad[buf][wave] = (uint16_t)bad;
+            }
+            if (blk + 1 < w.last) fetch_entry(blk + 1);
+        } else {
+            const bool whole = j0 + kPromptKeys <= w.len;  // (else the last key again in the rows behind it)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int64_t from = (int64_t)(whole ? j0 + 16 * i : j0) * a.kv_tok;
+                const uint32_t off = whole ? fetch_at : (uint32_t)min(fetch_row + 16 * i, w.len - 1 - j0) * (uint32_t)(2 * a.kv_tok) + fetch_chunk;
+                copy16(kb + from, off, to_k + buf * kBlockBytes + i * 16 * kRowBytes);
+                copy16(vb + from, off, to_v + buf * kBlockBytes + i * 16 * kRowBytes);
+            }
+        }
+    };
+    const auto arrive = [&](int buf) {
+        if constexpr (Q4) {
+            const float ks = __builtin_bit_cast(float, scale_kv << 23), vs = __builtin_bit_cast(float, scale_kv << 15);
+            const uint32_t kc[4] = {code_k.x, code_k.y, code_k.z, code_k.w}, vc[4] = {code_v.x, code_v.y, code_v.z, code_v.w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int to = token4 * kRowBytes + (((4 * part4 + c) ^ swizzle(token4)) << 4);
+                *reinterpret_cast<uint4 *>(sh.k[buf] + to) = decode8(kc[c], ks);
+                *reinterpret_cast<uint4 *>(sh.v[buf] + to) = decode8(vc[c], vs);
+            }
+        } else {
+            wait_copies();
+        }
+        __syncthreads();
+    };
+
+    f32x16_t o[4];
+    float m, l;
+    bool careful = false;
+    for (;;) {
+#pragma unroll
+        for (int db = 0; db < 4; ++db) o[db] = zero16();
+        m = -__builtin_inff();
+        l = 0.f;
+        if (w.first < w.last) {
+            if (Q4) fetch_entry(w.first);
+            fetch(w.first, 0);
+        }
+        arrive(0);
+        for (int blk = w.first; blk < w.last; ++blk) {
+            const int buf = (blk - w.first) & 1, j0 = blk * kPromptKeys;
+            if (blk + 1 < w.last) fetch(blk + 1, buf ^ 1);
+            const LYCHEE_LDS uint8_t *K = (const LYCHEE_LDS uint8_t *)sh.k[buf], *V = (const LYCHEE_LDS uint8_t *)sh.v[buf];
+            if (j0 <= highest) {
+                const uint32_t kat = opaque(row_at), vat = opaque(turn_at);
+                f32x16_t z[2] = {zero16(), zero16()};
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) z[x] = mfma(read_rows(K, kat, x, ks), qf[ks], z[x]);
+                uint64_t bad = 0;  // keys whose page is not there
+                if (Q4) {
+                    const uint2 words = *reinterpret_cast<const uint2 *>(sh.bad[buf]);
+                    bad = (uint64_t)__builtin_amdgcn_readfirstlane(words.y) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane(words.x);
+                }
+                const bool masked = j0 + kPromptKeys - 1 > lowest || bad != 0;
+                if (masked) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int n = min(max(pos - j0 - 32 * x + 1, 0), 32);
+                        uint32_t seen = n == 32 ? ~0u : (1u << n) - 1u;
+                        if (Q4) seen &= ~(uint32_t)(bad >> (32 * x));
+                        seen >>= 4 * hi;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) z[x][i] = seen >> (i % 4 + 8 * (i / 4)) & 1u ? z[x][i] : -__builtin_inff();
+                    }
+                }
+                float top = z[0][0];
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) top = fmaxf(top, z[x][i]);
+                top = max_halves32(top) * a.scale_log2e;
+                if (__ballot(top > m) != 0) {
+                    const float up = fmaxf(m, top);
+                    const float f = m == up ? 1.0f : fast_exp2(m - up);
+                    m = up;
+                    l *= f;
+#pragma unroll
+                    for (int db = 0; db < 4; ++db)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[db][i] *= f;
+                }
+                const float ref = m == -__builtin_inff() ? 0.f : m;
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        z[x][i] = fast_exp2(__builtin_fmaf(z[x][i], a.scale_log2e, -ref));
+                        l += z[x][i];
+                    }
+                bf16x8_t pf[4] = {operand<0>(z[0]), operand<8>(z[0]), operand<0>(z[1]), operand<8>(z[1])};
+                if (__builtin_expect(careful && masked, 0)) {
+#pragma unroll 1
+                    for (int s = 0; s < 4; ++s) {
+                        const bf16x8_t seen = seen_rows(hi, s, 0, pos - j0);
+                        const bf16x8_t weights = s < 2 ? (s == 0 ? pf[0] : pf[1]) : (s == 2 ? pf[2] : pf[3]);
+#pragma unroll
+                        for (int db = 0; db < 4; ++db) {
+                            o[db] = mfma_careful(read_turned(V, opaque(vat), db, s), weights, seen, o[db]);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int s = 0; s < 4; ++s)
+#pragma unroll
+                        for (int db = 0; db < 4; ++db) o[db] = mfma(read_turned(V, vat, db, s), pf[s], o[db]);
+                }
+            }
+            arrive(buf ^ 1);
+        }
+        // A key's value counts for the rows that see it alone, but a weight of zero times an infinite value or NaN is NaN: a
+        // tile in which that may have happened is done again, with care.
+        if (careful || !__syncthreads_or(!all_finite(o))) break;
+        careful = true;
+    }
+    l = sum_halves32(l);
+    if (w.parts == 1) {
+        const bool there = row < rows;
+        uint16_t *out = a.out + ((int64_t)(w.start + token) * (p.n_kv_heads * p.group) + head) * kHeadDim;
+        store_row(there ? out : nullptr, lane, o, l == 0.f ? 0.f : 1.f / l);
+        if (a.lse && there && hi == 0)
+            gstore(a.lse + (int64_t)head * p.n_tokens + w.start + token, l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * (1.f / kLog2e));
+    } else {
+        const int64_t slot = (int64_t)w.item * p.n_kv_heads + g;
+        float *po = a.part_o + (slot * kPromptRows + wave * 32 + (lane & 31)) * kHeadDim + 4 * hi;
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) *(LYCHEE_GLOBAL f32x4_t *)(po + 32 * db + 8 * j) = f32x4_t{o[db][4 * j], o[db][4 * j + 1], o[db][4 * j + 2], o[db][4 * j + 3]};
+        if (hi == 0) gstore_f2(a.part_ml + (slot * kPromptRows + wave * 32 + lane) * 2, make_float2(m, l));
+    }
+}
+
+// Rows of split tiles: o = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p, M = max m_p.  A workgroup has 16 rows of a tile, a
+// wavefront four, one after the other, two dimensions a lane.
+constexpr int kMergeRows = 16;
+__global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptArgs a)
+{
+    __shared__ SharedPlan sh;
+    const PromptRows &p = a.r;
+    constexpr int kParts = kPromptRows / kMergeRows;
+    const int g = blockIdx.x / kParts % p.n_kv_heads, tile = blockIdx.x / kParts / p.n_kv_heads, sub = blockIdx.x % kParts;
+    const Tile w = find_tile<true>(p, tile, a.slots, sh);
+    if (!w.found || w.parts == 1) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rows = w.n * p.group;
+    for (int i = 0; i < kMergeRows / kWaves; ++i) {
+        const int at = sub * kMergeRows + wave * (kMergeRows / kWaves) + i, row = w.tile * kPromptRows + at;
+        if (row >= rows) break;
+        const int token = token_of(p, row), head = g * p.group + row - token * p.group;
+        const auto slot = [&](int piece) { return ((int64_t)(w.item + piece) * p.n_kv_heads + g) * kPromptRows + at; };
+        float m = -__builtin_inff();
+        for (int q = lane; q < w.parts; q += 64) m = fmaxf(m, gload(a.part_ml + slot(q) * 2));
+        m = wave_max_f(m);
+        const float ref = m == -__builtin_inff() ? 0.f : m;
+        float l = 0.f, x = 0.f, y = 0.f;
+        for (int q = 0; q < w.parts; ++q) {
+            const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + slot(q) * 2);
+            const float f = fast_exp2(ml.x - ref);
+            const float2 o = *reinterpret_cast<const float2 *>(a.part_o + slot(q) * kHeadDim + 2 * lane);
+            l += f * ml.y;
+            x += f * o.x;
+            y += f * o.y;
+        }
+        const float f = l == 0.f ? 0.f : 1.f / l;
+        const int64_t to = (int64_t)(w.start + token) * (p.n_kv_heads * p.group) + head;
+        gstore(reinterpret_cast<uint32_t *>(a.out + to * kHeadDim) + lane, pk_bf16(x * f, y * f));
+        if (a.lse && lane == 0)
+            gstore(a.lse + (int64_t)head * p.n_tokens + w.start + token, l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * (1.f / kLog2e));
+    }
+}
+
+}  // namespace
+
+hipError_t launch_prompt(const PromptArgs &a, hipStream_t stream)
+{
+    const unsigned grid = (unsigned)a.n_items * (unsigned)a.r.n_kv_heads;
+    if (a.cache)
+        prompt_kernel<true><<<grid, kThreads, 0, stream>>>(a);
+    else
+        prompt_kernel<false><<<grid, kThreads, 0, stream>>>(a);
+    if (a.slots > 0) prompt_merge_kernel<<<(unsigned)a.n_tiles * (unsigned)a.r.n_kv_heads * (kPromptRows / kMergeRows), kThreads, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace lychee

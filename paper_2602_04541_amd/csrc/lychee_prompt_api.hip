@@ -1,0 +1,241 @@
+// Host side of attention over whole prompts: argument checks and launches of the calls that lychee.h declares for it.
+#include "lychee_context.h"
+#include "lychee_host.h"
+#include "lychee_prompt.h"
+
+#include <math.h>
+#include <string.h>
+
+using namespace lychee;
+
+namespace {
+
+constexpr int32_t kPromptSlots = 512;  // pieces that fill a device: two workgroups a compute unit
+constexpr int64_t kMaxGrid = 1 << 24;  // workgroups of 256 threads, which are counted in 32 bits
+
+int check_heads_of(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim)
+{
+    if (n_q_heads < 1 || n_kv_heads < 1 || n_q_heads % n_kv_heads != 0) return LYCHEE_EINVAL;
+    if (head_dim != kHeadDim || n_kv_heads > kMaxKvHeads || n_q_heads / n_kv_heads > kPromptMaxGroup) return LYCHEE_EUNSUPPORTED;
+    return LYCHEE_OK;
+}
+
+bool good_stride(int64_t s) { return s >= 0 && s % 8 == 0; }
+
+// Pieces and tiles of a batch's query rows, of a KV head.
+struct Grid {
+    int64_t tiles, items;
+    int32_t slots;
+};
+Grid grid_of(int32_t batch, int32_t n_kv_heads, int32_t group, int32_t n_tokens, int64_t max_len)
+{
+    Grid w;
+    w.tiles = (int64_t)n_tokens * group / kPromptRows + (batch < n_tokens ? batch : n_tokens);
+    // Few tiles over many keys are split along these: a piece has kPromptMinPiece blocks at least.
+    const bool split = w.tiles * n_kv_heads < 2 * kPromptSlots && max_len > 2 * kPromptMinPiece * kPromptKeys;
+    w.slots = split ? kPromptSlots : 0;
+    w.items = w.tiles + (split ? (kPromptSlots + n_kv_heads - 1) / n_kv_heads : 0);
+    return w;
+}
+
+struct CarvedPrompt {
+    size_t part_ml, stat, total;
+};
+CarvedPrompt carve(const Grid &w, int32_t n_kv_heads, int64_t stats)
+{
+    CarvedPrompt c;
+    const int64_t rows = w.slots > 0 ? w.items * n_kv_heads * kPromptRows : 0;
+    c.part_ml = (size_t)(rows * kHeadDim * (int64_t)sizeof(float));
+    c.stat = c.part_ml + (size_t)round_up(rows * 2 * (int64_t)sizeof(float), 256);
+    c.total = c.stat + (size_t)round_up(stats * 2 * (int64_t)sizeof(float), 256);
+    if (c.total == 0) c.total = 256;
+    return c;
+}
+
+int check_prompt(const lychee_prompt *p)
+{
+    if (p == nullptr) return LYCHEE_EINVAL;
+    if (p->batch < 1 || p->n_tokens < 0 || p->max_len < 0) return LYCHEE_EINVAL;
+    const int rc = check_heads_of(p->n_q_heads, p->n_kv_heads, p->head_dim);
+    if (rc != LYCHEE_OK) return rc;
+    if (!good_stride(p->q_stride_tok) || !good_stride(p->q_stride_head) || !good_stride(p->kv_stride_batch) ||
+        !good_stride(p->kv_stride_head) || !good_stride(p->kv_stride_tok) || p->q_stride_tok < kHeadDim || p->kv_stride_tok < kHeadDim)
+        return LYCHEE_EINVAL;
+    if (p->batch > kMaxBatch || p->max_len > kMaxContext) return LYCHEE_EUNSUPPORTED;
+    if (p->q_stride_tok > kPromptMaxStride || p->q_stride_head > kPromptMaxStride || p->kv_stride_tok > kPromptMaxStride) return LYCHEE_EUNSUPPORTED;
+    const int32_t G = p->n_q_heads / p->n_kv_heads;
+    if ((int64_t)p->n_tokens * G >= kPromptMaxRows) return LYCHEE_EUNSUPPORTED;
+    if (grid_of(p->batch, p->n_kv_heads, G, p->n_tokens, 0).tiles * p->n_kv_heads >= kMaxGrid) return LYCHEE_EUNSUPPORTED;
+    return LYCHEE_OK;
+}
+
+// (for either kind of keys: the longer request that a batch may hold)
+Grid grid_of(const lychee_prompt &p)
+{
+    return grid_of(p.batch, p.n_kv_heads, p.n_q_heads / p.n_kv_heads, p.n_tokens, p.max_len > p.n_tokens ? p.max_len : p.n_tokens);
+}
+CarvedPrompt carve(const lychee_prompt &p) { return carve(grid_of(p), p.n_kv_heads, (int64_t)p.n_tokens * p.n_q_heads); }
+
+PromptRows rows_of(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_tokens, int32_t max_len, int64_t q_tok, int64_t q_head,
+                   const int32_t *start, const int32_t *lengths)
+{
+    PromptRows r;
+    memset(&r, 0, sizeof r);
+    r.start = start;
+    r.lengths = lengths;
+    r.batch = batch;
+    r.n_kv_heads = n_kv_heads;
+    r.group = n_q_heads / n_kv_heads;
+    r.n_tokens = n_tokens;
+    r.max_len = max_len;
+    r.group_magic = r.group > 1 ? (uint32_t)(((1ull << 32) + (uint32_t)r.group - 1) / (uint32_t)r.group) : 0;
+    r.q_tok = q_tok;
+    r.q_head = q_head;
+    return r;
+}
+
+int check_workspace(const void *workspace, size_t bytes, const CarvedPrompt &c)
+{
+    return workspace == nullptr || !aligned(workspace, 256) || bytes < c.total ? LYCHEE_EWORKSPACE : LYCHEE_OK;
+}
+
+// A pending select still reads its workspace.
+bool still_read(const lychee_ctx *ctx, const void *workspace) { return ctx->pending.active && ctx->pending.workspace == workspace; }
+
+void fill_split(PromptArgs &a, const Grid &w, const CarvedPrompt &c, void *workspace)
+{
+    a.part_o = static_cast<float *>(workspace);
+    a.part_ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + c.part_ml);
+    a.slots = w.slots;
+    a.n_items = (int32_t)w.items;
+    a.n_tiles = (int32_t)w.tiles;
+    a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)kHeadDim));
+}
+
+}  // namespace
+
+extern "C" {
+
+int lychee_check_prompt(const lychee_prompt *prompt) { return check_prompt(prompt); }
+
+size_t lychee_prompt_workspace_bytes(const lychee_prompt *prompt) { return check_prompt(prompt) == LYCHEE_OK ? carve(*prompt).total : 0; }
+
+int lychee_prompt_attn(lychee_ctx *ctx, const lychee_prompt *prompt, const void *q, const void *k, const void *v, const int32_t *token_start,
+                       const int32_t *lengths, void *out, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (ctx == nullptr) return LYCHEE_EINVAL;
+    int rc = check_prompt(prompt);
+    if (rc != LYCHEE_OK) return rc;
+    const lychee_prompt &p = *prompt;
+    if (!token_start || !aligned(token_start, 4) || !aligned(lengths, 4) || !aligned(lse, 4)) return LYCHEE_EINVAL;
+    const CarvedPrompt c = carve(p);
+    if ((rc = check_workspace(workspace, workspace_bytes, c)) != LYCHEE_OK) return rc;
+    if (p.n_tokens == 0) return LYCHEE_OK;
+    if (!q || !k || !v || !out || !aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16)) return LYCHEE_EINVAL;
+    if (still_read(ctx, workspace)) return LYCHEE_EINVAL;
+    const OnDevice dev(ctx);
+    if (!dev.ok) return LYCHEE_EHIP;
+    PromptArgs a;
+    memset(&a, 0, sizeof a);
+    a.r = rows_of(p.batch, p.n_q_heads, p.n_kv_heads, p.n_tokens, p.max_len, p.q_stride_tok, p.q_stride_head, token_start, lengths);
+    a.q = static_cast<const uint16_t *>(q);
+    a.k = static_cast<const uint16_t *>(k);
+    a.v = static_cast<const uint16_t *>(v);
+    a.kv_batch = p.kv_stride_batch;
+    a.kv_head = p.kv_stride_head;
+    a.kv_tok = p.kv_stride_tok;
+    a.out = static_cast<uint16_t *>(out);
+    a.lse = lse;
+    fill_split(a, grid_of(p.batch, p.n_kv_heads, a.r.group, p.n_tokens, lengths ? p.max_len : p.n_tokens), c, workspace);
+    return done(launch_prompt(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+int lychee_prompt_attn_backward(lychee_ctx *ctx, const lychee_prompt *prompt, const void *d_out, const void *q, const void *k, const void *v,
+                                const void *out, const float *lse, const int32_t *token_start, void *dq, void *dk, void *dv,
+                                void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (ctx == nullptr) return LYCHEE_EINVAL;
+    int rc = check_prompt(prompt);
+    if (rc != LYCHEE_OK) return rc;
+    const lychee_prompt &p = *prompt;
+    if (!token_start || !aligned(token_start, 4) || !aligned(lse, 4)) return LYCHEE_EINVAL;
+    const CarvedPrompt c = carve(p);
+    if ((rc = check_workspace(workspace, workspace_bytes, c)) != LYCHEE_OK) return rc;
+    if (p.n_tokens == 0) return LYCHEE_OK;
+    if (!d_out || !q || !k || !v || !out || !lse || !dq || !dk || !dv) return LYCHEE_EINVAL;
+    if (!aligned(d_out, 16) || !aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16) || !aligned(dq, 16) ||
+        !aligned(dk, 16) || !aligned(dv, 16))
+        return LYCHEE_EINVAL;
+    // heads that share rows would share their gradients' too
+    if ((p.n_q_heads > 1 && p.q_stride_head < kHeadDim) || (p.n_kv_heads > 1 && p.kv_stride_head < kHeadDim)) return LYCHEE_EINVAL;
+    if (still_read(ctx, workspace)) return LYCHEE_EINVAL;
+    const OnDevice dev(ctx);
+    if (!dev.ok) return LYCHEE_EHIP;
+    PromptGradArgs a;
+    memset(&a, 0, sizeof a);
+    a.r = rows_of(p.batch, p.n_q_heads, p.n_kv_heads, p.n_tokens, p.max_len, p.q_stride_tok, p.q_stride_head, token_start, nullptr);
+    a.g = static_cast<const uint16_t *>(d_out);
+    a.q = static_cast<const uint16_t *>(q);
+    a.k = static_cast<const uint16_t *>(k);
+    a.v = static_cast<const uint16_t *>(v);
+    a.out = static_cast<const uint16_t *>(out);
+    a.lse = lse;
+    a.kv_head = p.kv_stride_head;
+    a.kv_tok = p.kv_stride_tok;
+    a.dq = static_cast<uint16_t *>(dq);
+    a.dk = static_cast<uint16_t *>(dk);
+    a.dv = static_cast<uint16_t *>(dv);
+    a.stat = reinterpret_cast<float *>(static_cast<char *>(workspace) + c.stat);
+    a.scale = (float)(1.0 / sqrt((double)kHeadDim));
+    a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)kHeadDim));
+    a.n_row_tiles = (int32_t)grid_of(p.batch, p.n_kv_heads, a.r.group, p.n_tokens, 0).tiles;
+    a.n_key_tiles = (int32_t)grid_of(p.batch, p.n_kv_heads, 1, p.n_tokens, 0).tiles;
+    return done(launch_prompt_grad(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t lychee_q4_prompt_workspace_bytes(const lychee_paged *paged, int32_t n_tokens)
+{
+    if (lychee_check_paged(paged, nullptr, 1) != LYCHEE_OK || n_tokens < 0) return 0;
+    const int32_t G = paged->n_q_heads / paged->n_kv_heads;
+    if (G > kPromptMaxGroup || (int64_t)n_tokens * G >= kPromptMaxRows) return 0;
+    return carve(grid_of(paged->batch, paged->n_kv_heads, G, n_tokens, (int64_t)paged->max_pages * paged->page_size), paged->n_kv_heads, 0).total;
+}
+
+int lychee_q4_prompt_attn(lychee_ctx *ctx, const lychee_paged *paged, const void *q, int64_t q_stride_tok, int64_t q_stride_head,
+                          int32_t n_tokens, const void *cache, const int32_t *block_table, const int32_t *lengths,
+                          const int32_t *token_start, void *out, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (ctx == nullptr) return LYCHEE_EINVAL;
+    int rc = lychee_check_paged(paged, nullptr, 1);
+    if (rc != LYCHEE_OK) return rc;
+    const lychee_paged &p = *paged;
+    if (n_tokens < 0) return LYCHEE_EINVAL;
+    if ((rc = check_heads_of(p.n_q_heads, p.n_kv_heads, p.head_dim)) != LYCHEE_OK) return rc;
+    const int32_t G = p.n_q_heads / p.n_kv_heads, max_len = p.max_pages * p.page_size;
+    if ((int64_t)n_tokens * G >= kPromptMaxRows || q_stride_tok > kPromptMaxStride || q_stride_head > kPromptMaxStride) return LYCHEE_EUNSUPPORTED;
+    if (!good_stride(q_stride_tok) || !good_stride(q_stride_head) || q_stride_tok < kHeadDim) return LYCHEE_EINVAL;
+    const Grid w = grid_of(p.batch, p.n_kv_heads, G, n_tokens, max_len);
+    if (w.tiles * p.n_kv_heads >= kMaxGrid) return LYCHEE_EUNSUPPORTED;
+    if (!cache || !block_table || !lengths || !token_start || !aligned(cache, 128) || !aligned(block_table, 4) || !aligned(lengths, 4) ||
+        !aligned(token_start, 4))
+        return LYCHEE_EINVAL;
+    const CarvedPrompt c = carve(w, p.n_kv_heads, 0);
+    if ((rc = check_workspace(workspace, workspace_bytes, c)) != LYCHEE_OK) return rc;
+    if (n_tokens == 0) return LYCHEE_OK;
+    if (!q || !out || !aligned(q, 16) || !aligned(out, 16)) return LYCHEE_EINVAL;
+    if (still_read(ctx, workspace)) return LYCHEE_EINVAL;
+    const OnDevice dev(ctx);
+    if (!dev.ok) return LYCHEE_EHIP;
+    PromptArgs a;
+    memset(&a, 0, sizeof a);
+    a.r = rows_of(p.batch, p.n_q_heads, p.n_kv_heads, n_tokens, max_len, q_stride_tok, q_stride_head, token_start, lengths);
+    a.q = static_cast<const uint16_t *>(q);
+    a.cache = static_cast<const uint8_t *>(cache);
+    a.table = block_table;
+    a.d = dims_of(p);
+    a.out = static_cast<uint16_t *>(out);
+    fill_split(a, w, c, workspace);
+    return done(launch_prompt(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+}  // extern "C"

@@ -1,0 +1,277 @@
+// Gradients of causal attention over packed sequences.
+//
+// With the notation of the forward pass (rows r are (query token, query head of the KV head), P_rj = 2^(s_rj - lse_r)) and g_r
+// the gradient of out_r:
+//     dP_rj = g_r . v_j,  delta_r = g_r . out_r,  dS_rj = P_rj (dP_rj - delta_r)
+//     dq_r = c sum_j dS_rj k_j,  dk_j = c sum_r dS_rj q_r,  dv_j = sum_r P_rj g_r,  c = 1 / sqrt(128)
+// Two launches, so that every sum is made by one wavefront in a fixed order and none needs atomics: the first goes over the keys
+// of 128 rows, the second over the rows of 128 keys (all query heads of the KV head, so that nothing is left to add up).
+// Scores and weights are made in both: seven products of a pair of tiles where five would do.
+#include "lychee_prompt_device.h"
+
+namespace lychee {
+namespace {
+
+struct SharedGrad {
+    __align__(16) uint8_t a[2][kBlockBytes];
+    __align__(16) uint8_t b[2][kBlockBytes];
+    __align__(16) float lse[2][kPromptKeys];
+    __align__(16) float delta[2][kPromptKeys];
+    SharedPlan plan;
+};
+
+__device__ __forceinline__ float dot8(bf16x8_t a, bf16x8_t b, float acc)
+{
+    const u32x4_t x = __builtin_bit_cast(u32x4_t, a), y = __builtin_bit_cast(u32x4_t, b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc = dot2_bf16(x[i], y[i], acc);
+    return acc;
+}
+
+// dq, and lse and delta of every row for the second launch.  Scores and dP are made turned, as in the forward pass.
+__global__ __launch_bounds__(kThreads, 2) void prompt_dq_kernel(PromptGradArgs a)
+{
+    __shared__ SharedGrad sh;
+    const PromptRows &p = a.r;
+    const int g = blockIdx.x % p.n_kv_heads;
+    const Tile w = find_tile<false>(p, blockIdx.x / p.n_kv_heads, 0, sh.plan);
+    if (!w.found) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hi = lane >> 5;
+    const int rows = w.n * p.group, row = w.tile * kPromptRows + wave * 32 + (lane & 31);
+    const int row_in = min(row, rows - 1), pos = token_of(p, row_in), head = g * p.group + row_in - pos * p.group;
+    const int lowest = token_of(p, min(w.tile * kPromptRows + wave * 32, rows - 1));
+    const int highest = token_of(p, min(w.tile * kPromptRows + wave * 32 + 31, rows - 1));
+    const int64_t token = w.start + pos, packed = (token * (p.n_kv_heads * p.group) + head) * kHeadDim;
+    const int64_t q_at = token * p.q_tok + (int64_t)head * p.q_head;
+
+    bf16x8_t qf[8], gf[8];
+    float delta = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) {
+        qf[ks] = *(const LYCHEE_GLOBAL bf16x8_t *)(a.q + q_at + 16 * ks + 8 * hi);
+        gf[ks] = *(const LYCHEE_GLOBAL bf16x8_t *)(a.g + packed + 16 * ks + 8 * hi);
+        delta = dot8(gf[ks], *(const LYCHEE_GLOBAL bf16x8_t *)(a.out + packed + 16 * ks + 8 * hi), delta);
+    }
+    delta = sum_halves32(delta);
+    const float lse = gload(a.lse + (int64_t)head * p.n_tokens + token) * kLog2e;
+    if (row < rows && hi == 0) gstore_f2(a.stat + ((int64_t)head * p.n_tokens + token) * 2, make_float2(lse, delta));
+
+    const uint32_t row_at = row_place(lane), turn_at = turn_place(lane);
+    const int64_t base = (int64_t)w.start * a.kv_tok + (int64_t)g * a.kv_head;
+    const uint32_t to_k = lds_address(sh.a) + wave * 4 * kRowBytes, to_v = lds_address(sh.b) + wave * 4 * kRowBytes;
+    const int fetch_row = 4 * wave + (lane >> 4);
+    const uint32_t fetch_chunk = (uint32_t)((lane & 15) ^ swizzle(fetch_row)) << 4;
+    const uint32_t fetch_at = (uint32_t)fetch_row * (uint32_t)(2 * a.kv_tok) + fetch_chunk;
+    const auto fetch = [&](int blk, int buf) {
+        const int j0 = blk * kPromptKeys;
+        const bool whole = j0 + kPromptKeys <= w.len;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t from = base + (int64_t)(whole ? j0 + 16 * i : j0) * a.kv_tok;
+            const uint32_t off = whole ? fetch_at : (uint32_t)min(fetch_row + 16 * i, w.len - 1 - j0) * (uint32_t)(2 * a.kv_tok) + fetch_chunk;
+            copy16(a.k + from, off, to_k + buf * kBlockBytes + i * 16 * kRowBytes);
+            copy16(a.v + from, off, to_v + buf * kBlockBytes + i * 16 * kRowBytes);
+        }
+    };
+
+    f32x16_t dq[4];
+    bool careful = false;
+    for (;;) {
+#pragma unroll
+        for (int db = 0; db < 4; ++db) dq[db] = zero16();
+        fetch(0, 0);
+        wait_copies();
+        __syncthreads();
+        for (int blk = 0; blk < w.last; ++blk) {
+            const int buf = blk & 1, j0 = blk * kPromptKeys;
+            if (blk + 1 < w.last) fetch(blk + 1, buf ^ 1);
+            const LYCHEE_LDS uint8_t *K = (const LYCHEE_LDS uint8_t *)sh.a[buf], *V = (const LYCHEE_LDS uint8_t *)sh.b[buf];
+            if (j0 <= highest) {
+                const bool masked = j0 + kPromptKeys - 1 > lowest;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const uint32_t kat = opaque(row_at), vat = opaque(turn_at);
+                    f32x16_t z = zero16(), dp = zero16();
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks) {
+                        z = mfma(read_rows(K, kat, x, ks), qf[ks], z);
+                        dp = mfma(read_rows(V, kat, x, ks), gf[ks], dp);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[i] = fast_exp2(__builtin_fmaf(z[i], a.scale_log2e, -lse)) * (dp[i] - delta);
+                    if (masked) {
+                        const int lim = pos - j0 - 32 * x - 4 * hi;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) z[i] = i % 4 + 8 * (i / 4) <= lim ? z[i] : 0.f;
+                    }
+                    const bf16x8_t ds[2] = {operand<0>(z), operand<8>(z)};
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        if (__builtin_expect(careful && masked, 0)) {
+                            const bf16x8_t seen = seen_rows(hi, 2 * x + s, 0, pos - j0);
+#pragma unroll
+                            for (int db = 0; db < 4; ++db) {
+                                dq[db] = mfma_careful(read_turned(K, opaque(vat), db, 2 * x + s), ds[s], seen, dq[db]);
+                                __builtin_amdgcn_sched_barrier(0);
+                            }
+                        } else {
+#pragma unroll
+                            for (int db = 0; db < 4; ++db) dq[db] = mfma(read_turned(K, vat, db, 2 * x + s), ds[s], dq[db]);
+                        }
+                    }
+                }
+            }
+            wait_copies();
+            __syncthreads();
+        }
+        if (careful || !__syncthreads_or(!all_finite(dq))) break;  // (as in the forward pass)
+        careful = true;
+    }
+    store_row(row < rows ? a.dq + q_at : nullptr, lane, dq, a.scale);
+}
+
+// dk and dv.  A wavefront has 32 keys, whose rows of K and V stay in registers, and goes over the rows that see them, 64 at a time:
+// queries and output gradients in LDS, scores and dP with a lane for a key, so that P and dS are B operands of the sums over
+// the rows.
+__global__ __launch_bounds__(kThreads, 2) void prompt_dkv_kernel(PromptGradArgs a)
+{
+    __shared__ SharedGrad sh;
+    const PromptRows &p = a.r;
+    const int g = blockIdx.x % p.n_kv_heads;
+    PromptRows keys = p;
+    keys.group = 1;  // (tiles of keys)
+    const Tile w = find_tile<false>(keys, blockIdx.x / p.n_kv_heads, 0, sh.plan);
+    if (!w.found) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hi = lane >> 5;
+    const int tile = tiles_of(w.n) - 1 - w.tile, rows = w.n * p.group;  // (the first keys are seen by most rows)
+    const int key = tile * kPromptRows + wave * 32 + (lane & 31), key_in = min(key, w.n - 1);
+    const int64_t kv_at = (int64_t)(w.start + key_in) * a.kv_tok + (int64_t)g * a.kv_head;
+    bf16x8_t kf[8], vf[8];
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) {
+        kf[ks] = *(const LYCHEE_GLOBAL bf16x8_t *)(a.k + kv_at + 16 * ks + 8 * hi);
+        vf[ks] = *(const LYCHEE_GLOBAL bf16x8_t *)(a.v + kv_at + 16 * ks + 8 * hi);
+    }
+    const uint32_t row_at = row_place(lane), turn_at = turn_place(lane);
+    const uint32_t to_q = lds_address(sh.a) + wave * 4 * kRowBytes, to_g = lds_address(sh.b) + wave * 4 * kRowBytes;
+    const int fetch_row = 4 * wave + (lane >> 4);
+    const uint32_t fetch_chunk = (uint32_t)((lane & 15) ^ swizzle(fetch_row)) << 4;
+    const int64_t packed_tok = (int64_t)p.n_kv_heads * p.group * kHeadDim;
+    float2 stat = make_float2(0.f, 0.f);
+    const auto fetch = [&](int blk, int buf) {
+        const int r0 = blk * kPromptKeys, t0 = token_of(p, r0);
+        const uint16_t *q = a.q + (int64_t)(w.start + t0) * p.q_tok + (int64_t)g * p.group * p.q_head;
+        const uint16_t *go = a.g + (int64_t)(w.start + t0) * packed_tok + (int64_t)g * p.group * kHeadDim;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = min(r0 + fetch_row + 16 * i, rows - 1), t = token_of(p, r), h = r - t * p.group;
+            copy16(q, (uint32_t)(t - t0) * (uint32_t)(2 * p.q_tok) + (uint32_t)h * (uint32_t)(2 * p.q_head) + fetch_chunk,
+                   to_q + buf * kBlockBytes + i * 16 * kRowBytes);
+            copy16(go, (uint32_t)(t - t0) * (uint32_t)(2 * packed_tok) + (uint32_t)h * (2 * kHeadDim) + fetch_chunk,
+                   to_g + buf * kBlockBytes + i * 16 * kRowBytes);
+        }
+        if (threadIdx.x < kPromptKeys) {
+            const int r = min(r0 + (int)threadIdx.x, rows - 1), t = token_of(p, r), h = g * p.group + r - t * p.group;
+            const f32x2_t s = *(const LYCHEE_GLOBAL f32x2_t *)(a.stat + ((int64_t)h * p.n_tokens + w.start + t) * 2);
+            stat = make_float2(s[0], s[1]);
+        }
+    };
+    const auto arrive = [&](int buf) {
+        if (threadIdx.x < kPromptKeys) {
+            sh.lse[buf][threadIdx.x] = stat.x;
+            sh.delta[buf][threadIdx.x] = stat.y;
+        }
+        wait_copies();
+        __syncthreads();
+    };
+    const int first = tile * kPromptRows * p.group / kPromptKeys, last = (rows + kPromptKeys - 1) / kPromptKeys;
+    const int wave_first = (tile * kPromptRows + wave * 32) * p.group;            // rows from here on see a key of the wavefront
+    const int wave_all = (tile * kPromptRows + wave * 32 + 31) * p.group;         // and from here on all of them
+
+    f32x16_t dk[4], dv[4];
+    bool careful = false;
+    for (;;) {
+#pragma unroll
+        for (int db = 0; db < 4; ++db) dk[db] = zero16(), dv[db] = zero16();
+        fetch(first, 0);
+        arrive(0);
+        for (int blk = first; blk < last; ++blk) {
+            const int buf = (blk - first) & 1, r0 = blk * kPromptKeys;
+            if (blk + 1 < last) fetch(blk + 1, buf ^ 1);
+            const LYCHEE_LDS uint8_t *Q = (const LYCHEE_LDS uint8_t *)sh.a[buf], *G = (const LYCHEE_LDS uint8_t *)sh.b[buf];
+            if (r0 + kPromptKeys > wave_first) {
+                const bool masked = r0 < wave_all || r0 + kPromptKeys > rows;
+                const int least = key * p.group - r0, most = rows - 1 - r0;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const uint32_t kat = opaque(row_at), vat = opaque(turn_at);
+                    f32x16_t z = zero16(), dp = zero16();
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks) {
+                        z = mfma(read_rows(Q, kat, x, ks), kf[ks], z);
+                        dp = mfma(read_rows(G, kat, x, ks), vf[ks], dp);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const f32x4_t lse = *reinterpret_cast<const f32x4_t *>(&sh.lse[buf][32 * x + 8 * j + 4 * hi]);
+                        const f32x4_t delta = *reinterpret_cast<const f32x4_t *>(&sh.delta[buf][32 * x + 8 * j + 4 * hi]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            z[4 * j + i] = fast_exp2(__builtin_fmaf(z[4 * j + i], a.scale_log2e, -lse[i]));
+                            dp[4 * j + i] = z[4 * j + i] * (dp[4 * j + i] - delta[i]);
+                        }
+                    }
+                    if (masked) {
+                        const int from = least - 32 * x - 4 * hi, to = most - 32 * x - 4 * hi;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const bool seen = i % 4 + 8 * (i / 4) >= from && i % 4 + 8 * (i / 4) <= to;
+                            z[i] = seen ? z[i] : 0.f;
+                            dp[i] = seen ? dp[i] : 0.f;
+                        }
+                    }
+                    const bf16x8_t pf[2] = {operand<0>(z), operand<8>(z)}, ds[2] = {operand<0>(dp), operand<8>(dp)};
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        if (__builtin_expect(careful && masked, 0)) {
+                            const bf16x8_t seen = seen_rows(hi, 2 * x + s, least, most);
+#pragma unroll
+                            for (int db = 0; db < 4; ++db) {
+                                dv[db] = mfma_careful(read_turned(G, opaque(vat), db, 2 * x + s), pf[s], seen, dv[db]);
+                                __builtin_amdgcn_sched_barrier(0);
+                                dk[db] = mfma_careful(read_turned(Q, opaque(vat), db, 2 * x + s), ds[s], seen, dk[db]);
+                                __builtin_amdgcn_sched_barrier(0);
+                            }
+                        } else {
+#pragma unroll
+                            for (int db = 0; db < 4; ++db) {
+                                dv[db] = mfma(read_turned(G, vat, db, 2 * x + s), pf[s], dv[db]);
+                                dk[db] = mfma(read_turned(Q, vat, db, 2 * x + s), ds[s], dk[db]);
+                            }
+                        }
+                    }
+                }
+            }
+            arrive(buf ^ 1);
+        }
+        if (careful || !__syncthreads_or(!all_finite(dk) || !all_finite(dv))) break;
+        careful = true;
+    }
+    const bool there = key < w.n;
+    store_row(there ? a.dk + kv_at : nullptr, lane, dk, a.scale);
+    store_row(there ? a.dv + kv_at : nullptr, lane, dv, 1.f);
+}
+
+}  // namespace
+
+hipError_t launch_prompt_grad(const PromptGradArgs &a, hipStream_t stream)
+{
+    const unsigned heads = (unsigned)a.r.n_kv_heads;
+    prompt_dq_kernel<<<(unsigned)a.n_row_tiles * heads, kThreads, 0, stream>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    prompt_dkv_kernel<<<(unsigned)a.n_key_tiles * heads, kThreads, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace lychee
