@@ -45,8 +45,8 @@ struct PromptGradArgs {
     const float *lse;
     int64_t kv_head, kv_tok;
     uint16_t *dq, *dk, *dv;  // strided like q, k and v
-    float *stat;             // [n_q_heads][n_tokens][2] lse in log2 units, g . out
-    float scale, scale_log2e;
+    float *stat;             // [2][n_q_heads][n_tokens] -lse sqrt(128), -(g . out): what the products of the second launch begin with
+    float scale, scale_log2e, root;  // 1 / sqrt(128), log2(e) / sqrt(128), sqrt(128)
     int32_t n_row_tiles, n_key_tiles;  // of a KV head, at most
 };
 

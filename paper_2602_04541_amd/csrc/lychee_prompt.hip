@@ -82,7 +82,6 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
                 for (int i = 0; i < 16; ++i) bad |= (uint32_t)(~there >> (4 * i) & 1) << i;
                 sh.bad[buf][wave] = (uint16_t)bad;
             }
-            if (blk + 1 < w.last) fetch_entry(blk + 1);
         } else {
             const bool whole = j0 + kPromptKeys <= w.len;  // (else the last key again in the rows behind it)
 #pragma unroll
@@ -114,20 +113,26 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
     float m, l;
     bool careful = false;
     for (;;) {
+        const int each = careful ? 3 : 1, turns = each * max(w.last - w.first, 0);  // (take_with_care)
+        const auto block_of = [&](int turn) { return w.first + (careful ? turn / 3 : turn); };
 #pragma unroll
         for (int db = 0; db < 4; ++db) o[db] = zero16();
         m = -__builtin_inff();
         l = 0.f;
-        if (w.first < w.last) {
+        if (turns > 0) {
             if (Q4) fetch_entry(w.first);
             fetch(w.first, 0);
+            if (Q4) fetch_entry(block_of(min(1, turns - 1)));
         }
         arrive(0);
-        for (int blk = w.first; blk < w.last; ++blk) {
-            const int buf = (blk - w.first) & 1, j0 = blk * kPromptKeys;
-            if (blk + 1 < w.last) fetch(blk + 1, buf ^ 1);
+        for (int turn = 0; turn < turns; ++turn) {
+            const int blk = block_of(turn), buf = turn & 1, j0 = blk * kPromptKeys;
+            if (turn + 1 < turns) {
+                fetch(block_of(turn + 1), buf ^ 1);
+                if (Q4) fetch_entry(block_of(min(turn + 2, turns - 1)));
+            }
             const LYCHEE_LDS uint8_t *K = (const LYCHEE_LDS uint8_t *)sh.k[buf], *V = (const LYCHEE_LDS uint8_t *)sh.v[buf];
-            if (j0 <= highest) {
+            if (careful || j0 <= highest) {
                 const uint32_t kat = opaque(row_at), vat = opaque(turn_at);
                 f32x16_t z[2] = {zero16(), zero16()};
 #pragma unroll
@@ -139,8 +144,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
                     const uint2 words = *reinterpret_cast<const uint2 *>(sh.bad[buf]);
                     bad = (uint64_t)__builtin_amdgcn_readfirstlane(words.y) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane(words.x);
                 }
-                const bool masked = j0 + kPromptKeys - 1 > lowest || bad != 0;
-                if (masked) {
+                if (j0 + kPromptKeys - 1 > lowest || bad != 0) {
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
                         const int n = min(max(pos - j0 - 32 * x + 1, 0), 32);
@@ -167,7 +171,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) o[db][i] *= f;
                 }
-                const float ref = m == -__builtin_inff() ? 0.f : m;
+                const float ref = m == -__builtin_inff() ? 0.f : m, before = l;
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
 #pragma unroll
@@ -176,28 +180,23 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
                         l += z[x][i];
                     }
                 bf16x8_t pf[4] = {operand<0>(z[0]), operand<8>(z[0]), operand<0>(z[1]), operand<8>(z[1])};
-                if (__builtin_expect(careful && masked, 0)) {
-#pragma unroll 1
-                    for (int s = 0; s < 4; ++s) {
-                        const bf16x8_t seen = seen_rows(hi, s, 0, pos - j0);
-                        const bf16x8_t weights = s < 2 ? (s == 0 ? pf[0] : pf[1]) : (s == 2 ? pf[2] : pf[3]);
+                if (__builtin_expect(careful, 0)) {
+                    __syncthreads();
+                    take_with_care(sh.v[buf], turn % 3);
+                    __syncthreads();
+                    if (turn % 3 != 0) {
+                        l = before;
 #pragma unroll
-                        for (int db = 0; db < 4; ++db) {
-                            o[db] = mfma_careful(read_turned(V, opaque(vat), db, s), weights, seen, o[db]);
-                            __builtin_amdgcn_sched_barrier(0);
-                        }
+                        for (int s = 0; s < 4; ++s) pf[s] = seen_rows(hi, s, 0, pos - j0);
                     }
-                } else {
-#pragma unroll
-                    for (int s = 0; s < 4; ++s)
-#pragma unroll
-                        for (int db = 0; db < 4; ++db) o[db] = mfma(read_turned(V, vat, db, s), pf[s], o[db]);
                 }
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+#pragma unroll
+                    for (int db = 0; db < 4; ++db) o[db] = mfma(read_turned(V, vat, db, s), pf[s], o[db]);
             }
             arrive(buf ^ 1);
         }
-        // A key's value counts for the rows that see it alone, but a weight of zero times an infinite value or NaN is NaN: a
-        // tile in which that may have happened is done again, with care.
         if (careful || !__syncthreads_or(!all_finite(o))) break;
         careful = true;
     }

@@ -188,6 +188,7 @@ int lychee_prompt_attn_backward(lychee_ctx *ctx, const lychee_prompt *prompt, co
     a.stat = reinterpret_cast<float *>(static_cast<char *>(workspace) + c.stat);
     a.scale = (float)(1.0 / sqrt((double)kHeadDim));
     a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)kHeadDim));
+    a.root = (float)sqrt((double)kHeadDim);
     a.n_row_tiles = (int32_t)grid_of(p.batch, p.n_kv_heads, a.r.group, p.n_tokens, 0).tiles;
     a.n_key_tiles = (int32_t)grid_of(p.batch, p.n_kv_heads, 1, p.n_tokens, 0).tiles;
     return done(launch_prompt_grad(a, static_cast<hipStream_t>(hip_stream)));

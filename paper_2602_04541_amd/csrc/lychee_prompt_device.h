@@ -54,13 +54,14 @@ __device__ __forceinline__ bf16x8_t operand(const f32x16_t &d)
                                                pk_bf16(d[kFirst + 4], d[kFirst + 5]), pk_bf16(d[kFirst + 6], d[kFirst + 7])});
 }
 
-__device__ __forceinline__ f32x16_t zero16()
+__device__ __forceinline__ f32x16_t all16(float x)
 {
     f32x16_t z;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) z[i] = 0.f;
+    for (int i = 0; i < 16; ++i) z[i] = x;
     return z;
 }
+__device__ __forceinline__ f32x16_t zero16() { return all16(0.f); }
 
 // ------------------------------------------------------------------------------ rows
 __device__ __forceinline__ int token_of(const PromptRows &p, int row) { return p.group == 1 ? row : (int)__umulhi((uint32_t)row, p.group_magic); }
@@ -183,6 +184,10 @@ __device__ __forceinline__ void copy16(const uint16_t *base, uint32_t offset, ui
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
 }
+__device__ __forceinline__ void copy4(const float *base, uint32_t offset, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+}
 __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(const LYCHEE_LDS uint8_t *)p; }
 
@@ -221,25 +226,28 @@ __device__ __forceinline__ uint32_t opaque(uint32_t x)
     return x;
 }
 
-// acc += A B where B is zero for pairs that must not count, although A may hold infinities and NaN, which times zero are NaN.
-// These are taken out of A, and put back through finite numbers: the largest bf16 number, squared, is an infinity in
-// fp32, for the pairs that count (`seen`: that number or zero), and a NaN is both infinities.
+// Pairs that must not count have a weight of zero, but zero times an infinity or NaN is NaN.  A workgroup whose sums hold
+// no numbers makes them again with care, every block three times: with zeros for such values (turn 0), and then with finite numbers
+// that put them back where they count.  The largest bf16 number, squared, is an infinity in fp32: turn 1 has it, with its
+// sign, for infinities and NaN, the products' other operand being that number for the pairs that count and zero for the others
+// (seen_rows), and turn 2 its negative for NaN, which both infinities add up to.  The block is changed in LDS, behind the products
+// that make the scores.
 constexpr uint32_t kLargest = 0x7F7Fu;
-__device__ __forceinline__ f32x16_t mfma_careful(bf16x8_t a, bf16x8_t b, bf16x8_t seen, f32x16_t acc)
+__device__ __forceinline__ void take_with_care(uint8_t *block, int turn)
 {
-    typedef unsigned short u16x8_t __attribute__((ext_vector_type(8)));
-    const u16x8_t x = __builtin_bit_cast(u16x8_t, a);
-    u16x8_t clean, first, second;
+#pragma unroll 1
+    for (int i = threadIdx.x; i < kBlockBytes / 4; i += kThreads) {
+        uint32_t *at = reinterpret_cast<uint32_t *>(block) + i, both = *at, to = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint32_t mag = x[e] & 0x7FFFu;
-        clean[e] = mag >= 0x7F80u ? 0 : x[e];
-        first[e] = mag == 0x7F80u ? (x[e] & 0x8000u) | kLargest : mag > 0x7F80u ? kLargest : 0;
-        second[e] = mag > 0x7F80u ? 0x8000u | kLargest : 0;
+        for (int h = 0; h < 32; h += 16) {
+            const uint32_t x = both >> h & 0xFFFFu, size = x & 0x7FFFu;
+            uint32_t y = size < 0x7F80u ? x : 0u;
+            if (turn == 1) y = size < 0x7F80u ? 0u : size > 0x7F80u ? kLargest : (x & 0x8000u) | kLargest;
+            if (turn == 2) y = size > 0x7F80u ? 0x8000u | kLargest : 0u;
+            to |= y << h;
+        }
+        *at = to;
     }
-    acc = mfma(__builtin_bit_cast(bf16x8_t, clean), b, acc);
-    acc = mfma(__builtin_bit_cast(bf16x8_t, first), seen, acc);
-    return mfma(__builtin_bit_cast(bf16x8_t, second), seen, acc);
 }
 // The pairs that count, of step s in the order of read_turned: rows least .. most of the block's.
 __device__ __forceinline__ bf16x8_t seen_rows(int hi, int s, int least, int most)

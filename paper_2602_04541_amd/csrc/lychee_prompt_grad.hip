@@ -12,13 +12,20 @@
 namespace lychee {
 namespace {
 
+constexpr int kHeld = 5;  // of the second launch's eight steps of V those that stay in registers
+
 struct SharedGrad {
-    __align__(16) uint8_t a[2][kBlockBytes];
-    __align__(16) uint8_t b[2][kBlockBytes];
-    __align__(16) float lse[2][kPromptKeys];
-    __align__(16) float delta[2][kPromptKeys];
-    SharedPlan plan;
+    union {
+        SharedPlan plan;
+        struct {
+            __align__(16) uint8_t a[2][kBlockBytes];
+            __align__(16) uint8_t b[2][kBlockBytes];
+            __align__(16) float stat[2][2][kPromptKeys];  // second launch, of a block's rows: -lse sqrt(128), -delta
+            __align__(16) bf16x8_t v[kWaves][8 - kHeld][64];
+        };
+    };
 };
+static_assert(sizeof(SharedGrad) <= 80 * 1024, "two workgroups a compute unit");
 
 __device__ __forceinline__ float dot8(bf16x8_t a, bf16x8_t b, float acc)
 {
@@ -36,6 +43,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dq_kernel(PromptGradArgs a
     const int g = blockIdx.x % p.n_kv_heads;
     const Tile w = find_tile<false>(p, blockIdx.x / p.n_kv_heads, 0, sh.plan);
     if (!w.found) return;
+    __syncthreads();  // (the plan's part of LDS is free)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hi = lane >> 5;
     const int rows = w.n * p.group, row = w.tile * kPromptRows + wave * 32 + (lane & 31);
     const int row_in = min(row, rows - 1), pos = token_of(p, row_in), head = g * p.group + row_in - pos * p.group;
@@ -52,9 +60,13 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dq_kernel(PromptGradArgs a
         gf[ks] = *(const LYCHEE_GLOBAL bf16x8_t *)(a.g + packed + 16 * ks + 8 * hi);
         delta = dot8(gf[ks], *(const LYCHEE_GLOBAL bf16x8_t *)(a.out + packed + 16 * ks + 8 * hi), delta);
     }
-    delta = sum_halves32(delta);
-    const float lse = gload(a.lse + (int64_t)head * p.n_tokens + token) * kLog2e;
-    if (row < rows && hi == 0) gstore_f2(a.stat + ((int64_t)head * p.n_tokens + token) * 2, make_float2(lse, delta));
+    // What the products begin with, in units of q . k and of g . v
+    const float less_delta = -sum_halves32(delta), less_lse = -gload(a.lse + (int64_t)head * p.n_tokens + token) * a.root;
+    if (row < rows && hi == 0) {
+        float *stat = a.stat + (int64_t)head * p.n_tokens + token;
+        gstore(stat, less_lse);
+        gstore(stat + (int64_t)p.n_kv_heads * p.group * p.n_tokens, less_delta);
+    }
 
     const uint32_t row_at = row_place(lane), turn_at = turn_place(lane);
     const int64_t base = (int64_t)w.start * a.kv_tok + (int64_t)g * a.kv_head;
@@ -77,54 +89,57 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dq_kernel(PromptGradArgs a
     f32x16_t dq[4];
     bool careful = false;
     for (;;) {
+        // with care, every block comes three times for either half of its keys (take_with_care)
+        const int turns = careful ? 6 * w.last : w.last;
+        const auto block_of = [&](int turn) { return careful ? turn / 6 : turn; };
 #pragma unroll
         for (int db = 0; db < 4; ++db) dq[db] = zero16();
         fetch(0, 0);
         wait_copies();
         __syncthreads();
-        for (int blk = 0; blk < w.last; ++blk) {
-            const int buf = blk & 1, j0 = blk * kPromptKeys;
-            if (blk + 1 < w.last) fetch(blk + 1, buf ^ 1);
+        for (int turn = 0; turn < turns; ++turn) {
+            const int blk = block_of(turn), buf = turn & 1, j0 = blk * kPromptKeys;
+            if (turn + 1 < turns) fetch(block_of(turn + 1), buf ^ 1);
             const LYCHEE_LDS uint8_t *K = (const LYCHEE_LDS uint8_t *)sh.a[buf], *V = (const LYCHEE_LDS uint8_t *)sh.b[buf];
-            if (j0 <= highest) {
+            if (careful || j0 <= highest) {
                 const bool masked = j0 + kPromptKeys - 1 > lowest;
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
+                    if (careful && turn % 2 != x) continue;
                     const uint32_t kat = opaque(row_at), vat = opaque(turn_at);
-                    f32x16_t z = zero16(), dp = zero16();
+                    f32x16_t z = all16(less_lse), dp = all16(less_delta);
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks) {
                         z = mfma(read_rows(K, kat, x, ks), qf[ks], z);
                         dp = mfma(read_rows(V, kat, x, ks), gf[ks], dp);
                     }
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) z[i] = fast_exp2(__builtin_fmaf(z[i], a.scale_log2e, -lse)) * (dp[i] - delta);
+                    for (int i = 0; i < 16; ++i) z[i] = fast_exp2(z[i] * a.scale_log2e) * dp[i];
                     if (masked) {
                         const int lim = pos - j0 - 32 * x - 4 * hi;
 #pragma unroll
                         for (int i = 0; i < 16; ++i) z[i] = i % 4 + 8 * (i / 4) <= lim ? z[i] : 0.f;
                     }
-                    const bf16x8_t ds[2] = {operand<0>(z), operand<8>(z)};
+                    bf16x8_t ds[2] = {operand<0>(z), operand<8>(z)};
+                    if (__builtin_expect(careful, 0)) {
+                        __syncthreads();
+                        take_with_care(sh.a[buf], turn / 2 % 3);
+                        __syncthreads();
+                        if (turn / 2 % 3 != 0) {
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        if (__builtin_expect(careful && masked, 0)) {
-                            const bf16x8_t seen = seen_rows(hi, 2 * x + s, 0, pos - j0);
-#pragma unroll
-                            for (int db = 0; db < 4; ++db) {
-                                dq[db] = mfma_careful(read_turned(K, opaque(vat), db, 2 * x + s), ds[s], seen, dq[db]);
-                                __builtin_amdgcn_sched_barrier(0);
-                            }
-                        } else {
-#pragma unroll
-                            for (int db = 0; db < 4; ++db) dq[db] = mfma(read_turned(K, vat, db, 2 * x + s), ds[s], dq[db]);
+                            for (int s = 0; s < 2; ++s) ds[s] = seen_rows(hi, 2 * x + s, 0, pos - j0);
                         }
                     }
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int db = 0; db < 4; ++db) dq[db] = mfma(read_turned(K, vat, db, 2 * x + s), ds[s], dq[db]);
                 }
             }
             wait_copies();
             __syncthreads();
         }
-        if (careful || !__syncthreads_or(!all_finite(dq))) break;  // (as in the forward pass)
+        if (careful || !__syncthreads_or(!all_finite(dq))) break;
         careful = true;
     }
     store_row(row < rows ? a.dq + q_at : nullptr, lane, dq, a.scale);
@@ -146,41 +161,41 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dkv_kernel(PromptGradArgs 
     const int tile = tiles_of(w.n) - 1 - w.tile, rows = w.n * p.group;  // (the first keys are seen by most rows)
     const int key = tile * kPromptRows + wave * 32 + (lane & 31), key_in = min(key, w.n - 1);
     const int64_t kv_at = (int64_t)(w.start + key_in) * a.kv_tok + (int64_t)g * a.kv_head;
-    bf16x8_t kf[8], vf[8];
+    __syncthreads();  // (the plan's part of LDS is free)
+    bf16x8_t kf[8], vf[kHeld];
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) {
         kf[ks] = *(const LYCHEE_GLOBAL bf16x8_t *)(a.k + kv_at + 16 * ks + 8 * hi);
-        vf[ks] = *(const LYCHEE_GLOBAL bf16x8_t *)(a.v + kv_at + 16 * ks + 8 * hi);
+        const bf16x8_t v = *(const LYCHEE_GLOBAL bf16x8_t *)(a.v + kv_at + 16 * ks + 8 * hi);
+        if (ks < kHeld)
+            vf[ks] = v;
+        else
+            sh.v[wave][ks - kHeld][lane] = v;
     }
     const uint32_t row_at = row_place(lane), turn_at = turn_place(lane);
     const uint32_t to_q = lds_address(sh.a) + wave * 4 * kRowBytes, to_g = lds_address(sh.b) + wave * 4 * kRowBytes;
-    const int fetch_row = 4 * wave + (lane >> 4);
-    const uint32_t fetch_chunk = (uint32_t)((lane & 15) ^ swizzle(fetch_row)) << 4;
     const int64_t packed_tok = (int64_t)p.n_kv_heads * p.group * kHeadDim;
-    float2 stat = make_float2(0.f, 0.f);
     const auto fetch = [&](int blk, int buf) {
-        const int r0 = blk * kPromptKeys, t0 = token_of(p, r0);
+        const int r0 = blk * kPromptKeys, t0 = token_of(p, r0), at = (int)opaque(lane);
+        const int fetch_row = r0 + 4 * wave + (at >> 4);
+        const uint32_t fetch_chunk = (uint32_t)((at & 15) ^ swizzle(fetch_row)) << 4;
         const uint16_t *q = a.q + (int64_t)(w.start + t0) * p.q_tok + (int64_t)g * p.group * p.q_head;
         const uint16_t *go = a.g + (int64_t)(w.start + t0) * packed_tok + (int64_t)g * p.group * kHeadDim;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int r = min(r0 + fetch_row + 16 * i, rows - 1), t = token_of(p, r), h = r - t * p.group;
+            const int r = min(fetch_row + 16 * i, rows - 1), t = token_of(p, r), h = r - t * p.group;
             copy16(q, (uint32_t)(t - t0) * (uint32_t)(2 * p.q_tok) + (uint32_t)h * (uint32_t)(2 * p.q_head) + fetch_chunk,
                    to_q + buf * kBlockBytes + i * 16 * kRowBytes);
             copy16(go, (uint32_t)(t - t0) * (uint32_t)(2 * packed_tok) + (uint32_t)h * (2 * kHeadDim) + fetch_chunk,
                    to_g + buf * kBlockBytes + i * 16 * kRowBytes);
         }
-        if (threadIdx.x < kPromptKeys) {
-            const int r = min(r0 + (int)threadIdx.x, rows - 1), t = token_of(p, r), h = g * p.group + r - t * p.group;
-            const f32x2_t s = *(const LYCHEE_GLOBAL f32x2_t *)(a.stat + ((int64_t)h * p.n_tokens + w.start + t) * 2);
-            stat = make_float2(s[0], s[1]);
+        if (wave < 2) {
+            const int r = min(r0 + at, rows - 1), t = token_of(p, r), h = r - t * p.group;
+            copy4(a.stat + ((int64_t)wave * p.n_kv_heads + g) * p.group * p.n_tokens + w.start, ((uint32_t)h * (uint32_t)p.n_tokens + (uint32_t)t) * 4u,
+                  lds_address(sh.stat[buf][wave]));
         }
     };
-    const auto arrive = [&](int buf) {
-        if (threadIdx.x < kPromptKeys) {
-            sh.lse[buf][threadIdx.x] = stat.x;
-            sh.delta[buf][threadIdx.x] = stat.y;
-        }
+    const auto arrive = [&](int) {
         wait_copies();
         __syncthreads();
     };
@@ -191,35 +206,40 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dkv_kernel(PromptGradArgs 
     f32x16_t dk[4], dv[4];
     bool careful = false;
     for (;;) {
+        const int turns = (careful ? 6 : 1) * (last - first);  // (as for dq)
+        const auto block_of = [&](int turn) { return first + (careful ? turn / 6 : turn); };
 #pragma unroll
         for (int db = 0; db < 4; ++db) dk[db] = zero16(), dv[db] = zero16();
         fetch(first, 0);
         arrive(0);
-        for (int blk = first; blk < last; ++blk) {
-            const int buf = (blk - first) & 1, r0 = blk * kPromptKeys;
-            if (blk + 1 < last) fetch(blk + 1, buf ^ 1);
+        for (int turn = 0; turn < turns; ++turn) {
+            const int blk = block_of(turn), buf = turn & 1, r0 = blk * kPromptKeys;
+            if (turn + 1 < turns) fetch(block_of(turn + 1), buf ^ 1);
             const LYCHEE_LDS uint8_t *Q = (const LYCHEE_LDS uint8_t *)sh.a[buf], *G = (const LYCHEE_LDS uint8_t *)sh.b[buf];
-            if (r0 + kPromptKeys > wave_first) {
+            if (careful || r0 + kPromptKeys > wave_first) {
                 const bool masked = r0 < wave_all || r0 + kPromptKeys > rows;
                 const int least = key * p.group - r0, most = rows - 1 - r0;
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
+                    if (careful && turn % 2 != x) continue;
                     const uint32_t kat = opaque(row_at), vat = opaque(turn_at);
-                    f32x16_t z = zero16(), dp = zero16();
+                    f32x16_t z, dp;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const f32x4_t l = *reinterpret_cast<const f32x4_t *>(&sh.stat[buf][0][32 * x + 8 * j + 4 * hi]);
+                        const f32x4_t d = *reinterpret_cast<const f32x4_t *>(&sh.stat[buf][1][32 * x + 8 * j + 4 * hi]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) z[4 * j + i] = l[i], dp[4 * j + i] = d[i];
+                    }
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks) {
                         z = mfma(read_rows(Q, kat, x, ks), kf[ks], z);
-                        dp = mfma(read_rows(G, kat, x, ks), vf[ks], dp);
+                        dp = mfma(read_rows(G, kat, x, ks), ks < kHeld ? vf[ks] : ((const LYCHEE_LDS bf16x8_t *)sh.v[wave][ks - kHeld])[lane], dp);
                     }
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const f32x4_t lse = *reinterpret_cast<const f32x4_t *>(&sh.lse[buf][32 * x + 8 * j + 4 * hi]);
-                        const f32x4_t delta = *reinterpret_cast<const f32x4_t *>(&sh.delta[buf][32 * x + 8 * j + 4 * hi]);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            z[4 * j + i] = fast_exp2(__builtin_fmaf(z[4 * j + i], a.scale_log2e, -lse[i]));
-                            dp[4 * j + i] = z[4 * j + i] * (dp[4 * j + i] - delta[i]);
-                        }
+                    for (int i = 0; i < 16; ++i) {
+                        z[i] = fast_exp2(z[i] * a.scale_log2e);
+                        dp[i] *= z[i];
                     }
                     if (masked) {
                         const int from = least - 32 * x - 4 * hi, to = most - 32 * x - 4 * hi;
@@ -230,26 +250,24 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dkv_kernel(PromptGradArgs 
                             dp[i] = seen ? dp[i] : 0.f;
                         }
                     }
-                    const bf16x8_t pf[2] = {operand<0>(z), operand<8>(z)}, ds[2] = {operand<0>(dp), operand<8>(dp)};
+                    bf16x8_t pf[2] = {operand<0>(z), operand<8>(z)}, ds[2] = {operand<0>(dp), operand<8>(dp)};
+                    if (__builtin_expect(careful, 0)) {
+                        __syncthreads();
+                        take_with_care(sh.a[buf], turn / 2 % 3);
+                        take_with_care(sh.b[buf], turn / 2 % 3);
+                        __syncthreads();
+                        if (turn / 2 % 3 != 0) {
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        if (__builtin_expect(careful && masked, 0)) {
-                            const bf16x8_t seen = seen_rows(hi, 2 * x + s, least, most);
-#pragma unroll
-                            for (int db = 0; db < 4; ++db) {
-                                dv[db] = mfma_careful(read_turned(G, opaque(vat), db, 2 * x + s), pf[s], seen, dv[db]);
-                                __builtin_amdgcn_sched_barrier(0);
-                                dk[db] = mfma_careful(read_turned(Q, opaque(vat), db, 2 * x + s), ds[s], seen, dk[db]);
-                                __builtin_amdgcn_sched_barrier(0);
-                            }
-                        } else {
-#pragma unroll
-                            for (int db = 0; db < 4; ++db) {
-                                dv[db] = mfma(read_turned(G, vat, db, 2 * x + s), pf[s], dv[db]);
-                                dk[db] = mfma(read_turned(Q, vat, db, 2 * x + s), ds[s], dk[db]);
-                            }
+                            for (int s = 0; s < 2; ++s) pf[s] = ds[s] = seen_rows(hi, 2 * x + s, least, most);
                         }
                     }
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int db = 0; db < 4; ++db) {
+                            dv[db] = mfma(read_turned(G, vat, db, 2 * x + s), pf[s], dv[db]);
+                            dk[db] = mfma(read_turned(Q, vat, db, 2 * x + s), ds[s], dk[db]);
+                        }
                 }
             }
             arrive(buf ^ 1);
