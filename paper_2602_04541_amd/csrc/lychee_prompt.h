@@ -10,6 +10,7 @@ constexpr int kPromptMaxGroup = 16;
 constexpr int kPromptRows = 128;          // query rows of a tile, a row being a (token, query head of the KV head)
 constexpr int kPromptKeys = 64;           // keys a workgroup takes at a time
 constexpr int kPromptMinPiece = 4;        // blocks of keys in a piece of a split tile, at least
+constexpr int kPromptMinRowPiece = 4;     // and blocks of rows in a piece of a tile of keys
 constexpr int64_t kPromptMaxRows = 1 << 28;  // query tokens times heads of a group (row numbers are divided with a multiplication)
 constexpr int64_t kPromptMaxStride = 1 << 24;  // elements from a token's row to the next (offsets within 64 rows fit 32 bits)
 
@@ -32,10 +33,11 @@ struct PromptArgs {
     PagedDims d;
     uint16_t *out;      // [n_tokens][n_q_heads][128]
     float *lse;         // [n_q_heads][n_tokens] or nullptr
-    float *part_o;      // [piece][kPromptRows][128] un-normalised partial outputs
-    float *part_ml;     // [piece][kPromptRows][2]   maximum (log2 units) and sum
+    float *part_o;      // [piece][wavefront][16][64][4] un-normalised partial outputs, as registers and lanes hold them
+    float *part_ml;     // [piece][kPromptRows][2]       maximum (log2 units) and sum
     int32_t slots;      // 0: tiles are not split; else the pieces that fill the device
-    int32_t n_items, n_tiles;  // pieces and tiles of a KV head that the launch has room for
+    int32_t merge_split;  // workgroups that share 32 rows of a tile in the merge
+    int32_t n_items, n_tiles, n_slots;  // pieces, tiles and partials of a KV head that the launch has room for
     float scale_log2e;
 };
 
@@ -47,7 +49,9 @@ struct PromptGradArgs {
     uint16_t *dq, *dk, *dv;  // strided like q, k and v
     float *stat;             // [2][n_q_heads][n_tokens] -lse sqrt(128), -(g . out): what the products of the second launch begin with
     float scale, scale_log2e, root;  // 1 / sqrt(128), log2(e) / sqrt(128), sqrt(128)
-    int32_t n_row_tiles, n_key_tiles;  // of a KV head, at most
+    float *part;             // [piece][wavefront][dk, dv][16][64][4] sums over a piece's rows, as registers and lanes hold them
+    int32_t slots;           // pieces that tiles of keys are split into, about
+    int32_t n_row_tiles, n_key_tiles, n_key_items, n_slots;  // of a KV head, at most
 };
 
 hipError_t launch_prompt(const PromptArgs &a, hipStream_t stream);

@@ -29,7 +29,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
     const PromptRows &p = a.r;
     const int g = blockIdx.x % p.n_kv_heads;
     const Tile w = find_tile<false>(p, blockIdx.x / p.n_kv_heads, a.slots, sh.plan);
-    if (!w.found || (w.piece > 0 && w.first >= w.last)) return;
+    if (!w.found || (w.piece > 0 && w.first >= w.last) || (w.parts > 1 && w.slot >= a.n_slots)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hi = lane >> 5;
     const int rows = w.n * p.group, row = w.tile * kPromptRows + wave * 32 + (lane & 31);
     const int row_in = min(row, rows - 1), token = token_of(p, row_in), head = g * p.group + row_in - token * p.group;
@@ -208,51 +208,91 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
         if (a.lse && there && hi == 0)
             gstore(a.lse + (int64_t)head * p.n_tokens + w.start + token, l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * (1.f / kLog2e));
     } else {
-        const int64_t slot = (int64_t)w.item * p.n_kv_heads + g;
-        float *po = a.part_o + (slot * kPromptRows + wave * 32 + (lane & 31)) * kHeadDim + 4 * hi;
+        // in the order of the registers: 1 KB a store, read back alike
+        const int64_t at = ((int64_t)w.slot * p.n_kv_heads + g) * kWaves + wave;
+        float *po = a.part_o + at * (64 * 64) + 4 * lane;
 #pragma unroll
         for (int db = 0; db < 4; ++db)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) *(LYCHEE_GLOBAL f32x4_t *)(po + 32 * db + 8 * j) = f32x4_t{o[db][4 * j], o[db][4 * j + 1], o[db][4 * j + 2], o[db][4 * j + 3]};
-        if (hi == 0) gstore_f2(a.part_ml + (slot * kPromptRows + wave * 32 + lane) * 2, make_float2(m, l));
+            for (int j = 0; j < 4; ++j)
+                *(LYCHEE_GLOBAL f32x4_t *)(po + (4 * db + j) * 256) = f32x4_t{o[db][4 * j], o[db][4 * j + 1], o[db][4 * j + 2], o[db][4 * j + 3]};
+        if (hi == 0) gstore_f2(a.part_ml + (at * 32 + lane) * 2, make_float2(m, l));
     }
 }
 
-// Rows of split tiles: o = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p, M = max m_p.  A workgroup has 16 rows of a tile, a
-// wavefront four, one after the other, two dimensions a lane.
-constexpr int kMergeRows = 16;
+// Rows of split tiles: o = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p, M = max m_p.  A workgroup has 32 rows of a tile and some of the
+// 16 groups of eight dimensions, its wavefronts a fourth of the pieces each, a lane four dimensions of a row, as the pieces left
+// them; the wavefronts' sums meet in LDS.
+constexpr int kMergeBatch = 8;  // pieces whose loads are in flight together
 __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptArgs a)
 {
     __shared__ SharedPlan sh;
+    __shared__ __align__(16) f32x4_t sum[kWaves][64];
+    __shared__ float2 ml[kWaves][64];
     const PromptRows &p = a.r;
-    constexpr int kParts = kPromptRows / kMergeRows;
-    const int g = blockIdx.x / kParts % p.n_kv_heads, tile = blockIdx.x / kParts / p.n_kv_heads, sub = blockIdx.x % kParts;
-    const Tile w = find_tile<true>(p, tile, a.slots, sh);
-    if (!w.found || w.parts == 1) return;
+    const int sub = blockIdx.x % a.merge_split, unit = blockIdx.x / a.merge_split, rows32 = unit % kWaves, g = unit / kWaves % p.n_kv_heads;
+    const Tile w = find_tile<true>(p, unit / kWaves / p.n_kv_heads, a.slots, sh);
+    if (!w.found || w.parts == 1 || w.slot + w.parts > a.n_slots) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rows = w.n * p.group;
-    for (int i = 0; i < kMergeRows / kWaves; ++i) {
-        const int at = sub * kMergeRows + wave * (kMergeRows / kWaves) + i, row = w.tile * kPromptRows + at;
-        if (row >= rows) break;
-        const int token = token_of(p, row), head = g * p.group + row - token * p.group;
-        const auto slot = [&](int piece) { return ((int64_t)(w.item + piece) * p.n_kv_heads + g) * kPromptRows + at; };
-        float m = -__builtin_inff();
-        for (int q = lane; q < w.parts; q += 64) m = fmaxf(m, gload(a.part_ml + slot(q) * 2));
-        m = wave_max_f(m);
-        const float ref = m == -__builtin_inff() ? 0.f : m;
-        float l = 0.f, x = 0.f, y = 0.f;
-        for (int q = 0; q < w.parts; ++q) {
-            const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + slot(q) * 2);
-            const float f = fast_exp2(ml.x - ref);
-            const float2 o = *reinterpret_cast<const float2 *>(a.part_o + slot(q) * kHeadDim + 2 * lane);
-            l += f * ml.y;
-            x += f * o.x;
-            y += f * o.y;
+    const int row = w.tile * kPromptRows + rows32 * 32 + (lane & 31), token = token_of(p, min(row, rows - 1)), head = g * p.group + min(row, rows - 1) - token * p.group;
+    const int64_t to = (int64_t)(w.start + token) * (p.n_kv_heads * p.group) + head;
+    const auto at = [&](int piece) { return ((int64_t)(w.slot + piece) * p.n_kv_heads + g) * kWaves + rows32; };
+    for (int dj = sub; dj < 16; dj += a.merge_split) {
+        float m = -__builtin_inff(), l = 0.f;
+        f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+        for (int first = wave; first < w.parts; first += kWaves * kMergeBatch) {
+            f32x2_t mls[kMergeBatch];
+            f32x4_t os[kMergeBatch];
+#pragma unroll
+            for (int i = 0; i < kMergeBatch; ++i) {
+                const int64_t from = at(min(first + kWaves * i, w.parts - 1));
+                mls[i] = *(const LYCHEE_GLOBAL f32x2_t *)(a.part_ml + (from * 32 + (lane & 31)) * 2);
+                os[i] = *(const LYCHEE_GLOBAL f32x4_t *)(a.part_o + from * (64 * 64) + dj * 256 + 4 * lane);
+            }
+            float up = m;
+#pragma unroll
+            for (int i = 0; i < kMergeBatch; ++i) {
+                if (first + kWaves * i >= w.parts) mls[i][0] = -__builtin_inff();
+                up = fmaxf(up, mls[i][0]);
+            }
+            const float ref = up == -__builtin_inff() ? 0.f : up, f = fast_exp2(m - ref);
+            m = up;
+            l *= f;
+            o *= f;
+#pragma unroll
+            for (int i = 0; i < kMergeBatch; ++i) {
+                const bool there = first + kWaves * i < w.parts;
+                const float e = fast_exp2(mls[i][0] - ref);
+                l += there ? e * mls[i][1] : 0.f;
+#pragma unroll
+                for (int d = 0; d < 4; ++d) o[d] += there ? e * os[i][d] : 0.f;
+            }
         }
-        const float f = l == 0.f ? 0.f : 1.f / l;
-        const int64_t to = (int64_t)(w.start + token) * (p.n_kv_heads * p.group) + head;
-        gstore(reinterpret_cast<uint32_t *>(a.out + to * kHeadDim) + lane, pk_bf16(x * f, y * f));
-        if (a.lse && lane == 0)
-            gstore(a.lse + (int64_t)head * p.n_tokens + w.start + token, l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * (1.f / kLog2e));
+        sum[wave][lane] = o;
+        ml[wave][lane] = make_float2(m, l);
+        __syncthreads();
+        if (wave == 0) {
+            float top = -__builtin_inff();
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) top = fmaxf(top, ml[i][lane].x);
+            const float ref = top == -__builtin_inff() ? 0.f : top;
+            l = 0.f;
+            o = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) {
+                const float e = fast_exp2(ml[i][lane].x - ref);
+                l += e * ml[i][lane].y;
+                o += e * sum[i][lane];
+            }
+            o *= l == 0.f ? 0.f : 1.f / l;
+            if (row < rows) {
+                // (dimensions of register group dj: 32 db + 8 j + 4 hi)
+                *(LYCHEE_GLOBAL u32x2_t *)(a.out + to * kHeadDim + 8 * dj + 4 * (lane >> 5)) = u32x2_t{pk_bf16(o[0], o[1]), pk_bf16(o[2], o[3])};
+                if (a.lse && dj == 0 && lane < 32)
+                    gstore(a.lse + (int64_t)head * p.n_tokens + w.start + token, l == 0.f ? -__builtin_inff() : (top + __log2f(l)) * (1.f / kLog2e));
+            }
+        }
+        __syncthreads();
     }
 }
 
@@ -265,7 +305,7 @@ hipError_t launch_prompt(const PromptArgs &a, hipStream_t stream)
         prompt_kernel<true><<<grid, kThreads, 0, stream>>>(a);
     else
         prompt_kernel<false><<<grid, kThreads, 0, stream>>>(a);
-    if (a.slots > 0) prompt_merge_kernel<<<(unsigned)a.n_tiles * (unsigned)a.r.n_kv_heads * (kPromptRows / kMergeRows), kThreads, 0, stream>>>(a);
+    if (a.slots > 0) prompt_merge_kernel<<<(unsigned)a.n_tiles * (unsigned)a.r.n_kv_heads * kWaves * (unsigned)a.merge_split, kThreads, 0, stream>>>(a);
     return hipGetLastError();
 }
 

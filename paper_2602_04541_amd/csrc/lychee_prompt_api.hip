@@ -11,6 +11,10 @@ using namespace lychee;
 namespace {
 
 constexpr int32_t kPromptSlots = 512;  // pieces that fill a device: two workgroups a compute unit
+#ifndef KEYSLOTS
+#define KEYSLOTS 1024
+#endif
+constexpr int32_t kPromptKeySlots = KEYSLOTS;
 constexpr int64_t kMaxGrid = 1 << 24;  // workgroups of 256 threads, which are counted in 32 bits
 
 int check_heads_of(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim)
@@ -38,16 +42,36 @@ Grid grid_of(int32_t batch, int32_t n_kv_heads, int32_t group, int32_t n_tokens,
     return w;
 }
 
-struct CarvedPrompt {
-    size_t part_ml, stat, total;
+// Tiles of keys of a KV head in the backward pass, their pieces (one more a tile than the blocks hold of the smallest piece, or the
+// device is filled with), and partials (find_key_tile: twice as many).
+struct KeyGrid {
+    int64_t tiles, items, slots;
 };
-CarvedPrompt carve(const Grid &w, int32_t n_kv_heads, int64_t stats)
+KeyGrid key_grid_of(int32_t batch, int32_t n_kv_heads, int32_t group, int32_t n_tokens)
+{
+    KeyGrid w;
+    const int64_t many = batch < n_tokens ? batch : n_tokens, blocks = (int64_t)n_tokens * group / kPromptKeys + 1;
+    w.tiles = n_tokens / kPromptRows + many;
+    const int64_t most = w.tiles * (blocks / kPromptMinRowPiece + 1), fill = (kPromptKeySlots + n_kv_heads - 1) / n_kv_heads;
+    w.items = w.tiles + (most < fill ? most : fill);
+    w.slots = 2 * (most < fill ? most : fill);
+    return w;
+}
+
+struct CarvedPrompt {
+    size_t part_ml, stat, part, total;
+};
+CarvedPrompt carve(const Grid &w, int32_t n_kv_heads, int64_t stats, int64_t key_slots)
 {
     CarvedPrompt c;
     const int64_t rows = w.slots > 0 ? w.items * n_kv_heads * kPromptRows : 0;
     c.part_ml = (size_t)(rows * kHeadDim * (int64_t)sizeof(float));
-    c.stat = c.part_ml + (size_t)round_up(rows * 2 * (int64_t)sizeof(float), 256);
-    c.total = c.stat + (size_t)round_up(stats * 2 * (int64_t)sizeof(float), 256);
+    c.stat = 0;
+    // (the forward pass's partials and those of the backward pass are not needed at once)
+    c.part = (size_t)round_up(stats * 2 * (int64_t)sizeof(float), 256);
+    c.total = c.part + (size_t)(key_slots * n_kv_heads * 2 * kPromptRows * kHeadDim * (int64_t)sizeof(float));
+    const size_t forward = c.part_ml + (size_t)round_up(rows * 2 * (int64_t)sizeof(float), 256);
+    if (c.total < forward) c.total = forward;
     if (c.total == 0) c.total = 256;
     return c;
 }
@@ -74,7 +98,11 @@ Grid grid_of(const lychee_prompt &p)
 {
     return grid_of(p.batch, p.n_kv_heads, p.n_q_heads / p.n_kv_heads, p.n_tokens, p.max_len > p.n_tokens ? p.max_len : p.n_tokens);
 }
-CarvedPrompt carve(const lychee_prompt &p) { return carve(grid_of(p), p.n_kv_heads, (int64_t)p.n_tokens * p.n_q_heads); }
+CarvedPrompt carve(const lychee_prompt &p)
+{
+    return carve(grid_of(p), p.n_kv_heads, (int64_t)p.n_tokens * p.n_q_heads,
+                 key_grid_of(p.batch, p.n_kv_heads, p.n_q_heads / p.n_kv_heads, p.n_tokens).slots);
+}
 
 PromptRows rows_of(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_tokens, int32_t max_len, int64_t q_tok, int64_t q_head,
                    const int32_t *start, const int32_t *lengths)
@@ -107,8 +135,12 @@ void fill_split(PromptArgs &a, const Grid &w, const CarvedPrompt &c, void *works
     a.part_o = static_cast<float *>(workspace);
     a.part_ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + c.part_ml);
     a.slots = w.slots;
+    // (about 1024 workgroups: two that fit a compute unit at a time)
+    a.merge_split = 1;
+    while (a.merge_split < 16 && w.tiles * a.r.n_kv_heads * kWaves * a.merge_split < 512) a.merge_split *= 2;
     a.n_items = (int32_t)w.items;
     a.n_tiles = (int32_t)w.tiles;
+    a.n_slots = w.slots > 0 ? a.n_items : 0;
     a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)kHeadDim));
 }
 
@@ -190,7 +222,12 @@ int lychee_prompt_attn_backward(lychee_ctx *ctx, const lychee_prompt *prompt, co
     a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)kHeadDim));
     a.root = (float)sqrt((double)kHeadDim);
     a.n_row_tiles = (int32_t)grid_of(p.batch, p.n_kv_heads, a.r.group, p.n_tokens, 0).tiles;
-    a.n_key_tiles = (int32_t)grid_of(p.batch, p.n_kv_heads, 1, p.n_tokens, 0).tiles;
+    const KeyGrid w = key_grid_of(p.batch, p.n_kv_heads, a.r.group, p.n_tokens);
+    a.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + c.part);
+    a.slots = kPromptKeySlots;
+    a.n_key_tiles = (int32_t)w.tiles;
+    a.n_key_items = (int32_t)w.items;
+    a.n_slots = (int32_t)w.slots;
     return done(launch_prompt_grad(a, static_cast<hipStream_t>(hip_stream)));
 }
 
@@ -199,7 +236,7 @@ size_t lychee_q4_prompt_workspace_bytes(const lychee_paged *paged, int32_t n_tok
     if (lychee_check_paged(paged, nullptr, 1) != LYCHEE_OK || n_tokens < 0) return 0;
     const int32_t G = paged->n_q_heads / paged->n_kv_heads;
     if (G > kPromptMaxGroup || (int64_t)n_tokens * G >= kPromptMaxRows) return 0;
-    return carve(grid_of(paged->batch, paged->n_kv_heads, G, n_tokens, (int64_t)paged->max_pages * paged->page_size), paged->n_kv_heads, 0).total;
+    return carve(grid_of(paged->batch, paged->n_kv_heads, G, n_tokens, (int64_t)paged->max_pages * paged->page_size), paged->n_kv_heads, 0, 0).total;
 }
 
 int lychee_q4_prompt_attn(lychee_ctx *ctx, const lychee_paged *paged, const void *q, int64_t q_stride_tok, int64_t q_stride_head,
@@ -220,7 +257,7 @@ int lychee_q4_prompt_attn(lychee_ctx *ctx, const lychee_paged *paged, const void
     if (!cache || !block_table || !lengths || !token_start || !aligned(cache, 128) || !aligned(block_table, 4) || !aligned(lengths, 4) ||
         !aligned(token_start, 4))
         return LYCHEE_EINVAL;
-    const CarvedPrompt c = carve(w, p.n_kv_heads, 0);
+    const CarvedPrompt c = carve(w, p.n_kv_heads, 0, 0);
     if ((rc = check_workspace(workspace, workspace_bytes, c)) != LYCHEE_OK) return rc;
     if (n_tokens == 0) return LYCHEE_OK;
     if (!q || !out || !aligned(q, 16) || !aligned(out, 16)) return LYCHEE_EINVAL;

@@ -18,6 +18,7 @@ namespace {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 #define LYCHEE_LDS __attribute__((address_space(3)))
 
@@ -73,13 +74,13 @@ struct Tile {
     int start;             // its first token among the packed rows
     int piece, parts;      // this piece and how many the tile has that hold keys (at least 1)
     int first, last;       // blocks of keys of the piece
-    int item;              // the piece's number in its KV head (in a merge: that of the tile's first piece)
+    int slot;              // of the piece's partial in its KV head (in a merge: of the tile's first piece)
     bool found;
 };
 
 struct SharedPlan {
-    int32_t n[kMaxBatch], len[kMaxBatch], start[kMaxBatch];
-    int32_t tiles[kMaxBatch], items[kMaxBatch];  // by rank
+    int32_t n[kMaxBatch], len[kMaxBatch], start[kMaxBatch], weight[kMaxBatch];
+    int32_t items[kMaxBatch], slots[kMaxBatch];  // by rank
     uint8_t who[kMaxBatch];                      // the request of a rank
     uint32_t wave[2][kWaves];
     unsigned long long work[kWaves];
@@ -97,66 +98,80 @@ __device__ __forceinline__ void request_of(const PromptRows &p, int b, int &star
 __device__ __forceinline__ int blocks_of(int keys) { return (int)(((int64_t)keys + kPromptKeys - 1) / kPromptKeys); }
 __device__ __forceinline__ int tiles_of(int rows) { return (rows + kPromptRows - 1) / kPromptRows; }
 
-// The piece with this number (MERGE: the tile).  Requests come in the order of their keys, the longest first, and of a
-// request the last tile first, so that what takes longest begins first.  `slots` > 0: tiles are split into pieces of so many
-// blocks that there are about `slots` of them in all KV heads.
+// Sum over the workgroup's threads, for all of them.
+__device__ __forceinline__ unsigned long long sum_all(unsigned long long w, SharedPlan &sh)
+{
+    for (int d = 32; d > 0; d >>= 1) w += __shfl_xor(w, d);
+    if ((threadIdx.x & 63) == 0) sh.work[threadIdx.x >> 6] = w;
+    __syncthreads();
+    w = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) w += sh.work[i];
+    return w;
+}
+
+// Which request has the `number`th of all the requests' `items`, where thread b knows request b's numbers of items and of `slots`
+// for partials.  Requests come in descending order of `weight`, so that what takes longest begins first.  The answer
+// is sh.found: the request or -1, the number within it, the slots of the requests before it.
+__device__ __forceinline__ void find_request(int batch, int number, int weight, int items, int slots, SharedPlan &sh)
+{
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    sh.weight[t] = weight;
+    if (t == 0) sh.found[0] = -1;
+    __syncthreads();
+    int rank = t;
+    if (batch > 1) {
+        rank = 0;
+        for (int i = 0; i < batch; ++i) {
+            const int other = sh.weight[i];
+            rank += other > weight || (other == weight && i < t);
+        }
+    }
+    if (t < batch) {
+        sh.items[rank] = items;
+        sh.slots[rank] = slots;
+        sh.who[rank] = (uint8_t)t;
+    }
+    __syncthreads();
+    const uint32_t items_here = t < batch ? (uint32_t)sh.items[t] : 0u, slots_here = t < batch ? (uint32_t)sh.slots[t] : 0u;
+    const uint32_t items_upto = wave_scan(items_here), slots_upto = wave_scan(slots_here);
+    if (lane == 63) {
+        sh.wave[0][wave] = items_upto;
+        sh.wave[1][wave] = slots_upto;
+    }
+    __syncthreads();
+    uint32_t items_before = items_upto - items_here, slots_before = slots_upto - slots_here;
+    for (int i = 0; i < wave; ++i) {
+        items_before += sh.wave[0][i];
+        slots_before += sh.wave[1][i];
+    }
+    if ((uint32_t)number - items_before < items_here) {
+        sh.found[0] = sh.who[t];
+        sh.found[1] = number - (int)items_before;
+        sh.found[2] = (int)slots_before;
+    }
+    __syncthreads();
+}
+
+// The piece with this number (MERGE: the tile); of a request the last tile first, which sees most keys.  `slots` > 0: tiles are
+// split into pieces of so many blocks that there are about `slots` of them in all KV heads.
 template <bool MERGE>
 __device__ __forceinline__ Tile find_tile(const PromptRows &p, int number, int slots, SharedPlan &sh)
 {
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int t = threadIdx.x;
     int start = 0, n = 0, len = 0;
     if (t < p.batch) request_of(p, t, start, n, len);
     const int tiles = tiles_of(n * p.group), blocks = blocks_of(len);
     sh.n[t] = n;
     sh.len[t] = len;
     sh.start[t] = start;
-    if (t == 0) sh.found[0] = -1;
     int size = 1 << 30;
     if (slots > 0) {
-        unsigned long long w = (unsigned long long)tiles * (unsigned)max(blocks, 1) * (unsigned)p.n_kv_heads;
-        for (int d = 32; d > 0; d >>= 1) w += __shfl_xor(w, d);
-        if (lane == 0) sh.work[wave] = w;
-    }
-    __syncthreads();
-    if (slots > 0) {
-        unsigned long long w = 0;
-#pragma unroll
-        for (int i = 0; i < kWaves; ++i) w += sh.work[i];
+        const unsigned long long w = sum_all((unsigned long long)tiles * (unsigned)max(blocks, 1) * (unsigned)p.n_kv_heads, sh);
         size = max((int)min((w + slots - 1) / slots, 1ull << 30), kPromptMinPiece);
     }
-    int rank = t;
-    if (p.batch > 1) {
-        rank = 0;
-        for (int i = 0; i < p.batch; ++i) {
-            const int other = sh.len[i];
-            rank += other > len || (other == len && i < t);
-        }
-    }
-    if (t < p.batch) {
-        sh.tiles[rank] = tiles;
-        sh.items[rank] = tiles * max(1, (blocks + size - 1) / size);
-        sh.who[rank] = (uint8_t)t;
-    }
-    __syncthreads();
-    const uint32_t tiles_here = t < p.batch ? (uint32_t)sh.tiles[t] : 0u, items_here = t < p.batch ? (uint32_t)sh.items[t] : 0u;
-    const uint32_t items_upto = wave_scan(items_here), tiles_upto = MERGE ? wave_scan(tiles_here) : 0u;
-    if (lane == 63) {
-        sh.wave[0][wave] = items_upto;
-        sh.wave[1][wave] = tiles_upto;
-    }
-    __syncthreads();
-    uint32_t items_before = items_upto - items_here, tiles_before = tiles_upto - tiles_here;
-    for (int i = 0; i < wave; ++i) {
-        items_before += sh.wave[0][i];
-        tiles_before += sh.wave[1][i];
-    }
-    const uint32_t from = MERGE ? tiles_before : items_before, here = MERGE ? tiles_here : items_here;
-    if ((uint32_t)number - from < here) {
-        sh.found[0] = sh.who[t];
-        sh.found[1] = number - (int)from;
-        sh.found[2] = (int)items_before;
-    }
-    __syncthreads();
+    const int items = tiles * max(1, (blocks + size - 1) / size);
+    find_request(p.batch, number, len, MERGE ? tiles : items, items, sh);
     Tile w;
     w.b = __builtin_amdgcn_readfirstlane(sh.found[0]);
     w.found = w.b >= 0;
@@ -168,11 +183,57 @@ __device__ __forceinline__ Tile find_tile(const PromptRows &p, int number, int s
     const int rows = w.n * p.group, of_tiles = tiles_of(rows), pieces = max(1, (blocks_of(w.len) + size - 1) / size);
     w.tile = of_tiles - 1 - (MERGE ? at : at / pieces);
     w.piece = MERGE ? 0 : at % pieces;
-    w.item = before + (MERGE ? at * pieces : at);
+    w.slot = before + (MERGE ? at * pieces : at);
     const int seen = max(0, w.len - w.n + token_of(p, min((w.tile + 1) * kPromptRows, rows) - 1) + 1);  // keys of the last row
     w.parts = max(1, (blocks_of(seen) + size - 1) / size);
     w.first = pieces == 1 ? 0 : w.piece * size;
     w.last = min(blocks_of(seen), pieces == 1 ? 1 << 30 : w.first + size);
+    return w;
+}
+
+// The same for tiles of kPromptRows keys, which the rows from the tile's first key on see: blocks first .. last-1 of
+// kPromptKeys rows.  Tile k of a request with `end` blocks has end - 2 G k of them, and its pieces are numbered from
+// (what the tiles before it have) / size + k on, which leaves room for the last one of each.
+__device__ __forceinline__ int64_t blocks_before(int64_t tile, int end, int group) { return tile * end - (int64_t)group * tile * (tile - 1); }
+
+template <bool MERGE>
+__device__ __forceinline__ Tile find_key_tile(const PromptRows &p, int number, int slots, SharedPlan &sh)
+{
+    static_assert(kPromptRows == 2 * kPromptKeys, "");
+    const int t = threadIdx.x;
+    int start = 0, n = 0, len = 0;
+    if (t < p.batch) request_of(p, t, start, n, len);
+    const int tiles = tiles_of(n);
+    const int64_t work = blocks_before(tiles, blocks_of(n * p.group), p.group);
+    sh.n[t] = n;
+    sh.start[t] = start;
+    const unsigned long long all = sum_all((unsigned long long)work * (unsigned)p.n_kv_heads, sh);
+    const int size = max((int)min((all + slots - 1) / slots, 1ull << 30), kPromptMinRowPiece);
+    // (tiles of several pieces are the first ones, fewer than work / size)
+    find_request(p.batch, number, n, MERGE ? tiles : (int)(work / size) + tiles, 2 * (int)(work / size), sh);
+    Tile w;
+    w.b = __builtin_amdgcn_readfirstlane(sh.found[0]);
+    w.found = w.b >= 0;
+    if (!w.found) return w;
+    const int at = __builtin_amdgcn_readfirstlane(sh.found[1]), before = __builtin_amdgcn_readfirstlane(sh.found[2]);
+    w.n = __builtin_amdgcn_readfirstlane(sh.n[w.b]);
+    w.len = w.n;
+    w.start = __builtin_amdgcn_readfirstlane(sh.start[w.b]);
+    const int end = blocks_of(w.n * p.group);
+    int tile = at;
+    if (!MERGE) {  // the last tile that begins at or before the piece
+        tile = 0;
+        for (int step = 1 << 17; step > 0; step >>= 1)
+            if (tile + step < tiles_of(w.n) && blocks_before(tile + step, end, p.group) / size + tile + step <= at) tile += step;
+    }
+    const int from = (int)(blocks_before(tile, end, p.group) / size) + tile;
+    w.tile = tile;
+    w.piece = MERGE ? 0 : at - from;
+    w.slot = before + from + w.piece;
+    const int first = 2 * p.group * tile;
+    w.parts = max(1, (end - first + size - 1) / size);
+    w.first = first + w.piece * size;
+    w.last = min(end, w.first + size);
     return w;
 }
 

@@ -12,6 +12,7 @@
 namespace lychee {
 namespace {
 
+constexpr int kPartFloats = 2 * 16 * 64 * 4;  // a wavefront's part of a piece's sums
 constexpr int kHeld = 5;  // of the second launch's eight steps of V those that stay in registers
 
 struct SharedGrad {
@@ -153,12 +154,10 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dkv_kernel(PromptGradArgs 
     __shared__ SharedGrad sh;
     const PromptRows &p = a.r;
     const int g = blockIdx.x % p.n_kv_heads;
-    PromptRows keys = p;
-    keys.group = 1;  // (tiles of keys)
-    const Tile w = find_tile<false>(keys, blockIdx.x / p.n_kv_heads, 0, sh.plan);
-    if (!w.found) return;
+    const Tile w = find_key_tile<false>(p, blockIdx.x / p.n_kv_heads, a.slots, sh.plan);
+    if (!w.found || w.piece >= w.parts || (w.parts > 1 && w.slot >= a.n_slots)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hi = lane >> 5;
-    const int tile = tiles_of(w.n) - 1 - w.tile, rows = w.n * p.group;  // (the first keys are seen by most rows)
+    const int tile = w.tile, rows = w.n * p.group;
     const int key = tile * kPromptRows + wave * 32 + (lane & 31), key_in = min(key, w.n - 1);
     const int64_t kv_at = (int64_t)(w.start + key_in) * a.kv_tok + (int64_t)g * a.kv_head;
     __syncthreads();  // (the plan's part of LDS is free)
@@ -199,7 +198,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dkv_kernel(PromptGradArgs 
         wait_copies();
         __syncthreads();
     };
-    const int first = tile * kPromptRows * p.group / kPromptKeys, last = (rows + kPromptKeys - 1) / kPromptKeys;
+    const int first = w.first, last = w.last;
     const int wave_first = (tile * kPromptRows + wave * 32) * p.group;            // rows from here on see a key of the wavefront
     const int wave_all = (tile * kPromptRows + wave * 32 + 31) * p.group;         // and from here on all of them
 
@@ -275,9 +274,49 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dkv_kernel(PromptGradArgs 
         if (careful || !__syncthreads_or(!all_finite(dk) || !all_finite(dv))) break;
         careful = true;
     }
-    const bool there = key < w.n;
-    store_row(there ? a.dk + kv_at : nullptr, lane, dk, a.scale);
-    store_row(there ? a.dv + kv_at : nullptr, lane, dv, 1.f);
+    if (w.parts == 1) {
+        const bool there = key < w.n;
+        store_row(there ? a.dk + kv_at : nullptr, lane, dk, a.scale);
+        store_row(there ? a.dv + kv_at : nullptr, lane, dv, 1.f);
+    } else {
+        float *to = a.part + (((int64_t)w.slot * p.n_kv_heads + g) * kWaves + wave) * kPartFloats + 4 * lane;
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                *(LYCHEE_GLOBAL f32x4_t *)(to + (4 * db + j) * 256) = f32x4_t{dk[db][4 * j], dk[db][4 * j + 1], dk[db][4 * j + 2], dk[db][4 * j + 3]};
+                *(LYCHEE_GLOBAL f32x4_t *)(to + (16 + 4 * db + j) * 256) = f32x4_t{dv[db][4 * j], dv[db][4 * j + 1], dv[db][4 * j + 2], dv[db][4 * j + 3]};
+            }
+    }
+}
+
+// The sums of tiles with several pieces, piece after piece: a workgroup has 32 keys, a wavefront every fourth group of four
+// dimensions, a lane four of a key.
+__global__ __launch_bounds__(kThreads) void prompt_dkv_merge_kernel(PromptGradArgs a)
+{
+    __shared__ SharedPlan sh;
+    const PromptRows &p = a.r;
+    const int keys32 = blockIdx.x % kWaves, g = blockIdx.x / kWaves % p.n_kv_heads;
+    const Tile w = find_key_tile<true>(p, blockIdx.x / kWaves / p.n_kv_heads, a.slots, sh);
+    if (!w.found || w.parts == 1 || w.slot + w.parts > a.n_slots) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, key = w.tile * kPromptRows + keys32 * 32 + (lane & 31);
+    const float *from = a.part + (((int64_t)w.slot * p.n_kv_heads + g) * kWaves + keys32) * kPartFloats + 4 * lane;
+    const int64_t apart = (int64_t)p.n_kv_heads * kWaves * kPartFloats;
+    f32x4_t sum[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = *(const LYCHEE_GLOBAL f32x4_t *)(from + (4 * i + wave) * 256);
+    for (int q = 1; q < w.parts; ++q) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += *(const LYCHEE_GLOBAL f32x4_t *)(from + q * apart + (4 * i + wave) * 256);
+    }
+    if (key >= w.n) return;
+    const int64_t to = (int64_t)(w.start + key) * a.kv_tok + (int64_t)g * a.kv_head + 4 * (lane >> 5);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int dj = (4 * i + wave) % 16;
+        const float f = i < 4 ? a.scale : 1.f;
+        *(LYCHEE_GLOBAL u32x2_t *)((i < 4 ? a.dk : a.dv) + to + 8 * dj) = u32x2_t{pk_bf16(sum[i][0] * f, sum[i][1] * f), pk_bf16(sum[i][2] * f, sum[i][3] * f)};
+    }
 }
 
 }  // namespace
@@ -288,7 +327,8 @@ hipError_t launch_prompt_grad(const PromptGradArgs &a, hipStream_t stream)
     prompt_dq_kernel<<<(unsigned)a.n_row_tiles * heads, kThreads, 0, stream>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    prompt_dkv_kernel<<<(unsigned)a.n_key_tiles * heads, kThreads, 0, stream>>>(a);
+    prompt_dkv_kernel<<<(unsigned)a.n_key_items * heads, kThreads, 0, stream>>>(a);
+    prompt_dkv_merge_kernel<<<(unsigned)a.n_key_tiles * heads * kWaves, kThreads, 0, stream>>>(a);
     return hipGetLastError();
 }
 

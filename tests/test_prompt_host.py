@@ -60,9 +60,9 @@ def test_workspace(lb):
     for p in (shape(lb), many, long):
         n = lb.prompt_workspace_bytes(p)
         assert n >= stats(p) and n % 256 == 0
-    assert lb.prompt_workspace_bytes(many) < stats(many) + 4096       # many tiles: none is split
+    for p in (many, long):                                             # (partials: as many as fill the device, however many tokens)
+        assert lb.prompt_workspace_bytes(p) < stats(p) + (320 << 20)
     assert lb.prompt_workspace_bytes(long) > 1 << 20                   # few tiles over many keys
-    assert lb.prompt_workspace_bytes(long) < 256 << 20
     assert lb.q4_prompt_workspace_bytes(paged(lb), 9) > 0
     assert lb.q4_prompt_workspace_bytes(paged(lb), 0) > 0
     assert lb.q4_prompt_workspace_bytes(paged(lb), -1) == 0
