@@ -15,6 +15,9 @@
 namespace lychee {
 namespace {
 
+constexpr int kAhead = 2;        // of the four steps of the second product those whose values are read before the softmax
+constexpr float kSlack = 8.f;    // powers of two by which a score may exceed the maximum that weights are measured against
+
 struct SharedPrompt {
     __align__(16) uint8_t k[2][kBlockBytes];
     __align__(16) uint8_t v[2][kBlockBytes];
@@ -53,98 +56,119 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
     const uint32_t fetch_chunk = (uint32_t)((lane & 15) ^ swizzle(fetch_row)) << 4;  // (the same for rows 16 apart)
     const uint32_t fetch_at = (uint32_t)fetch_row * (uint32_t)(2 * a.kv_tok) + fetch_chunk;
     // 4 bits: a thread takes a quarter (one scale's dimensions) of a token's key and of its value, and writes their bf16 numbers.
-    const int token4 = threadIdx.x >> 2, part4 = threadIdx.x & 3;
+    // (16 lanes the same quarter of 16 tokens, whose rows lie in 16 places)
+    const int token4 = wave * 16 + (lane & 15), part4 = lane >> 4;
     uint4 code_k = make_uint4(0, 0, 0, 0), code_v = code_k;
-    uint32_t scale_kv = 0;  // bytes: key, value
-    int entry = -1;         // of the block table, for the block after the one that is loaded
+    uint32_t scale_k = 0, scale_v = 0;
+    int entry = -1;  // of the block table, for the block that is loaded next
     const auto fetch_entry = [&](int blk) {
         const int t = min(blk * kPromptKeys + token4, w.len - 1);
-        entry = gload(a.table + (int64_t)w.b * a.d.table_stride + (t >> a.d.page_shift));
+        return gload(a.table + (int64_t)w.b * a.d.table_stride + (t >> a.d.page_shift));
     };
-    const auto fetch = [&](int blk, int buf) {
-        const int j0 = blk * kPromptKeys;
-        if constexpr (Q4) {
-            const int t = j0 + token4, off = t & ((1 << a.d.page_shift) - 1);
-            const bool ok = t < w.len && (uint32_t)entry < (uint32_t)a.d.n_pages;
-            const uint8_t *tile = a.cache + ((int64_t)(ok ? entry : 0) * a.d.page_tiles + (int64_t)g * ((1 << a.d.page_shift) / kTileTokens) +
-                                             off / kTileTokens) * kTileBytes;
-            const int sub = off & (kTileTokens - 1);
-            const u32x4_t k4 = *(const LYCHEE_GLOBAL u32x4_t *)(tile + sub * kTokenBytes + 16 * part4);
-            const u32x4_t v4 = *(const LYCHEE_GLOBAL u32x4_t *)(tile + sub * kTokenBytes + 64 + 16 * part4);
-            code_k = make_uint4(k4[0], k4[1], k4[2], k4[3]);
-            code_v = make_uint4(v4[0], v4[1], v4[2], v4[3]);
-            const uint32_t ks = gload(tile + kTileScales + part4 * kTileTokens + sub), vs = gload(tile + kTileScales + (4 + part4) * kTileTokens + sub);
-            scale_kv = ok ? ks | vs << 8 : 0u;  // (a scale of 0 makes numbers that are no NaN: a weight of 0 times NaN is NaN)
-            const uint64_t there = __ballot(ok);
-            if (lane == 0) {
-                uint32_t bad = 0;  // (four lanes a token)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) bad |= (uint32_t)(~there >> (4 * i) & 1) << i;
-                sh.bad[buf][wave] = (uint16_t)bad;
-            }
-        } else {
-            const bool whole = j0 + kPromptKeys <= w.len;  // (else the last key again in the rows behind it)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int64_t from = (int64_t)(whole ? j0 + 16 * i : j0) * a.kv_tok;
-                const uint32_t off = whole ? fetch_at : (uint32_t)min(fetch_row + 16 * i, w.len - 1 - j0) * (uint32_t)(2 * a.kv_tok) + fetch_chunk;
-                copy16(kb + from, off, to_k + buf * kBlockBytes + i * 16 * kRowBytes);
-                copy16(vb + from, off, to_v + buf * kBlockBytes + i * 16 * kRowBytes);
-            }
-        }
+    const auto load4 = [&](int blk) {
+        const int t = blk * kPromptKeys + token4, off = t & ((1 << a.d.page_shift) - 1), sub = off & (kTileTokens - 1);
+        const bool ok = t < w.len && (uint32_t)entry < (uint32_t)a.d.n_pages;
+        const uint8_t *tile = a.cache + ((int64_t)(ok ? entry : 0) * a.d.page_tiles + (int64_t)g * ((1 << a.d.page_shift) / kTileTokens) +
+                                         off / kTileTokens) * kTileBytes;
+        const u32x4_t k = *(const LYCHEE_GLOBAL u32x4_t *)(tile + sub * kTokenBytes + 16 * part4);
+        const u32x4_t v = *(const LYCHEE_GLOBAL u32x4_t *)(tile + sub * kTokenBytes + 64 + 16 * part4);
+        const uint32_t ks = gload(tile + kTileScales + part4 * kTileTokens + sub), vs = gload(tile + kTileScales + (4 + part4) * kTileTokens + sub);
+        code_k = make_uint4(k[0], k[1], k[2], k[3]);
+        code_v = make_uint4(v[0], v[1], v[2], v[3]);
+        scale_k = ok ? ks << 23 : 0u;  // (a scale of 0 makes numbers that are no NaN: a weight of 0 times NaN is NaN)
+        scale_v = ok ? vs << 23 : 0u;
+        return __ballot(ok);
     };
-    const auto arrive = [&](int buf) {
-        if constexpr (Q4) {
-            const float ks = __builtin_bit_cast(float, scale_kv << 23), vs = __builtin_bit_cast(float, scale_kv << 15);
-            const uint32_t kc[4] = {code_k.x, code_k.y, code_k.z, code_k.w}, vc[4] = {code_v.x, code_v.y, code_v.z, code_v.w};
+    const auto store4 = [&](uint8_t *block, uint4 code, uint32_t scale) {
+        const float f = __builtin_bit_cast(float, scale);
+        const uint32_t c4[4] = {code.x, code.y, code.z, code.w};
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const int to = token4 * kRowBytes + (((4 * part4 + c) ^ swizzle(token4)) << 4);
-                *reinterpret_cast<uint4 *>(sh.k[buf] + to) = decode8(kc[c], ks);
-                *reinterpret_cast<uint4 *>(sh.v[buf] + to) = decode8(vc[c], vs);
-            }
-        } else {
-            wait_copies();
+        for (int c = 0; c < 4; ++c)
+            *reinterpret_cast<uint4 *>(block + token4 * kRowBytes + (((4 * part4 + c) ^ swizzle(token4)) << 4)) = decode8(c4[c], f);
+    };
+    uint32_t offset[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) offset[i] = fetch_at + (uint32_t)i * 32u * (uint32_t)a.kv_tok;
+    const auto copy_rows = [&](const uint16_t *from, int blk, uint32_t to) {
+        const uint16_t *at = from + (int64_t)(blk * kPromptKeys) * a.kv_tok;
+        const int left = w.len - 1 - blk * kPromptKeys;
+        if (left >= kPromptKeys - 1) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) copy16(at, offset[i], to + i * 16 * kRowBytes);
+        } else {  // the last key again in the rows behind it
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                copy16(at, (uint32_t)min(fetch_row + 16 * i, left) * (uint32_t)(2 * a.kv_tok) + fetch_chunk, to + i * 16 * kRowBytes);
         }
-        __syncthreads();
     };
 
     f32x16_t o[4];
     float m, l;
     bool careful = false;
     for (;;) {
-        const int each = careful ? 3 : 1, turns = each * max(w.last - w.first, 0);  // (take_with_care)
+        // Turns: a block each (with care three of them, take_with_care).
+        const int turns = (careful ? 3 : 1) * max(w.last - w.first, 0);
         const auto block_of = [&](int turn) { return w.first + (careful ? turn / 3 : turn); };
+        const auto fetch = [&](int turn) {
+            const int blk = block_of(turn);
+            if constexpr (Q4) {
+                const uint64_t there = load4(blk);
+                if (lane == 0) sh.bad[turn & 1][wave] = (uint16_t)~there;
+                entry = fetch_entry(block_of(min(turn + 1, turns - 1)));
+            } else {
+                copy_rows(kb, blk, to_k + (turn & 1) * kBlockBytes);
+                copy_rows(vb, blk, to_v + (turn & 1) * kBlockBytes);
+            }
+        };
+        const auto arrive = [&](int turn) {
+            if constexpr (Q4) {
+                store4(sh.k[turn & 1], code_k, scale_k);
+                store4(sh.v[turn & 1], code_v, scale_v);
+            } else {
+                wait_copies();
+            }
+            __syncthreads();
+        };
 #pragma unroll
         for (int db = 0; db < 4; ++db) o[db] = zero16();
         m = -__builtin_inff();
         l = 0.f;
         if (turns > 0) {
-            if (Q4) fetch_entry(w.first);
-            fetch(w.first, 0);
-            if (Q4) fetch_entry(block_of(min(1, turns - 1)));
+            if (Q4) entry = fetch_entry(w.first);
+            fetch(0);
+            arrive(0);
         }
-        arrive(0);
         for (int turn = 0; turn < turns; ++turn) {
-            const int blk = block_of(turn), buf = turn & 1, j0 = blk * kPromptKeys;
-            if (turn + 1 < turns) {
-                fetch(block_of(turn + 1), buf ^ 1);
-                if (Q4) fetch_entry(block_of(min(turn + 2, turns - 1)));
-            }
-            const LYCHEE_LDS uint8_t *K = (const LYCHEE_LDS uint8_t *)sh.k[buf], *V = (const LYCHEE_LDS uint8_t *)sh.v[buf];
+            const int j0 = block_of(turn) * kPromptKeys;
+            if (turn + 1 < turns) fetch(turn + 1);
             if (careful || j0 <= highest) {
+                const LYCHEE_LDS uint8_t *K = (const LYCHEE_LDS uint8_t *)sh.k[turn & 1], *V = (const LYCHEE_LDS uint8_t *)sh.v[turn & 1];
                 const uint32_t kat = opaque(row_at), vat = opaque(turn_at);
                 f32x16_t z[2] = {zero16(), zero16()};
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks)
 #pragma unroll
                     for (int x = 0; x < 2; ++x) z[x] = mfma(read_rows(K, kat, x, ks), qf[ks], z[x]);
+                // (eight reads ahead of the products that need them)
+                __builtin_amdgcn_sched_group_barrier(kGroupRead, 8, 0);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(kGroupMfma, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(kGroupRead, 1, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(kGroupMfma, 8, 0);
+                bf16x8_t vf[kAhead][4];  // values of the first steps, on their way while the weights are made
+#pragma unroll
+                for (int s = 0; s < kAhead; ++s)
+#pragma unroll
+                    for (int db = 0; db < 4; ++db) vf[s][db] = read_turned(V, vat, db, s);
                 uint64_t bad = 0;  // keys whose page is not there
                 if (Q4) {
-                    const uint2 words = *reinterpret_cast<const uint2 *>(sh.bad[buf]);
+                    const uint2 words = *reinterpret_cast<const uint2 *>(sh.bad[turn & 1]);
                     bad = (uint64_t)__builtin_amdgcn_readfirstlane(words.y) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane(words.x);
                 }
                 if (j0 + kPromptKeys - 1 > lowest || bad != 0) {
+                    asm volatile("");  // (a branch: these are many instructions, and rare)
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
                         const int n = min(max(pos - j0 - 32 * x + 1, 0), 32);
@@ -161,8 +185,11 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) top = fmaxf(top, z[x][i]);
                 top = max_halves32(top) * a.scale_log2e;
-                if (__ballot(top > m) != 0) {
-                    const float up = fmaxf(m, top);
+                // m is some maximum of late: weights of up to 2^kSlack are as exact as others, and a new maximum costs 65 products.  (By
+                // the row's own scores alone, so that no row's bits depend on another's.)
+                if (__ballot(top > m + kSlack) != 0) {
+                    asm volatile("");
+                    const float up = top > m + kSlack ? top : m;
                     const float f = m == up ? 1.0f : fast_exp2(m - up);
                     m = up;
                     l *= f;
@@ -172,31 +199,39 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
                         for (int i = 0; i < 16; ++i) o[db][i] *= f;
                 }
                 const float ref = m == -__builtin_inff() ? 0.f : m, before = l;
+                float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         z[x][i] = fast_exp2(__builtin_fmaf(z[x][i], a.scale_log2e, -ref));
-                        l += z[x][i];
+                        part[i % 4] += z[x][i];
                     }
+                l += (part[0] + part[1]) + (part[2] + part[3]);
                 bf16x8_t pf[4] = {operand<0>(z[0]), operand<8>(z[0]), operand<0>(z[1]), operand<8>(z[1])};
                 if (__builtin_expect(careful, 0)) {
                     __syncthreads();
-                    take_with_care(sh.v[buf], turn % 3);
+                    take_with_care(sh.v[turn & 1], turn % 3);
                     __syncthreads();
                     if (turn % 3 != 0) {
                         l = before;
 #pragma unroll
                         for (int s = 0; s < 4; ++s) pf[s] = seen_rows(hi, s, 0, pos - j0);
                     }
+#pragma unroll
+                    for (int s = 0; s < kAhead; ++s)
+#pragma unroll
+                        for (int db = 0; db < 4; ++db) vf[s][db] = read_turned(V, vat, db, s);
                 }
 #pragma unroll
                 for (int s = 0; s < 4; ++s)
 #pragma unroll
-                    for (int db = 0; db < 4; ++db) o[db] = mfma(read_turned(V, vat, db, s), pf[s], o[db]);
+                    for (int db = 0; db < 4; ++db) o[db] = mfma(s < kAhead ? vf[s][db] : read_turned(V, vat, db, s), pf[s], o[db]);
             }
-            arrive(buf ^ 1);
+            arrive(turn + 1);
         }
+        // A key's value counts for the rows that see it alone, but a weight of zero times an infinite value or NaN is NaN: a
+        // tile in which that may have happened is done again, with care.
         if (careful || !__syncthreads_or(!all_finite(o))) break;
         careful = true;
     }

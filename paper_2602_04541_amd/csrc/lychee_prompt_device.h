@@ -6,9 +6,10 @@
 // 16 rows of one product's D therefore takes its B operand from D as it is, eight neighbouring registers a lane: the lane
 // then has rows 16 s + 4 hi + {0..3} and 16 s + 8 + 4 hi + {0..3}, and the A operand is read in the same order.
 //
-// In LDS a block is 64 rows of 256 bytes, 16 chunks of 16 bytes, chunk c of row r at place c ^ swizzle(r).  Read along
-// the rows (ds_read_b128, lane n its row's chunk) 16 rows are in 16 places; read across them (ds_read_b64_tr_b16, 16 lanes
-// take 4 rows of two neighbouring chunks and turn them) 8 rows are in 16 places: neither meets a bank twice.
+// In LDS a block is 64 rows of 256 bytes, 16 chunks of 16 bytes, chunk c of row r at place c ^ swizzle(r).  LDS serves 256 bytes
+// a cycle: along the rows (ds_read_b128, lane n its row's chunk) 16 rows, which are in 16 places; across them
+// (ds_read_b64_tr_b16, 16 lanes take 4 rows of two neighbouring chunks and turn them) four rows of four chunks, in 16 places
+// too.  Neither meets a bank twice.
 #pragma once
 #include "lychee_device.h"
 #include "lychee_prompt.h"
@@ -22,10 +23,11 @@ typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 #define LYCHEE_LDS __attribute__((address_space(3)))
 
+constexpr int kGroupMfma = 0x8, kGroupRead = 0x100;  // kinds of instructions, for the scheduler: matrix products, reads of LDS
 constexpr int kRowBytes = 2 * kHeadDim;
 constexpr int kBlockBytes = kPromptKeys * kRowBytes;
 
-__device__ __forceinline__ int swizzle(int row) { return ((2 * row) & 15) | ((row >> 3) & 1); }
+__device__ __forceinline__ int swizzle(int row) { return (row & 3) << 2 | ((row >> 2) & 3); }
 
 __device__ __forceinline__ f32x16_t mfma(bf16x8_t a, bf16x8_t b, f32x16_t c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 
@@ -241,13 +243,19 @@ __device__ __forceinline__ Tile find_key_tile(const PromptRows &p, int number, i
 // Sixteen bytes a lane from global memory to LDS, lane after lane from `to` on (base and to: the same for the wavefront).  In
 // assembly, because the compiler lets every later read of LDS wait for such a copy at once, whichever part of LDS it writes; the
 // kernels wait themselves, before the barrier behind which the copied block is read.
+template <typename T>
+__device__ __forceinline__ const T *uniform(const T *p)  // (in scalar registers, whatever the compiler knows of it)
+{
+    const uint64_t u = reinterpret_cast<uint64_t>(p);
+    return reinterpret_cast<const T *>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)u));
+}
 __device__ __forceinline__ void copy16(const uint16_t *base, uint32_t offset, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane((int)to)), "v"(offset), "s"(uniform(base)) : "memory");
 }
 __device__ __forceinline__ void copy4(const float *base, uint32_t offset, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(__builtin_amdgcn_readfirstlane((int)to)), "v"(offset), "s"(uniform(base)) : "memory");
 }
 __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(const LYCHEE_LDS uint8_t *)p; }
@@ -275,7 +283,7 @@ __device__ __forceinline__ bf16x8_t read_turned(const LYCHEE_LDS uint8_t *block,
 {
     const LYCHEE_LDS uint8_t *p = block + s * 16 * kRowBytes;
     const s16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LYCHEE_LDS s16x4_t *)(p + (place ^ (uint32_t)(db << 6))));
-    const s16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LYCHEE_LDS s16x4_t *)(p + 8 * kRowBytes + (place ^ (uint32_t)(db << 6 | 16))));
+    const s16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LYCHEE_LDS s16x4_t *)(p + 8 * kRowBytes + (place ^ (uint32_t)(db << 6 | 32))));
     typedef short s16x8_t __attribute__((ext_vector_type(8)));
     return __builtin_bit_cast(bf16x8_t, (s16x8_t)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
