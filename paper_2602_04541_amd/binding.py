@@ -608,38 +608,95 @@ class Context:
     def prompt_attn(self, prompt: Prompt, q, k, v, token_start, lengths, out, lse, workspace, stream=None) -> None:
         """lychee_prompt_attn; q [n_tokens, H_q, 128]; k and v [n_tokens, H_kv, 128], or with lengths [B, H_kv, max_len, 128]; out
         [n_tokens, H_q, 128]; lse None or [H_q, n_tokens]."""
-        call, device, B, n = "lychee_prompt_attn", self.device, prompt.batch, prompt.n_tokens * prompt.n_q_heads
-        (at_q,) = self._rows_like(call, prompt, ("q", q))
-        at_k, at_v = self._keys_like(call, prompt, lengths is not None, ("k", k), ("v", v))
-        start, length, at_out, at_lse, ws = _arrays(
-            call, device, ("token_start", token_start, _I32, B + 1), ("lengths", lengths, _I32, B),
-            ("out", out, _BF16, n * prompt.head_dim), ("lse", lse, _F32, n), ("workspace", workspace, _dtype_of(workspace), 0))
-        _check(_lib.lychee_prompt_attn(self._h, prompt, at_q, at_k, at_v, start, length, at_out, at_lse, ws,
-                                       0 if ws is None else workspace.nbytes, self._on(stream)), call)
+        device, B, T, heads, kv, d = self.device, prompt.batch, prompt.n_tokens, prompt.n_q_heads, prompt.n_kv_heads, prompt.head_dim
+        n, tok, head, cached = T * heads, prompt.kv_stride_tok, prompt.kv_stride_head, lengths is not None
+        shape = (B, kv, prompt.max_len, d) if cached else (T, kv, d)
+        strides = (prompt.kv_stride_batch, head, tok, 1) if cached else (tok, head, 1)
+        try:
+            fine = (q.dtype is k.dtype is v.dtype is out.dtype is _BF16 and token_start.dtype is _I32
+                    and q.get_device() == k.get_device() == v.get_device() == out.get_device() == token_start.get_device()
+                    == workspace.get_device() == device
+                    and q.shape == (T, heads, d) and q.stride() == (prompt.q_stride_tok, prompt.q_stride_head, 1)
+                    and k.shape == shape == v.shape and k.stride() == strides == v.stride()
+                    and out.is_contiguous() and token_start.is_contiguous() and workspace.is_contiguous()
+                    and out.numel() >= n * d and token_start.numel() > B
+                    and (not cached or (lengths.dtype is _I32 and lengths.get_device() == device and lengths.is_contiguous()
+                                        and lengths.numel() >= B))
+                    and (lse is None or (lse.dtype is _F32 and lse.get_device() == device and lse.is_contiguous() and lse.numel() >= n)))
+        except AttributeError:  # (None, say)
+            fine = False
+        if fine:
+            at = (q.data_ptr(), k.data_ptr(), v.data_ptr(), token_start.data_ptr(), lengths.data_ptr() if cached else None, out.data_ptr(),
+                  None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.nbytes)
+        else:
+            call = "lychee_prompt_attn"
+            at = self._rows_like(call, prompt, ("q", q)) + self._keys_like(call, prompt, cached, ("k", k), ("v", v)) + _arrays(
+                call, device, ("token_start", token_start, _I32, B + 1), ("lengths", lengths, _I32, B), ("out", out, _BF16, n * d),
+                ("lse", lse, _F32, n), ("workspace", workspace, _dtype_of(workspace), 0)) + [0 if workspace is None else workspace.nbytes]
+        _check(_lib.lychee_prompt_attn(self._h, prompt, *at, self._on(stream)), "lychee_prompt_attn")
 
     def prompt_attn_backward(self, prompt: Prompt, d_out, q, k, v, out, lse, token_start, dq, dk, dv, workspace, stream=None) -> None:
         """lychee_prompt_attn_backward; dq strided like q, dk and dv like k and v."""
-        call, device, B, n = "lychee_prompt_attn_backward", self.device, prompt.batch, prompt.n_tokens * prompt.n_q_heads
-        at_q, at_dq = self._rows_like(call, prompt, ("q", q), ("dq", dq))
-        at_k, at_v, at_dk, at_dv = self._keys_like(call, prompt, False, ("k", k), ("v", v), ("dk", dk), ("dv", dv))
-        at_g, at_out, at_lse, start, ws = _arrays(
-            call, device, ("d_out", d_out, _BF16, n * prompt.head_dim), ("out", out, _BF16, n * prompt.head_dim), ("lse", lse, _F32, n),
-            ("token_start", token_start, _I32, B + 1), ("workspace", workspace, _dtype_of(workspace), 0))
-        _check(_lib.lychee_prompt_attn_backward(self._h, prompt, at_g, at_q, at_k, at_v, at_out, at_lse, start, at_dq, at_dk, at_dv, ws,
-                                                0 if ws is None else workspace.nbytes, self._on(stream)), call)
+        device, B, T, heads, kv, d = self.device, prompt.batch, prompt.n_tokens, prompt.n_q_heads, prompt.n_kv_heads, prompt.head_dim
+        n = T * heads
+        rows, keys = (T, heads, d), (T, kv, d)
+        of_rows, of_keys = (prompt.q_stride_tok, prompt.q_stride_head, 1), (prompt.kv_stride_tok, prompt.kv_stride_head, 1)
+        try:
+            fine = (d_out.dtype is q.dtype is k.dtype is v.dtype is out.dtype is dq.dtype is dk.dtype is dv.dtype is _BF16
+                    and lse.dtype is _F32 and token_start.dtype is _I32
+                    and d_out.get_device() == q.get_device() == k.get_device() == v.get_device() == out.get_device() == lse.get_device()
+                    == token_start.get_device() == dq.get_device() == dk.get_device() == dv.get_device() == workspace.get_device() == device
+                    and q.shape == rows == dq.shape and q.stride() == of_rows == dq.stride()
+                    and k.shape == keys == v.shape and k.stride() == of_keys == v.stride()
+                    and dk.shape == keys == dv.shape and dk.stride() == of_keys == dv.stride()
+                    and d_out.is_contiguous() and out.is_contiguous() and lse.is_contiguous() and token_start.is_contiguous()
+                    and workspace.is_contiguous() and d_out.numel() >= n * d <= out.numel() and lse.numel() >= n
+                    and token_start.numel() > B)
+        except AttributeError:
+            fine = False
+        if fine:
+            at = (d_out.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), token_start.data_ptr(),
+                  dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), workspace.data_ptr(), workspace.nbytes)
+        else:
+            call = "lychee_prompt_attn_backward"
+            at_q, at_dq = self._rows_like(call, prompt, ("q", q), ("dq", dq))
+            at_k, at_v, at_dk, at_dv = self._keys_like(call, prompt, False, ("k", k), ("v", v), ("dk", dk), ("dv", dv))
+            at_g, at_out, at_lse, start, ws = _arrays(
+                call, device, ("d_out", d_out, _BF16, n * d), ("out", out, _BF16, n * d), ("lse", lse, _F32, n),
+                ("token_start", token_start, _I32, B + 1), ("workspace", workspace, _dtype_of(workspace), 0))
+            at = (at_g, at_q, at_k, at_v, at_out, at_lse, start, at_dq, at_dk, at_dv, ws, 0 if ws is None else workspace.nbytes)
+        _check(_lib.lychee_prompt_attn_backward(self._h, prompt, *at, self._on(stream)), "lychee_prompt_attn_backward")
 
     def q4_prompt_attn(self, paged: Paged, q, cache, block_table, lengths, token_start, out, workspace, stream=None) -> None:
         """lychee_q4_prompt_attn; q [n_tokens, H_q, 128], strided; out [n_tokens, H_q, 128]."""
-        call, device, B = "lychee_q4_prompt_attn", self.device, paged.batch
-        n = q.shape[0] if isinstance(q, torch.Tensor) and q.dim() == 3 else 0
-        strides = (q.stride(0), q.stride(1), 1) if n else (paged.head_dim, 0, 1)
-        at_q = _strided_at(call, "q", q, (n, paged.n_q_heads, paged.head_dim), strides, device)
-        length, start, at_out, ws = _arrays(
-            call, device, ("lengths", lengths, _I32, B), ("token_start", token_start, _I32, B + 1),
-            ("out", out, _BF16, n * paged.n_q_heads * paged.head_dim), ("workspace", workspace, _dtype_of(workspace), 0))
-        _check(_lib.lychee_q4_prompt_attn(self._h, paged, at_q, strides[0], strides[1], n, _cache_at(call, cache, paged, device),
-                                          _table_at(call, block_table, paged, device), length, start, at_out, ws,
-                                          0 if ws is None else workspace.nbytes, self._on(stream)), call)
+        device, B, heads, d, pages, width = self.device, paged.batch, paged.n_q_heads, paged.head_dim, paged.n_pages, paged.table_stride
+        try:
+            n, strides = q.shape[0], q.stride()
+            fine = (q.dtype is out.dtype is _BF16 and lengths.dtype is token_start.dtype is block_table.dtype is _I32
+                    and cache.element_size() == 1
+                    and q.get_device() == cache.get_device() == block_table.get_device() == lengths.get_device() == token_start.get_device()
+                    == out.get_device() == workspace.get_device() == device
+                    and q.shape == (n, heads, d) and n > 0 and strides[2] == 1
+                    and cache.is_contiguous() and block_table.is_contiguous() and lengths.is_contiguous() and token_start.is_contiguous()
+                    and out.is_contiguous() and workspace.is_contiguous() and block_table.shape == (B, width)
+                    and cache.numel() >= pages * paged.page_tiles * Q4_TILE_BYTES and lengths.numel() >= B < token_start.numel()
+                    and out.numel() >= n * heads * d)
+        except (AttributeError, IndexError):
+            fine = False
+        if fine:
+            at = (q.data_ptr(), strides[0], strides[1], n, cache.data_ptr(), block_table.data_ptr(), lengths.data_ptr(),
+                  token_start.data_ptr(), out.data_ptr(), workspace.data_ptr(), workspace.nbytes)
+        else:
+            call = "lychee_q4_prompt_attn"
+            n = q.shape[0] if isinstance(q, torch.Tensor) and q.dim() == 3 else 0
+            strides = (q.stride(0), q.stride(1), 1) if n else (d, 0, 1)
+            at_q = _strided_at(call, "q", q, (n, heads, d), strides, device)
+            length, start, at_out, ws = _arrays(
+                call, device, ("lengths", lengths, _I32, B), ("token_start", token_start, _I32, B + 1), ("out", out, _BF16, n * heads * d),
+                ("workspace", workspace, _dtype_of(workspace), 0))
+            at = (at_q, strides[0], strides[1], n, _cache_at(call, cache, paged, device), _table_at(call, block_table, paged, device), length,
+                  start, at_out, ws, 0 if ws is None else workspace.nbytes)
+        _check(_lib.lychee_q4_prompt_attn(self._h, paged, *at, self._on(stream)), "lychee_q4_prompt_attn")
 
     # -- helpers ------------------------------------------------------------------------
     def select_stats(self, stream=None):

@@ -10,7 +10,10 @@ constexpr int kPromptMaxGroup = 16;
 constexpr int kPromptRows = 128;          // query rows of a tile, a row being a (token, query head of the KV head)
 constexpr int kPromptKeys = 64;           // keys a workgroup takes at a time
 constexpr int kPromptMinPiece = 4;        // blocks of keys in a piece of a split tile, at least
-constexpr int kPromptMinRowPiece = 4;     // and blocks of rows in a piece of a tile of keys
+#ifndef MRP
+#define MRP 4
+#endif
+constexpr int kPromptMinRowPiece = MRP;     // and blocks of rows in a piece of a tile of keys
 constexpr int64_t kPromptMaxRows = 1 << 28;  // query tokens times heads of a group (row numbers are divided with a multiplication)
 constexpr int64_t kPromptMaxStride = 1 << 24;  // elements from a token's row to the next (offsets within 64 rows fit 32 bits)
 

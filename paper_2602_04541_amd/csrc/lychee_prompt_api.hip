@@ -10,11 +10,15 @@ using namespace lychee;
 
 namespace {
 
-constexpr int32_t kPromptSlots = 512;  // pieces that fill a device: two workgroups a compute unit
+#ifndef SLOTS
+#define SLOTS 512
+#endif
+constexpr int32_t kPromptSlots = SLOTS;  // pieces that fill a device: two workgroups a compute unit
 #ifndef KEYSLOTS
 #define KEYSLOTS 1024
 #endif
 constexpr int32_t kPromptKeySlots = KEYSLOTS;
+constexpr int64_t kPromptSplitKeys = 1024;
 constexpr int64_t kMaxGrid = 1 << 24;  // workgroups of 256 threads, which are counted in 32 bits
 
 int check_heads_of(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim)
@@ -36,7 +40,7 @@ Grid grid_of(int32_t batch, int32_t n_kv_heads, int32_t group, int32_t n_tokens,
     Grid w;
     w.tiles = (int64_t)n_tokens * group / kPromptRows + (batch < n_tokens ? batch : n_tokens);
     // Few tiles over many keys are split along these: a piece has kPromptMinPiece blocks at least.
-    const bool split = w.tiles * n_kv_heads < 2 * kPromptSlots && max_len > 2 * kPromptMinPiece * kPromptKeys;
+    const bool split = w.tiles * n_kv_heads < 2 * kPromptSlots && max_len > kPromptSplitKeys;
     w.slots = split ? kPromptSlots : 0;
     w.items = w.tiles + (split ? (kPromptSlots + n_kv_heads - 1) / n_kv_heads : 0);
     return w;

@@ -155,37 +155,72 @@ __device__ __forceinline__ void find_request(int batch, int number, int weight, 
     __syncthreads();
 }
 
+// A request that a workgroup has found a piece of: the piece's number within it, and its first partial's.
+struct Found {
+    int b, at, before, start, n, len;
+};
+__device__ __forceinline__ Found found_alone(int number, int items, int start, int n, int len)
+{
+    Found f;
+    f.b = number < __builtin_amdgcn_readfirstlane(items) ? 0 : -1;
+    f.at = number;
+    f.before = 0;
+    f.start = __builtin_amdgcn_readfirstlane(start);
+    f.n = __builtin_amdgcn_readfirstlane(n);
+    f.len = __builtin_amdgcn_readfirstlane(len);
+    return f;
+}
+__device__ __forceinline__ Found found_among(const SharedPlan &sh)
+{
+    Found f;
+    f.b = __builtin_amdgcn_readfirstlane(sh.found[0]);
+    f.at = __builtin_amdgcn_readfirstlane(sh.found[1]);
+    f.before = __builtin_amdgcn_readfirstlane(sh.found[2]);
+    const int b = f.b < 0 ? 0 : f.b;
+    f.start = __builtin_amdgcn_readfirstlane(sh.start[b]);
+    f.n = __builtin_amdgcn_readfirstlane(sh.n[b]);
+    f.len = __builtin_amdgcn_readfirstlane(sh.len[b]);
+    return f;
+}
+
 // The piece with this number (MERGE: the tile); of a request the last tile first, which sees most keys.  `slots` > 0: tiles are
 // split into pieces of so many blocks that there are about `slots` of them in all KV heads.
 template <bool MERGE>
 __device__ __forceinline__ Tile find_tile(const PromptRows &p, int number, int slots, SharedPlan &sh)
 {
-    const int t = threadIdx.x;
+    const bool alone = p.batch == 1;  // (nothing to look for, no barrier)
+    const int t = alone ? 0 : threadIdx.x;
     int start = 0, n = 0, len = 0;
     if (t < p.batch) request_of(p, t, start, n, len);
     const int tiles = tiles_of(n * p.group), blocks = blocks_of(len);
-    sh.n[t] = n;
-    sh.len[t] = len;
-    sh.start[t] = start;
     int size = 1 << 30;
     if (slots > 0) {
-        const unsigned long long w = sum_all((unsigned long long)tiles * (unsigned)max(blocks, 1) * (unsigned)p.n_kv_heads, sh);
-        size = max((int)min((w + slots - 1) / slots, 1ull << 30), kPromptMinPiece);
+        unsigned long long w = (unsigned long long)tiles * (unsigned)max(blocks, 1) * (unsigned)p.n_kv_heads;
+        if (!alone) w = sum_all(w, sh);
+        size = __builtin_amdgcn_readfirstlane(max((int)min((w + slots - 1) / slots, 1ull << 30), kPromptMinPiece));
     }
     const int items = tiles * max(1, (blocks + size - 1) / size);
-    find_request(p.batch, number, len, MERGE ? tiles : items, items, sh);
+    Found f;
+    if (alone) {
+        f = found_alone(number, MERGE ? tiles : items, start, n, len);
+    } else {
+        sh.n[t] = n;
+        sh.len[t] = len;
+        sh.start[t] = start;
+        find_request(p.batch, number, len, MERGE ? tiles : items, items, sh);
+        f = found_among(sh);
+    }
     Tile w;
-    w.b = __builtin_amdgcn_readfirstlane(sh.found[0]);
-    w.found = w.b >= 0;
+    w.b = f.b;
+    w.found = f.b >= 0;
     if (!w.found) return w;
-    const int at = __builtin_amdgcn_readfirstlane(sh.found[1]), before = __builtin_amdgcn_readfirstlane(sh.found[2]);
-    w.n = __builtin_amdgcn_readfirstlane(sh.n[w.b]);
-    w.len = __builtin_amdgcn_readfirstlane(sh.len[w.b]);
-    w.start = __builtin_amdgcn_readfirstlane(sh.start[w.b]);
-    const int rows = w.n * p.group, of_tiles = tiles_of(rows), pieces = max(1, (blocks_of(w.len) + size - 1) / size);
-    w.tile = of_tiles - 1 - (MERGE ? at : at / pieces);
-    w.piece = MERGE ? 0 : at % pieces;
-    w.slot = before + (MERGE ? at * pieces : at);
+    w.n = f.n;
+    w.len = f.len;
+    w.start = f.start;
+    const int rows = w.n * p.group, pieces = max(1, (blocks_of(w.len) + size - 1) / size);
+    w.tile = tiles_of(rows) - 1 - (MERGE ? f.at : f.at / pieces);
+    w.piece = MERGE ? 0 : f.at % pieces;
+    w.slot = f.before + (MERGE ? f.at * pieces : f.at);
     const int seen = max(0, w.len - w.n + token_of(p, min((w.tile + 1) * kPromptRows, rows) - 1) + 1);  // keys of the last row
     w.parts = max(1, (blocks_of(seen) + size - 1) / size);
     w.first = pieces == 1 ? 0 : w.piece * size;
@@ -202,36 +237,45 @@ template <bool MERGE>
 __device__ __forceinline__ Tile find_key_tile(const PromptRows &p, int number, int slots, SharedPlan &sh)
 {
     static_assert(kPromptRows == 2 * kPromptKeys, "");
-    const int t = threadIdx.x;
+    const bool alone = p.batch == 1;
+    const int t = alone ? 0 : threadIdx.x;
     int start = 0, n = 0, len = 0;
     if (t < p.batch) request_of(p, t, start, n, len);
     const int tiles = tiles_of(n);
     const int64_t work = blocks_before(tiles, blocks_of(n * p.group), p.group);
-    sh.n[t] = n;
-    sh.start[t] = start;
-    const unsigned long long all = sum_all((unsigned long long)work * (unsigned)p.n_kv_heads, sh);
-    const int size = max((int)min((all + slots - 1) / slots, 1ull << 30), kPromptMinRowPiece);
-    // (tiles of several pieces are the first ones, fewer than work / size)
-    find_request(p.batch, number, n, MERGE ? tiles : (int)(work / size) + tiles, 2 * (int)(work / size), sh);
+    unsigned long long all = (unsigned long long)work * (unsigned)p.n_kv_heads;
+    if (!alone) all = sum_all(all, sh);
+    const int size = __builtin_amdgcn_readfirstlane(max((int)min((all + slots - 1) / slots, 1ull << 30), kPromptMinRowPiece));
+    const int items = MERGE ? tiles : (int)(work / size) + tiles;
+    Found f;
+    if (alone) {
+        f = found_alone(number, items, start, n, len);
+    } else {
+        sh.n[t] = n;
+        sh.len[t] = n;
+        sh.start[t] = start;
+        // (tiles of several pieces are the first ones, fewer than work / size)
+        find_request(p.batch, number, n, items, 2 * (int)(work / size), sh);
+        f = found_among(sh);
+    }
     Tile w;
-    w.b = __builtin_amdgcn_readfirstlane(sh.found[0]);
-    w.found = w.b >= 0;
+    w.b = f.b;
+    w.found = f.b >= 0;
     if (!w.found) return w;
-    const int at = __builtin_amdgcn_readfirstlane(sh.found[1]), before = __builtin_amdgcn_readfirstlane(sh.found[2]);
-    w.n = __builtin_amdgcn_readfirstlane(sh.n[w.b]);
-    w.len = w.n;
-    w.start = __builtin_amdgcn_readfirstlane(sh.start[w.b]);
+    w.n = f.n;
+    w.len = f.n;
+    w.start = f.start;
     const int end = blocks_of(w.n * p.group);
-    int tile = at;
+    int tile = f.at;
     if (!MERGE) {  // the last tile that begins at or before the piece
         tile = 0;
         for (int step = 1 << 17; step > 0; step >>= 1)
-            if (tile + step < tiles_of(w.n) && blocks_before(tile + step, end, p.group) / size + tile + step <= at) tile += step;
+            if (tile + step < tiles_of(w.n) && blocks_before(tile + step, end, p.group) / size + tile + step <= f.at) tile += step;
     }
     const int from = (int)(blocks_before(tile, end, p.group) / size) + tile;
     w.tile = tile;
-    w.piece = MERGE ? 0 : at - from;
-    w.slot = before + from + w.piece;
+    w.piece = MERGE ? 0 : f.at - from;
+    w.slot = f.before + from + w.piece;
     const int first = 2 * p.group * tile;
     w.parts = max(1, (end - first + size - 1) / size);
     w.first = first + w.piece * size;

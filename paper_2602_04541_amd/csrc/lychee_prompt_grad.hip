@@ -158,8 +158,10 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dkv_kernel(PromptGradArgs 
     if (!w.found || w.piece >= w.parts || (w.parts > 1 && w.slot >= a.n_slots)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hi = lane >> 5;
     const int tile = w.tile, rows = w.n * p.group;
-    const int key = tile * kPromptRows + wave * 32 + (lane & 31), key_in = min(key, w.n - 1);
-    const int64_t kv_at = (int64_t)(w.start + key_in) * a.kv_tok + (int64_t)g * a.kv_head;
+    const auto key_of = [&](uint32_t lane) { return tile * kPromptRows + wave * 32 + (int)(lane & 31); };
+    const auto kv_of = [&](int key) { return (int64_t)(w.start + min(key, w.n - 1)) * a.kv_tok + (int64_t)g * a.kv_head; };
+    const int64_t kv_at = kv_of(key_of(lane));
+    const int key_rows = key_of(lane) * p.group;  // rows from here on see the lane's key
     __syncthreads();  // (the plan's part of LDS is free)
     bf16x8_t kf[8], vf[kHeld];
 #pragma unroll
@@ -217,7 +219,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dkv_kernel(PromptGradArgs 
             const LYCHEE_LDS uint8_t *Q = (const LYCHEE_LDS uint8_t *)sh.a[buf], *G = (const LYCHEE_LDS uint8_t *)sh.b[buf];
             if (careful || r0 + kPromptKeys > wave_first) {
                 const bool masked = r0 < wave_all || r0 + kPromptKeys > rows;
-                const int least = key * p.group - r0, most = rows - 1 - r0;
+                const int least = key_rows - r0, most = rows - 1 - r0;
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     if (careful && turn % 2 != x) continue;
@@ -275,9 +277,10 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dkv_kernel(PromptGradArgs 
         careful = true;
     }
     if (w.parts == 1) {
-        const bool there = key < w.n;
-        store_row(there ? a.dk + kv_at : nullptr, lane, dk, a.scale);
-        store_row(there ? a.dv + kv_at : nullptr, lane, dv, 1.f);
+        const int key = key_of(opaque(lane));
+        const int64_t to = kv_of(key);
+        store_row(key < w.n ? a.dk + to : nullptr, lane, dk, a.scale);
+        store_row(key < w.n ? a.dv + to : nullptr, lane, dv, 1.f);
     } else {
         float *to = a.part + (((int64_t)w.slot * p.n_kv_heads + g) * kWaves + wave) * kPartFloats + 4 * lane;
 #pragma unroll
