@@ -211,7 +211,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
                 bf16x8_t pf[4] = {operand<0>(z[0]), operand<8>(z[0]), operand<0>(z[1]), operand<8>(z[1])};
                 if (__builtin_expect(careful, 0)) {
                     __syncthreads();
-                    take_with_care(sh.v[turn & 1], turn % 3);
+                    take_with_care(sh.v[turn & 1], kBlockBytes, turn % 3);
                     __syncthreads();
                     if (turn % 3 != 0) {
                         l = before;

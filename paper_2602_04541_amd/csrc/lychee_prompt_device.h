@@ -346,10 +346,10 @@ __device__ __forceinline__ uint32_t opaque(uint32_t x)
 // (seen_rows), and turn 2 its negative for NaN, which both infinities add up to.  The block is changed in LDS, behind the products
 // that make the scores.
 constexpr uint32_t kLargest = 0x7F7Fu;
-__device__ __forceinline__ void take_with_care(uint8_t *block, int turn)
+__device__ __forceinline__ void take_with_care(uint8_t *block, int bytes, int turn)
 {
 #pragma unroll 1
-    for (int i = threadIdx.x; i < kBlockBytes / 4; i += kThreads) {
+    for (int i = threadIdx.x; i < bytes / 4; i += kThreads) {
         uint32_t *at = reinterpret_cast<uint32_t *>(block) + i, both = *at, to = 0;
 #pragma unroll
         for (int h = 0; h < 32; h += 16) {

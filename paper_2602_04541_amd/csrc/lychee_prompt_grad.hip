@@ -13,7 +13,8 @@ namespace lychee {
 namespace {
 
 constexpr int kPartFloats = 2 * 16 * 64 * 4;  // a wavefront's part of a piece's sums
-constexpr int kHeld = 5;  // of the second launch's eight steps of V those that stay in registers
+constexpr int kGradRows = 32;  // rows that the second launch takes at a time
+constexpr int kGradBytes = kGradRows * kRowBytes;
 
 struct SharedGrad {
     union {
@@ -21,9 +22,13 @@ struct SharedGrad {
         struct {
             __align__(16) uint8_t a[2][kBlockBytes];
             __align__(16) uint8_t b[2][kBlockBytes];
-            __align__(16) float stat[2][2][kPromptKeys];  // second launch, of a block's rows: -lse sqrt(128), -delta
-            __align__(16) bf16x8_t v[kWaves][8 - kHeld][64];
         };
+        struct {
+            __align__(16) uint8_t q[2][kGradBytes];
+            __align__(16) uint8_t g[2][kGradBytes];
+            __align__(16) float stat[2][2][kGradRows];  // of a block's rows: -lse sqrt(128), -delta
+            __align__(16) bf16x8_t v[kWaves][8][64];
+        } keys;
     };
 };
 static_assert(sizeof(SharedGrad) <= 80 * 1024, "two workgroups a compute unit");
@@ -124,7 +129,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dq_kernel(PromptGradArgs a
                     bf16x8_t ds[2] = {operand<0>(z), operand<8>(z)};
                     if (__builtin_expect(careful, 0)) {
                         __syncthreads();
-                        take_with_care(sh.a[buf], turn / 2 % 3);
+                        take_with_care(sh.a[buf], kBlockBytes, turn / 2 % 3);
                         __syncthreads();
                         if (turn / 2 % 3 != 0) {
 #pragma unroll
@@ -163,115 +168,123 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dkv_kernel(PromptGradArgs 
     const int64_t kv_at = kv_of(key_of(lane));
     const int key_rows = key_of(lane) * p.group;  // rows from here on see the lane's key
     __syncthreads();  // (the plan's part of LDS is free)
-    bf16x8_t kf[8], vf[kHeld];
+    bf16x8_t kf[8];
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) {
         kf[ks] = *(const LYCHEE_GLOBAL bf16x8_t *)(a.k + kv_at + 16 * ks + 8 * hi);
-        const bf16x8_t v = *(const LYCHEE_GLOBAL bf16x8_t *)(a.v + kv_at + 16 * ks + 8 * hi);
-        if (ks < kHeld)
-            vf[ks] = v;
-        else
-            sh.v[wave][ks - kHeld][lane] = v;
+        sh.keys.v[wave][ks][lane] = *(const LYCHEE_GLOBAL bf16x8_t *)(a.v + kv_at + 16 * ks + 8 * hi);
     }
     const uint32_t row_at = row_place(lane), turn_at = turn_place(lane);
-    const uint32_t to_q = lds_address(sh.a) + wave * 4 * kRowBytes, to_g = lds_address(sh.b) + wave * 4 * kRowBytes;
+    const uint32_t to_q = lds_address(sh.keys.q) + wave * 4 * kRowBytes, to_g = lds_address(sh.keys.g) + wave * 4 * kRowBytes;
     const int64_t packed_tok = (int64_t)p.n_kv_heads * p.group * kHeadDim;
-    const auto fetch = [&](int blk, int buf) {
-        const int r0 = blk * kPromptKeys, t0 = token_of(p, r0), at = (int)opaque(lane);
+    const auto fetch = [&](int r0, int buf) {
+        const int t0 = token_of(p, r0), at = (int)opaque(lane);
         const int fetch_row = r0 + 4 * wave + (at >> 4);
         const uint32_t fetch_chunk = (uint32_t)((at & 15) ^ swizzle(fetch_row)) << 4;
         const uint16_t *q = a.q + (int64_t)(w.start + t0) * p.q_tok + (int64_t)g * p.group * p.q_head;
         const uint16_t *go = a.g + (int64_t)(w.start + t0) * packed_tok + (int64_t)g * p.group * kHeadDim;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < kGradRows / 16; ++i) {
             const int r = min(fetch_row + 16 * i, rows - 1), t = token_of(p, r), h = r - t * p.group;
             copy16(q, (uint32_t)(t - t0) * (uint32_t)(2 * p.q_tok) + (uint32_t)h * (uint32_t)(2 * p.q_head) + fetch_chunk,
-                   to_q + buf * kBlockBytes + i * 16 * kRowBytes);
+                   to_q + buf * kGradBytes + i * 16 * kRowBytes);
             copy16(go, (uint32_t)(t - t0) * (uint32_t)(2 * packed_tok) + (uint32_t)h * (2 * kHeadDim) + fetch_chunk,
-                   to_g + buf * kBlockBytes + i * 16 * kRowBytes);
+                   to_g + buf * kGradBytes + i * 16 * kRowBytes);
         }
-        if (wave < 2) {
+        if (wave < 2 && at < kGradRows) {  // (one wavefront lse, one delta)
             const int r = min(r0 + at, rows - 1), t = token_of(p, r), h = r - t * p.group;
-            copy4(a.stat + ((int64_t)wave * p.n_kv_heads + g) * p.group * p.n_tokens + w.start, ((uint32_t)h * (uint32_t)p.n_tokens + (uint32_t)t) * 4u,
-                  lds_address(sh.stat[buf][wave]));
+            copy4(a.stat + ((int64_t)wave * p.n_kv_heads + g) * p.group * p.n_tokens + w.start,
+                  ((uint32_t)h * (uint32_t)p.n_tokens + (uint32_t)t) * 4u, lds_address(sh.keys.stat[buf][wave]));
         }
     };
-    const auto arrive = [&](int) {
+    const auto arrive = [&]() {
         wait_copies();
         __syncthreads();
     };
-    const int first = w.first, last = w.last;
-    const int wave_first = (tile * kPromptRows + wave * 32) * p.group;            // rows from here on see a key of the wavefront
-    const int wave_all = (tile * kPromptRows + wave * 32 + 31) * p.group;         // and from here on all of them
+    const int from = w.first * kPromptKeys, blocks = (min(w.last * kPromptKeys, rows) - from + kGradRows - 1) / kGradRows;
+    const int wave_first = (tile * kPromptRows + wave * 32) * p.group;     // rows from here on see a key of the wavefront
+    const int wave_all = (tile * kPromptRows + wave * 32 + 31) * p.group;  // and from here on all of them
 
     f32x16_t dk[4], dv[4];
     bool careful = false;
     for (;;) {
-        const int turns = (careful ? 6 : 1) * (last - first);  // (as for dq)
-        const auto block_of = [&](int turn) { return first + (careful ? turn / 6 : turn); };
+        const int turns = (careful ? 3 : 1) * blocks;  // (take_with_care)
+        const auto row_of = [&](int turn) { return from + (careful ? turn / 3 : turn) * kGradRows; };
 #pragma unroll
         for (int db = 0; db < 4; ++db) dk[db] = zero16(), dv[db] = zero16();
-        fetch(first, 0);
-        arrive(0);
+        fetch(row_of(0), 0);
+        arrive();
         for (int turn = 0; turn < turns; ++turn) {
-            const int blk = block_of(turn), buf = turn & 1, r0 = blk * kPromptKeys;
-            if (turn + 1 < turns) fetch(block_of(turn + 1), buf ^ 1);
-            const LYCHEE_LDS uint8_t *Q = (const LYCHEE_LDS uint8_t *)sh.a[buf], *G = (const LYCHEE_LDS uint8_t *)sh.b[buf];
-            if (careful || r0 + kPromptKeys > wave_first) {
-                const bool masked = r0 < wave_all || r0 + kPromptKeys > rows;
+            const int r0 = row_of(turn), buf = turn & 1;
+            if (turn + 1 < turns) fetch(row_of(turn + 1), buf ^ 1);
+            const LYCHEE_LDS uint8_t *Q = (const LYCHEE_LDS uint8_t *)sh.keys.q[buf], *G = (const LYCHEE_LDS uint8_t *)sh.keys.g[buf];
+            if (careful || r0 + kGradRows > wave_first) {
+                const uint32_t kat = opaque(row_at), vat = opaque(turn_at);
+                f32x16_t z, dp;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const f32x4_t l = *reinterpret_cast<const f32x4_t *>(&sh.keys.stat[buf][0][8 * j + 4 * hi]);
+                    const f32x4_t d = *reinterpret_cast<const f32x4_t *>(&sh.keys.stat[buf][1][8 * j + 4 * hi]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z[4 * j + i] = l[i], dp[4 * j + i] = d[i];
+                }
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks) {
+                    z = mfma(read_rows(Q, kat, 0, ks), kf[ks], z);
+                    dp = mfma(read_rows(G, kat, 0, ks), ((const LYCHEE_LDS bf16x8_t *)sh.keys.v[wave][ks])[lane], dp);
+                }
+                // (the first operands, and six reads ahead of the products from there)
+                __builtin_amdgcn_sched_group_barrier(kGroupRead, 14, 0);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(kGroupMfma, 1, 0);
+                    if (i % 2)
+                        __builtin_amdgcn_sched_group_barrier(kGroupRead, 2, 0);
+                    else
+                        __builtin_amdgcn_sched_group_barrier(kGroupRead, 1, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    z[i] = fast_exp2(z[i] * a.scale_log2e);
+                    dp[i] *= z[i];
+                }
                 const int least = key_rows - r0, most = rows - 1 - r0;
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    if (careful && turn % 2 != x) continue;
-                    const uint32_t kat = opaque(row_at), vat = opaque(turn_at);
-                    f32x16_t z, dp;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const f32x4_t l = *reinterpret_cast<const f32x4_t *>(&sh.stat[buf][0][32 * x + 8 * j + 4 * hi]);
-                        const f32x4_t d = *reinterpret_cast<const f32x4_t *>(&sh.stat[buf][1][32 * x + 8 * j + 4 * hi]);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) z[4 * j + i] = l[i], dp[4 * j + i] = d[i];
-                    }
-#pragma unroll
-                    for (int ks = 0; ks < 8; ++ks) {
-                        z = mfma(read_rows(Q, kat, x, ks), kf[ks], z);
-                        dp = mfma(read_rows(G, kat, x, ks), ks < kHeld ? vf[ks] : ((const LYCHEE_LDS bf16x8_t *)sh.v[wave][ks - kHeld])[lane], dp);
-                    }
+                if (r0 < wave_all || r0 + kGradRows > rows) {
+                    asm volatile("");
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        z[i] = fast_exp2(z[i] * a.scale_log2e);
-                        dp[i] *= z[i];
+                        const int r = i % 4 + 8 * (i / 4) + 4 * hi;
+                        const bool seen = r >= least && r <= most;
+                        z[i] = seen ? z[i] : 0.f;
+                        dp[i] = seen ? dp[i] : 0.f;
                     }
-                    if (masked) {
-                        const int from = least - 32 * x - 4 * hi, to = most - 32 * x - 4 * hi;
+                }
+                bf16x8_t pf[2] = {operand<0>(z), operand<8>(z)}, ds[2] = {operand<0>(dp), operand<8>(dp)};
+                if (__builtin_expect(careful, 0)) {
+                    __syncthreads();
+                    take_with_care(sh.keys.q[buf], kGradBytes, turn % 3);
+                    take_with_care(sh.keys.g[buf], kGradBytes, turn % 3);
+                    __syncthreads();
+                    if (turn % 3 != 0) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const bool seen = i % 4 + 8 * (i / 4) >= from && i % 4 + 8 * (i / 4) <= to;
-                            z[i] = seen ? z[i] : 0.f;
-                            dp[i] = seen ? dp[i] : 0.f;
-                        }
+                        for (int s = 0; s < 2; ++s) pf[s] = ds[s] = seen_rows(hi, s, least, most);
                     }
-                    bf16x8_t pf[2] = {operand<0>(z), operand<8>(z)}, ds[2] = {operand<0>(dp), operand<8>(dp)};
-                    if (__builtin_expect(careful, 0)) {
-                        __syncthreads();
-                        take_with_care(sh.a[buf], turn / 2 % 3);
-                        take_with_care(sh.b[buf], turn / 2 % 3);
-                        __syncthreads();
-                        if (turn / 2 % 3 != 0) {
+                }
 #pragma unroll
-                            for (int s = 0; s < 2; ++s) pf[s] = ds[s] = seen_rows(hi, 2 * x + s, least, most);
-                        }
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int db = 0; db < 4; ++db) {
+                        dv[db] = mfma(read_turned(G, vat, db, s), pf[s], dv[db]);
+                        dk[db] = mfma(read_turned(Q, vat, db, s), ds[s], dk[db]);
                     }
+                __builtin_amdgcn_sched_group_barrier(kGroupRead, 8, 0);
 #pragma unroll
-                    for (int s = 0; s < 2; ++s)
-#pragma unroll
-                        for (int db = 0; db < 4; ++db) {
-                            dv[db] = mfma(read_turned(G, vat, db, 2 * x + s), pf[s], dv[db]);
-                            dk[db] = mfma(read_turned(Q, vat, db, 2 * x + s), ds[s], dk[db]);
-                        }
+                for (int i = 0; i < 16; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(kGroupMfma, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(kGroupRead, 2, 0);
                 }
             }
-            arrive(buf ^ 1);
+            arrive();
         }
         if (careful || !__syncthreads_or(!all_finite(dk) || !all_finite(dv))) break;
         careful = true;
