@@ -10,10 +10,7 @@ constexpr int kPromptMaxGroup = 16;
 constexpr int kPromptRows = 128;          // query rows of a tile, a row being a (token, query head of the KV head)
 constexpr int kPromptKeys = 64;           // keys a workgroup takes at a time
 constexpr int kPromptMinPiece = 4;        // blocks of keys in a piece of a split tile, at least
-#ifndef MRP
-#define MRP 4
-#endif
-constexpr int kPromptMinRowPiece = MRP;     // and blocks of rows in a piece of a tile of keys
+constexpr int kPromptMinRowPiece = 2;     // and blocks of rows in a range of tiles of keys
 constexpr int64_t kPromptMaxRows = 1 << 28;  // query tokens times heads of a group (row numbers are divided with a multiplication)
 constexpr int64_t kPromptMaxStride = 1 << 24;  // elements from a token's row to the next (offsets within 64 rows fit 32 bits)
 
@@ -52,9 +49,10 @@ struct PromptGradArgs {
     uint16_t *dq, *dk, *dv;  // strided like q, k and v
     float *stat;             // [2][n_q_heads][n_tokens] -lse sqrt(128), -(g . out): what the products of the second launch begin with
     float scale, scale_log2e, root;  // 1 / sqrt(128), log2(e) / sqrt(128), sqrt(128)
-    float *part;             // [piece][wavefront][dk, dv][16][64][4] sums over a piece's rows, as registers and lanes hold them
-    int32_t slots;           // pieces that tiles of keys are split into, about
-    int32_t n_row_tiles, n_key_tiles, n_key_items, n_slots;  // of a KV head, at most
+    float *part;             // [range][2][KV head][wavefront][dk, dv][16][64][4] sums over a part of a tile's rows, as registers
+                             // and lanes hold them
+    int32_t n_ranges;        // workgroups of the second launch that share a KV head's tiles of keys
+    int32_t n_row_tiles, n_key_tiles;  // of a KV head, at most
 };
 
 hipError_t launch_prompt(const PromptArgs &a, hipStream_t stream);

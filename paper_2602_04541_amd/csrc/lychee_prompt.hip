@@ -258,10 +258,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
 // Rows of split tiles: o = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p, M = max m_p.  A workgroup has 32 rows of a tile and some of the
 // 16 groups of eight dimensions, its wavefronts a fourth of the pieces each, a lane four dimensions of a row, as the pieces left
 // them; the wavefronts' sums meet in LDS.
-#ifndef MB
-#define MB 8
-#endif
-constexpr int kMergeBatch = MB;  // pieces whose loads are in flight together
+constexpr int kMergeBatch = 16;  // pieces whose loads are in flight together
 __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptArgs a)
 {
     __shared__ SharedPlan sh;

@@ -10,14 +10,7 @@ using namespace lychee;
 
 namespace {
 
-#ifndef SLOTS
-#define SLOTS 512
-#endif
-constexpr int32_t kPromptSlots = SLOTS;  // pieces that fill a device: two workgroups a compute unit
-#ifndef KEYSLOTS
-#define KEYSLOTS 1024
-#endif
-constexpr int32_t kPromptKeySlots = KEYSLOTS;
+constexpr int32_t kPromptSlots = 512;  // pieces that fill a device: two workgroups a compute unit
 constexpr int64_t kPromptSplitKeys = 1024;
 constexpr int64_t kMaxGrid = 1 << 24;  // workgroups of 256 threads, which are counted in 32 bits
 
@@ -46,26 +39,25 @@ Grid grid_of(int32_t batch, int32_t n_kv_heads, int32_t group, int32_t n_tokens,
     return w;
 }
 
-// Tiles of keys of a KV head in the backward pass, their pieces (one more a tile than the blocks hold of the smallest piece, or the
-// device is filled with), and partials (find_key_tile: twice as many).
+// Ranges that a KV head's tiles of keys are shared out to in the backward pass: what fills the device, no more than there are
+// smallest pieces.
 struct KeyGrid {
-    int64_t tiles, items, slots;
+    int64_t tiles, ranges;
 };
 KeyGrid key_grid_of(int32_t batch, int32_t n_kv_heads, int32_t group, int32_t n_tokens)
 {
     KeyGrid w;
-    const int64_t many = batch < n_tokens ? batch : n_tokens, blocks = (int64_t)n_tokens * group / kPromptKeys + 1;
-    w.tiles = n_tokens / kPromptRows + many;
-    const int64_t most = w.tiles * (blocks / kPromptMinRowPiece + 1), fill = (kPromptKeySlots + n_kv_heads - 1) / n_kv_heads;
-    w.items = w.tiles + (most < fill ? most : fill);
-    w.slots = 2 * (most < fill ? most : fill);
+    w.tiles = n_tokens / kPromptRows + (batch < n_tokens ? batch : n_tokens);
+    const int64_t blocks = w.tiles * ((int64_t)n_tokens * group / kPromptKeys + 1), fill = kPromptSlots / n_kv_heads;
+    w.ranges = blocks / kPromptMinRowPiece + 1;
+    if (w.ranges > fill) w.ranges = fill;
     return w;
 }
 
 struct CarvedPrompt {
     size_t part_ml, stat, part, total;
 };
-CarvedPrompt carve(const Grid &w, int32_t n_kv_heads, int64_t stats, int64_t key_slots)
+CarvedPrompt carve(const Grid &w, int32_t n_kv_heads, int64_t stats, int64_t ranges)
 {
     CarvedPrompt c;
     const int64_t rows = w.slots > 0 ? w.items * n_kv_heads * kPromptRows : 0;
@@ -73,7 +65,7 @@ CarvedPrompt carve(const Grid &w, int32_t n_kv_heads, int64_t stats, int64_t key
     c.stat = 0;
     // (the forward pass's partials and those of the backward pass are not needed at once)
     c.part = (size_t)round_up(stats * 2 * (int64_t)sizeof(float), 256);
-    c.total = c.part + (size_t)(key_slots * n_kv_heads * 2 * kPromptRows * kHeadDim * (int64_t)sizeof(float));
+    c.total = c.part + (size_t)(ranges * 2 * n_kv_heads * 2 * kPromptRows * kHeadDim * (int64_t)sizeof(float));
     const size_t forward = c.part_ml + (size_t)round_up(rows * 2 * (int64_t)sizeof(float), 256);
     if (c.total < forward) c.total = forward;
     if (c.total == 0) c.total = 256;
@@ -105,7 +97,7 @@ Grid grid_of(const lychee_prompt &p)
 CarvedPrompt carve(const lychee_prompt &p)
 {
     return carve(grid_of(p), p.n_kv_heads, (int64_t)p.n_tokens * p.n_q_heads,
-                 key_grid_of(p.batch, p.n_kv_heads, p.n_q_heads / p.n_kv_heads, p.n_tokens).slots);
+                 key_grid_of(p.batch, p.n_kv_heads, p.n_q_heads / p.n_kv_heads, p.n_tokens).ranges);
 }
 
 PromptRows rows_of(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_tokens, int32_t max_len, int64_t q_tok, int64_t q_head,
@@ -228,10 +220,8 @@ int lychee_prompt_attn_backward(lychee_ctx *ctx, const lychee_prompt *prompt, co
     a.n_row_tiles = (int32_t)grid_of(p.batch, p.n_kv_heads, a.r.group, p.n_tokens, 0).tiles;
     const KeyGrid w = key_grid_of(p.batch, p.n_kv_heads, a.r.group, p.n_tokens);
     a.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + c.part);
-    a.slots = kPromptKeySlots;
+    a.n_ranges = (int32_t)w.ranges;
     a.n_key_tiles = (int32_t)w.tiles;
-    a.n_key_items = (int32_t)w.items;
-    a.n_slots = (int32_t)w.slots;
     return done(launch_prompt_grad(a, static_cast<hipStream_t>(hip_stream)));
 }
 

@@ -228,59 +228,79 @@ __device__ __forceinline__ Tile find_tile(const PromptRows &p, int number, int s
     return w;
 }
 
-// The same for tiles of kPromptRows keys, which the rows from the tile's first key on see: blocks first .. last-1 of
-// kPromptKeys rows.  Tile k of a request with `end` blocks has end - 2 G k of them, and its pieces are numbered from
-// (what the tiles before it have) / size + k on, which leaves room for the last one of each.
+// Tiles of kPromptRows keys, which the rows from the tile's first key on see, as a line of blocks of kPromptKeys rows:
+// request after request and tile after tile.  Tile k of a request with `end` blocks of rows has end - 2 G k of them.  A
+// workgroup has a range of the line, all of the same size, whatever tiles it holds the parts of.
 __device__ __forceinline__ int64_t blocks_before(int64_t tile, int end, int group) { return tile * end - (int64_t)group * tile * (tile - 1); }
 
-template <bool MERGE>
-__device__ __forceinline__ Tile find_key_tile(const PromptRows &p, int number, int slots, SharedPlan &sh)
+struct SharedLine {
+    int32_t n[kMaxBatch], start[kMaxBatch];
+    int64_t before[kMaxBatch];  // blocks of the requests before
+    int64_t wave[kWaves];
+};
+struct Line {
+    int64_t all, size;  // blocks of the line, and of a range
+};
+__device__ __forceinline__ int64_t uniform64(int64_t x)
+{
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+}
+__device__ __forceinline__ Line lay_line(const PromptRows &p, int ranges, SharedLine &sh)
 {
     static_assert(kPromptRows == 2 * kPromptKeys, "");
-    const bool alone = p.batch == 1;
-    const int t = alone ? 0 : threadIdx.x;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     int start = 0, n = 0, len = 0;
     if (t < p.batch) request_of(p, t, start, n, len);
-    const int tiles = tiles_of(n);
-    const int64_t work = blocks_before(tiles, blocks_of(n * p.group), p.group);
-    unsigned long long all = (unsigned long long)work * (unsigned)p.n_kv_heads;
-    if (!alone) all = sum_all(all, sh);
-    const int size = __builtin_amdgcn_readfirstlane(max((int)min((all + slots - 1) / slots, 1ull << 30), kPromptMinRowPiece));
-    const int items = MERGE ? tiles : (int)(work / size) + tiles;
-    Found f;
-    if (alone) {
-        f = found_alone(number, items, start, n, len);
-    } else {
-        sh.n[t] = n;
-        sh.len[t] = n;
-        sh.start[t] = start;
-        // (tiles of several pieces are the first ones, fewer than work / size)
-        find_request(p.batch, number, n, items, 2 * (int)(work / size), sh);
-        f = found_among(sh);
+    const int64_t work = blocks_before(tiles_of(n), blocks_of(n * p.group), p.group);
+    int64_t upto = work;
+    if (p.batch > 1) {
+        for (int d = 1; d < 64; d <<= 1) {
+            const int64_t x = __shfl_up(upto, d);
+            upto += lane >= d ? x : 0;
+        }
+        if (lane == 63) sh.wave[wave] = upto;
+        __syncthreads();
+        for (int i = 0; i < wave; ++i) upto += sh.wave[i];
     }
-    Tile w;
-    w.b = f.b;
-    w.found = f.b >= 0;
-    if (!w.found) return w;
-    w.n = f.n;
-    w.len = f.n;
-    w.start = f.start;
-    const int end = blocks_of(w.n * p.group);
-    int tile = f.at;
-    if (!MERGE) {  // the last tile that begins at or before the piece
-        tile = 0;
-        for (int step = 1 << 17; step > 0; step >>= 1)
-            if (tile + step < tiles_of(w.n) && blocks_before(tile + step, end, p.group) / size + tile + step <= f.at) tile += step;
-    }
-    const int from = (int)(blocks_before(tile, end, p.group) / size) + tile;
-    w.tile = tile;
-    w.piece = MERGE ? 0 : f.at - from;
-    w.slot = f.before + from + w.piece;
-    const int first = 2 * p.group * tile;
-    w.parts = max(1, (end - first + size - 1) / size);
-    w.first = first + w.piece * size;
-    w.last = min(end, w.first + size);
-    return w;
+    sh.n[t] = n;
+    sh.start[t] = start;
+    sh.before[t] = upto - work;
+    __syncthreads();
+    Line l;
+    const int last = p.batch - 1, n_last = sh.n[last];
+    l.all = uniform64(sh.before[last] + blocks_before(tiles_of(n_last), blocks_of(n_last * p.group), p.group));
+    l.size = max((l.all + ranges - 1) / ranges, (int64_t)kPromptMinRowPiece);
+    return l;
+}
+
+struct KeyTile {
+    int n, start, tile;
+    int64_t at;       // of its first block on the line
+    int first, end;   // its blocks of rows
+};
+__device__ __forceinline__ KeyTile key_tile(const PromptRows &p, int b, int tile, int64_t before, const SharedLine &sh)
+{
+    KeyTile k;
+    k.n = __builtin_amdgcn_readfirstlane(sh.n[b]);
+    k.start = __builtin_amdgcn_readfirstlane(sh.start[b]);
+    k.end = blocks_of(k.n * p.group);
+    k.tile = tile;
+    k.first = 2 * p.group * tile;
+    k.at = before + blocks_before(tile, k.end, p.group);
+    return k;
+}
+// The tile that holds a block of the line.
+__device__ __forceinline__ KeyTile tile_at(const PromptRows &p, int64_t at, const SharedLine &sh)
+{
+    int b = 0;
+    for (int step = kMaxBatch / 2; step > 0; step >>= 1)
+        if (b + step < p.batch && uniform64(sh.before[b + step]) <= at) b += step;
+    const int64_t before = uniform64(sh.before[b]);
+    const int n = __builtin_amdgcn_readfirstlane(sh.n[b]), end = blocks_of(n * p.group), tiles = tiles_of(n);
+    int tile = 0;
+    for (int step = tiles > 1 ? 1 << (31 - __builtin_clz(tiles - 1)) : 0; step > 0; step >>= 1)
+        if (tile + step < tiles && blocks_before(tile + step, end, p.group) <= at - before) tile += step;
+    return key_tile(p, b, tile, before, sh);
 }
 
 // ------------------------------------------------------------------------------ LDS

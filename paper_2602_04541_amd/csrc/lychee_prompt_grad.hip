@@ -28,6 +28,7 @@ struct SharedGrad {
             __align__(16) uint8_t g[2][kGradBytes];
             __align__(16) float stat[2][2][kGradRows];  // of a block's rows: -lse sqrt(128), -delta
             __align__(16) bf16x8_t v[kWaves][8][64];
+            SharedLine line;
         } keys;
     };
 };
@@ -119,6 +120,12 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dq_kernel(PromptGradArgs a
                         z = mfma(read_rows(K, kat, x, ks), qf[ks], z);
                         dp = mfma(read_rows(V, kat, x, ks), gf[ks], dp);
                     }
+                    __builtin_amdgcn_sched_group_barrier(kGroupRead, 6, 0);  // (reads ahead of their products)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        __builtin_amdgcn_sched_group_barrier(kGroupMfma, 1, 0);
+                        if (i < 10) __builtin_amdgcn_sched_group_barrier(kGroupRead, 1, 0);
+                    }
 #pragma unroll
                     for (int i = 0; i < 16; ++i) z[i] = fast_exp2(z[i] * a.scale_log2e) * dp[i];
                     if (masked) {
@@ -140,6 +147,12 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dq_kernel(PromptGradArgs a
                     for (int s = 0; s < 2; ++s)
 #pragma unroll
                         for (int db = 0; db < 4; ++db) dq[db] = mfma(read_turned(K, vat, db, 2 * x + s), ds[s], dq[db]);
+                    __builtin_amdgcn_sched_group_barrier(kGroupRead, 6, 0);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        __builtin_amdgcn_sched_group_barrier(kGroupMfma, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(kGroupRead, 2, 0);
+                    }
                 }
             }
             wait_copies();
@@ -159,15 +172,19 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dkv_kernel(PromptGradArgs 
     __shared__ SharedGrad sh;
     const PromptRows &p = a.r;
     const int g = blockIdx.x % p.n_kv_heads;
-    const Tile w = find_key_tile<false>(p, blockIdx.x / p.n_kv_heads, a.slots, sh.plan);
-    if (!w.found || w.piece >= w.parts || (w.parts > 1 && w.slot >= a.n_slots)) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hi = lane >> 5;
+    const Line line = lay_line(p, a.n_ranges, sh.keys.line);
+    const int range = blockIdx.x / p.n_kv_heads;
+    int64_t at = range * line.size;
+    const int64_t until = min(at + line.size, line.all);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    while (at < until) {
+    const KeyTile w = tile_at(p, at, sh.keys.line);
+    const int block = w.first + (int)(at - w.at), block_end = (int)min((int64_t)w.end, block + (until - at));
     const int tile = w.tile, rows = w.n * p.group;
+    const int lane = (int)opaque(threadIdx.x & 63), hi = lane >> 5;
     const auto key_of = [&](uint32_t lane) { return tile * kPromptRows + wave * 32 + (int)(lane & 31); };
     const auto kv_of = [&](int key) { return (int64_t)(w.start + min(key, w.n - 1)) * a.kv_tok + (int64_t)g * a.kv_head; };
     const int64_t kv_at = kv_of(key_of(lane));
-    const int key_rows = key_of(lane) * p.group;  // rows from here on see the lane's key
-    __syncthreads();  // (the plan's part of LDS is free)
     bf16x8_t kf[8];
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) {
@@ -201,7 +218,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dkv_kernel(PromptGradArgs 
         wait_copies();
         __syncthreads();
     };
-    const int from = w.first * kPromptKeys, blocks = (min(w.last * kPromptKeys, rows) - from + kGradRows - 1) / kGradRows;
+    const int from = block * kPromptKeys, blocks = (min(block_end * kPromptKeys, rows) - from + kGradRows - 1) / kGradRows;
     const int wave_first = (tile * kPromptRows + wave * 32) * p.group;     // rows from here on see a key of the wavefront
     const int wave_all = (tile * kPromptRows + wave * 32 + 31) * p.group;  // and from here on all of them
 
@@ -248,9 +265,11 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dkv_kernel(PromptGradArgs 
                     z[i] = fast_exp2(z[i] * a.scale_log2e);
                     dp[i] *= z[i];
                 }
-                const int least = key_rows - r0, most = rows - 1 - r0;
+                const auto least_of = [&]() { return key_of(opaque(lane)) * p.group - r0; };  // rows that see the lane's key
+                const int most = rows - 1 - r0;
                 if (r0 < wave_all || r0 + kGradRows > rows) {
                     asm volatile("");
+                    const int least = least_of();
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int r = i % 4 + 8 * (i / 4) + 4 * hi;
@@ -267,7 +286,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dkv_kernel(PromptGradArgs 
                     __syncthreads();
                     if (turn % 3 != 0) {
 #pragma unroll
-                        for (int s = 0; s < 2; ++s) pf[s] = ds[s] = seen_rows(hi, s, least, most);
+                        for (int s = 0; s < 2; ++s) pf[s] = ds[s] = seen_rows(hi, s, least_of(), most);
                     }
                 }
 #pragma unroll
@@ -289,13 +308,15 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dkv_kernel(PromptGradArgs 
         if (careful || !__syncthreads_or(!all_finite(dk) || !all_finite(dv))) break;
         careful = true;
     }
-    if (w.parts == 1) {
+    if (block == w.first && block_end == w.end) {
         const int key = key_of(opaque(lane));
         const int64_t to = kv_of(key);
         store_row(key < w.n ? a.dk + to : nullptr, lane, dk, a.scale);
         store_row(key < w.n ? a.dv + to : nullptr, lane, dv, 1.f);
     } else {
-        float *to = a.part + (((int64_t)w.slot * p.n_kv_heads + g) * kWaves + wave) * kPartFloats + 4 * lane;
+        // (of the two partials a range can leave the second is that of a tile's first blocks)
+        const int64_t slot = ((int64_t)range * 2 + (block == w.first)) * p.n_kv_heads + g;
+        float *to = a.part + (slot * kWaves + wave) * kPartFloats + 4 * lane;
 #pragma unroll
         for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -304,26 +325,41 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dkv_kernel(PromptGradArgs 
                 *(LYCHEE_GLOBAL f32x4_t *)(to + (16 + 4 * db + j) * 256) = f32x4_t{dv[db][4 * j], dv[db][4 * j + 1], dv[db][4 * j + 2], dv[db][4 * j + 3]};
             }
     }
+    at += block_end - block;
+    }
 }
 
-// The sums of tiles with several pieces, piece after piece: a workgroup has 32 keys, a wavefront every fourth group of four
-// dimensions, a lane four of a key.
+// The sums of tiles that lie in several ranges, range after range: a workgroup has 32 keys, a wavefront every fourth group of
+// eight dimensions, a lane four of a key.
 __global__ __launch_bounds__(kThreads) void prompt_dkv_merge_kernel(PromptGradArgs a)
 {
-    __shared__ SharedPlan sh;
+    __shared__ SharedLine sh;
+    __shared__ SharedPlan plan;
     const PromptRows &p = a.r;
-    const int keys32 = blockIdx.x % kWaves, g = blockIdx.x / kWaves % p.n_kv_heads;
-    const Tile w = find_key_tile<true>(p, blockIdx.x / kWaves / p.n_kv_heads, a.slots, sh);
-    if (!w.found || w.parts == 1 || w.slot + w.parts > a.n_slots) return;
+    const int keys32 = blockIdx.x % kWaves, g = blockIdx.x / kWaves % p.n_kv_heads, number = blockIdx.x / kWaves / p.n_kv_heads;
+    const Line line = lay_line(p, a.n_ranges, sh);
+    int b = number < tiles_of(sh.n[0]) ? 0 : -1, tile = number;
+    if (p.batch > 1) {
+        const int t = threadIdx.x;
+        find_request(p.batch, number, 0, t < p.batch ? tiles_of(sh.n[t]) : 0, 0, plan);
+        b = plan.found[0];
+        tile = plan.found[1];
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
+    if (b < 0) return;
+    const KeyTile w = key_tile(p, b, __builtin_amdgcn_readfirstlane(tile), uniform64(sh.before[b]), sh);
+    const int first = (int)(w.at / line.size), last = (int)((w.at + (w.end - w.first) - 1) / line.size);
+    if (first == last || last >= a.n_ranges) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, key = w.tile * kPromptRows + keys32 * 32 + (lane & 31);
-    const float *from = a.part + (((int64_t)w.slot * p.n_kv_heads + g) * kWaves + keys32) * kPartFloats + 4 * lane;
-    const int64_t apart = (int64_t)p.n_kv_heads * kWaves * kPartFloats;
+    const auto part_of = [&](int range, int second) {
+        return a.part + ((((int64_t)range * 2 + second) * p.n_kv_heads + g) * kWaves + keys32) * kPartFloats + 4 * lane;
+    };
     f32x4_t sum[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum[i] = *(const LYCHEE_GLOBAL f32x4_t *)(from + (4 * i + wave) * 256);
-    for (int q = 1; q < w.parts; ++q) {
+    for (int i = 0; i < 8; ++i) sum[i] = *(const LYCHEE_GLOBAL f32x4_t *)(part_of(first, 1) + (4 * i + wave) * 256);
+    for (int q = first + 1; q <= last; ++q) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] += *(const LYCHEE_GLOBAL f32x4_t *)(from + q * apart + (4 * i + wave) * 256);
+        for (int i = 0; i < 8; ++i) sum[i] += *(const LYCHEE_GLOBAL f32x4_t *)(part_of(q, 0) + (4 * i + wave) * 256);
     }
     if (key >= w.n) return;
     const int64_t to = (int64_t)(w.start + key) * a.kv_tok + (int64_t)g * a.kv_head + 4 * (lane >> 5);
@@ -343,7 +379,7 @@ hipError_t launch_prompt_grad(const PromptGradArgs &a, hipStream_t stream)
     prompt_dq_kernel<<<(unsigned)a.n_row_tiles * heads, kThreads, 0, stream>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    prompt_dkv_kernel<<<(unsigned)a.n_key_items * heads, kThreads, 0, stream>>>(a);
+    prompt_dkv_kernel<<<(unsigned)a.n_ranges * heads, kThreads, 0, stream>>>(a);
     prompt_dkv_merge_kernel<<<(unsigned)a.n_key_tiles * heads * kWaves, kThreads, 0, stream>>>(a);
     return hipGetLastError();
 }
