@@ -9,8 +9,13 @@ namespace lychee {
 constexpr int kPromptMaxGroup = 16;
 constexpr int kPromptRows = 128;          // query rows of a tile, a row being a (token, query head of the KV head)
 constexpr int kPromptKeys = 64;           // keys a workgroup takes at a time
-constexpr int kPromptMinPiece = 4;        // blocks of keys in a piece of a split tile, at least
-constexpr int kPromptMinRowPiece = 2;     // and blocks of rows in a range of tiles of keys
+constexpr int kPromptMinRange = 3;        // blocks in a range of row tiles, at least,
+constexpr int kPromptMinKeyRange = 2;     //   and of key tiles
+// Rows' tiles are shared out where the longest has kPromptShareCost blocks more than kPromptShareSize times a range's (tiles_to_share).
+constexpr int kPromptShareCost = 14;
+constexpr float kPromptShareSize = 1.6f;
+constexpr int kPromptTileCost = 3;        // blocks that a row tile takes besides its own
+constexpr int kRecordWords = 8;           // of a tile that several ranges share
 constexpr int64_t kPromptMaxRows = 1 << 28;  // query tokens times heads of a group (row numbers are divided with a multiplication)
 constexpr int64_t kPromptMaxStride = 1 << 24;  // elements from a token's row to the next (offsets within 64 rows fit 32 bits)
 
@@ -33,11 +38,14 @@ struct PromptArgs {
     PagedDims d;
     uint16_t *out;      // [n_tokens][n_q_heads][128]
     float *lse;         // [n_q_heads][n_tokens] or nullptr
-    float *part_o;      // [piece][wavefront][16][64][4] un-normalised partial outputs, as registers and lanes hold them
-    float *part_ml;     // [piece][kPromptRows][2]       maximum (log2 units) and sum
-    int32_t slots;      // 0: tiles are not split; else the pieces that fill the device
+    float *part_o;      // [range][2][KV head][wavefront][16][64][4] un-normalised partial outputs, as registers and lanes hold them
+    float *part_ml;     // [range][2][KV head][kPromptRows][2]       maximum (log2 units) and sum
+    int32_t *records;   // [n_records][kRecordWords], by tile or by range
+    int32_t n_records, by_number;
+    double one_range;   // 1 / n_ranges
+    int32_t n_ranges;   // 0: a workgroup a tile; else the workgroups that share a KV head's tiles
+    int32_t n_tiles;    // of a KV head, at most
     int32_t merge_split;  // workgroups that share 32 rows of a tile in the merge
-    int32_t n_items, n_tiles, n_slots;  // pieces, tiles and partials of a KV head that the launch has room for
     float scale_log2e;
 };
 
@@ -49,10 +57,13 @@ struct PromptGradArgs {
     uint16_t *dq, *dk, *dv;  // strided like q, k and v
     float *stat;             // [2][n_q_heads][n_tokens] -lse sqrt(128), -(g . out): what the products of the second launch begin with
     float scale, scale_log2e, root;  // 1 / sqrt(128), log2(e) / sqrt(128), sqrt(128)
-    float *part;             // [range][2][KV head][wavefront][dk, dv][16][64][4] sums over a part of a tile's rows, as registers
-                             // and lanes hold them
-    int32_t n_ranges;        // workgroups of the second launch that share a KV head's tiles of keys
-    int32_t n_row_tiles, n_key_tiles;  // of a KV head, at most
+    float *part;             // partials of dq: [range][2][KV head][wavefront][16][64][4]; of dk and dv: twice as many in a wavefront
+    int32_t *records;        // [n_records][kRecordWords], by tile or by range, of one launch after the other
+    int32_t n_row_records, rows_by_number, n_key_records, keys_by_number;
+    double one_row_range, one_key_range;
+    int32_t n_row_ranges;    // 0: a workgroup a tile of rows; else those that share a KV head's
+    int32_t n_key_ranges;    // workgroups that share a KV head's tiles of keys
+    int32_t n_row_tiles;     // of a KV head, at most
 };
 
 hipError_t launch_prompt(const PromptArgs &a, hipStream_t stream);

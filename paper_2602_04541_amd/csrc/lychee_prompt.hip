@@ -12,247 +12,285 @@
 // product O^T = V^T P^T as they stand.
 #include "lychee_prompt_device.h"
 
+#include <type_traits>
+
 namespace lychee {
 namespace {
 
-constexpr int kAhead = 2;        // of the four steps of the second product those whose values are read before the softmax
+// Reads of keys ahead of their products (four, six and eight are as fast).  Of values eight are read before the weights are made, six of
+// a 4-bit cache, whose next block is written into LDS between the last products: 6.69 ms for two pieces of 4096 tokens behind 64 K
+// (7.00 with the block written behind them).
+constexpr int kAhead = 6;
 constexpr float kSlack = 8.f;    // powers of two by which a score may exceed the maximum that weights are measured against
 
 struct SharedPrompt {
     __align__(16) uint8_t k[2][kBlockBytes];
     __align__(16) uint8_t v[2][kBlockBytes];
     __align__(8) uint16_t bad[2][kWaves];  // of a block's keys those whose page is not there, a bit each
-    SharedPlan plan;
+    int said[kWaves];                      // (any_thread)
+    union {
+        SharedPlan plan;
+        SharedLine line;
+    };
 };
 
-template <bool Q4>
+template <bool Q4, bool SHARE>
 __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
 {
     __shared__ SharedPrompt sh;
+    constexpr int kAheadValues = Q4 ? 6 : 8;
     const PromptRows &p = a.r;
     const int g = blockIdx.x % p.n_kv_heads;
-    const Tile w = find_tile<false>(p, blockIdx.x / p.n_kv_heads, a.slots, sh.plan);
-    if (!w.found || (w.piece > 0 && w.first >= w.last) || (w.parts > 1 && w.slot >= a.n_slots)) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hi = lane >> 5;
-    const int rows = w.n * p.group, row = w.tile * kPromptRows + wave * 32 + (lane & 31);
-    const int row_in = min(row, rows - 1), token = token_of(p, row_in), head = g * p.group + row_in - token * p.group;
-    const int pos = w.len - w.n + token;  // keys 0 .. pos are seen
-    const int lowest = w.len - w.n + token_of(p, min(w.tile * kPromptRows + wave * 32, rows - 1));  // of the wavefront's rows
-    const int highest = w.len - w.n + token_of(p, min(w.tile * kPromptRows + wave * 32 + 31, rows - 1));
-
-    bf16x8_t qf[8];
-    {
-        const uint16_t *q = a.q + (int64_t)(w.start + token) * p.q_tok + (int64_t)head * p.q_head + 8 * hi;
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks) qf[ks] = *(const LYCHEE_GLOBAL bf16x8_t *)(q + 16 * ks);
+    Tile w;
+    Line line;
+    bool share = false;
+    int64_t at = 0, until = 0, slot = -1;
+    const int range = blockIdx.x / p.n_kv_heads;
+    if (SHARE) {
+        line = lay_line<kLineRows>(p, a.one_range, sh.line);
+        share = line.share;
+        at = range * line.size;
+        until = share ? min(at + line.size, line.all) : 0;
+        if (g == 0) clear_records(a.records, a.n_records, a.by_number, line, range);
+        if (share && at >= until) return;
     }
-    const uint32_t row_at = row_place(lane), turn_at = turn_place(lane);
-
-    // bf16: copies go to LDS as they are, 16 rows of either operand a step, four a wavefront.
-    const int64_t base = p.lengths ? (int64_t)w.b * a.kv_batch : (int64_t)w.start * a.kv_tok;
-    const uint16_t *kb = a.k + base + (int64_t)g * a.kv_head, *vb = a.v + base + (int64_t)g * a.kv_head;
-    const uint32_t to_k = lds_address(sh.k) + wave * 4 * kRowBytes, to_v = lds_address(sh.v) + wave * 4 * kRowBytes;
-    const int fetch_row = 4 * wave + (lane >> 4);
-    const uint32_t fetch_chunk = (uint32_t)((lane & 15) ^ swizzle(fetch_row)) << 4;  // (the same for rows 16 apart)
-    const uint32_t fetch_at = (uint32_t)fetch_row * (uint32_t)(2 * a.kv_tok) + fetch_chunk;
-    // 4 bits: a thread takes a quarter (one scale's dimensions) of a token's key and of its value, and writes their bf16 numbers.
-    // (16 lanes the same quarter of 16 tokens, whose rows lie in 16 places)
-    const int token4 = wave * 16 + (lane & 15), part4 = lane >> 4;
-    uint4 code_k = make_uint4(0, 0, 0, 0), code_v = code_k;
-    uint32_t scale_k = 0, scale_v = 0;
-    int entry = -1;  // of the block table, for the block that is loaded next
-    const auto fetch_entry = [&](int blk) {
-        const int t = min(blk * kPromptKeys + token4, w.len - 1);
-        return gload(a.table + (int64_t)w.b * a.d.table_stride + (t >> a.d.page_shift));
-    };
-    const auto load4 = [&](int blk) {
-        const int t = blk * kPromptKeys + token4, off = t & ((1 << a.d.page_shift) - 1), sub = off & (kTileTokens - 1);
-        const bool ok = t < w.len && (uint32_t)entry < (uint32_t)a.d.n_pages;
-        const uint8_t *tile = a.cache + ((int64_t)(ok ? entry : 0) * a.d.page_tiles + (int64_t)g * ((1 << a.d.page_shift) / kTileTokens) +
-                                         off / kTileTokens) * kTileBytes;
-        const u32x4_t k = *(const LYCHEE_GLOBAL u32x4_t *)(tile + sub * kTokenBytes + 16 * part4);
-        const u32x4_t v = *(const LYCHEE_GLOBAL u32x4_t *)(tile + sub * kTokenBytes + 64 + 16 * part4);
-        const uint32_t ks = gload(tile + kTileScales + part4 * kTileTokens + sub), vs = gload(tile + kTileScales + (4 + part4) * kTileTokens + sub);
-        code_k = make_uint4(k[0], k[1], k[2], k[3]);
-        code_v = make_uint4(v[0], v[1], v[2], v[3]);
-        scale_k = ok ? ks << 23 : 0u;  // (a scale of 0 makes numbers that are no NaN: a weight of 0 times NaN is NaN)
-        scale_v = ok ? vs << 23 : 0u;
-        return __ballot(ok);
-    };
-    const auto store4 = [&](uint8_t *block, uint4 code, uint32_t scale) {
-        const float f = __builtin_bit_cast(float, scale);
-        const uint32_t c4[4] = {code.x, code.y, code.z, code.w};
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-            *reinterpret_cast<uint4 *>(block + token4 * kRowBytes + (((4 * part4 + c) ^ swizzle(token4)) << 4)) = decode8(c4[c], f);
-    };
-    uint32_t offset[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) offset[i] = fetch_at + (uint32_t)i * 32u * (uint32_t)a.kv_tok;
-    const auto copy_rows = [&](const uint16_t *from, int blk, uint32_t to) {
-        const uint16_t *at = from + (int64_t)(blk * kPromptKeys) * a.kv_tok;
-        const int left = w.len - 1 - blk * kPromptKeys;
-        if (left >= kPromptKeys - 1) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) copy16(at, offset[i], to + i * 16 * kRowBytes);
-        } else {  // the last key again in the rows behind it
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                copy16(at, (uint32_t)min(fetch_row + 16 * i, left) * (uint32_t)(2 * a.kv_tok) + fetch_chunk, to + i * 16 * kRowBytes);
+    if (!share) {
+        if (SHARE) __syncthreads();
+        w = find_tile(p, range, sh.plan);
+        if (!w.found) return;
+    }
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    do {
+        if (share) {
+            const LineTile k = line_tile_at<kLineRows>(p, at, line, sh.line);
+            w = Tile{k.b, k.tile, k.n, k.len, k.start, 0, blocks_seen(p, k.tile, k.n, k.len), true};
+            const int64_t from = at - k.at, to = min(opaque64(until) - k.at, k.weight);
+            const int blocks = w.last;
+            w.first = cut_at(from, k.weight, blocks);
+            w.last = cut_at(to, k.weight, blocks);
+            slot = from == 0 && to == k.weight ? -1 : part_slot(range, from == 0, p.n_kv_heads, g);
+            if (from == 0 && g == 0) record_tile(a.records, a.n_records, a.by_number, line, k, range, to == k.weight);
+            at += to - from;
         }
-    };
+        const int lane = (int)opaque(threadIdx.x & 63), hi = lane >> 5;
+        const int rows = w.n * p.group, row = w.tile * kPromptRows + wave * 32 + (lane & 31);
+        const int row_in = min(row, rows - 1), token = token_of(p, row_in), head = g * p.group + row_in - token * p.group;
+        const int pos = w.len - w.n + token;  // keys 0 .. pos are seen
+        const int lowest = w.len - w.n + token_of(p, min(w.tile * kPromptRows + wave * 32, rows - 1));  // of the wavefront's rows
+        const int highest = w.len - w.n + token_of(p, min(w.tile * kPromptRows + wave * 32 + 31, rows - 1));
 
-    f32x16_t o[4];
-    float m, l;
-    bool careful = false;
-    for (;;) {
-        // Turns: a block each (with care three of them, take_with_care).
-        const int turns = (careful ? 3 : 1) * max(w.last - w.first, 0);
-        const auto block_of = [&](int turn) { return w.first + (careful ? turn / 3 : turn); };
-        const auto fetch = [&](int turn) {
-            const int blk = block_of(turn);
-            if constexpr (Q4) {
-                const uint64_t there = load4(blk);
-                if (lane == 0) sh.bad[turn & 1][wave] = (uint16_t)~there;
-                entry = fetch_entry(block_of(min(turn + 1, turns - 1)));
-            } else {
-                copy_rows(kb, blk, to_k + (turn & 1) * kBlockBytes);
-                copy_rows(vb, blk, to_v + (turn & 1) * kBlockBytes);
+        bf16x8_t qf[8];
+        {
+            const uint16_t *q = a.q + (int64_t)(w.start + token) * p.q_tok + (int64_t)head * p.q_head + 8 * hi;
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) qf[ks] = *(const LYCHEE_GLOBAL bf16x8_t *)(q + 16 * ks);
+        }
+        const uint32_t row_at = row_place(lane), turn_at = turn_place(lane);
+
+        // bf16: copies go to LDS as they are, 16 rows of either operand a step, four a wavefront.
+        const int64_t base = p.lengths ? (int64_t)w.b * a.kv_batch : (int64_t)w.start * a.kv_tok;
+        const uint16_t *kb = a.k + base + (int64_t)g * a.kv_head, *vb = a.v + base + (int64_t)g * a.kv_head;
+        const uint32_t to_k = lds_address(sh.k) + wave * 4 * kRowBytes, to_v = lds_address(sh.v) + wave * 4 * kRowBytes;
+        const int fetch_row = 4 * wave + (lane >> 4);
+        const uint32_t fetch_chunk = (uint32_t)((lane & 15) ^ swizzle(fetch_row)) << 4;  // (the same for rows 16 apart)
+        const uint32_t fetch_at = (uint32_t)fetch_row * (uint32_t)(2 * a.kv_tok) + fetch_chunk;
+        uint32_t offset[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) offset[i] = fetch_at + (uint32_t)i * 32u * (uint32_t)a.kv_tok;
+        const auto copy_rows = [&](const uint16_t *from, int blk, uint32_t to) {
+            const uint16_t *at = from + (int64_t)(blk * kPromptKeys) * a.kv_tok;
+            const int left = w.len - 1 - blk * kPromptKeys;
+            if (left >= kPromptKeys - 1) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) copy16(at, offset[i], to + i * 16 * kRowBytes);
+            } else {  // the last key again in the rows behind it
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    copy16(at, (uint32_t)min(fetch_row + 16 * i, left) * (uint32_t)(2 * a.kv_tok) + fetch_chunk, to + i * 16 * kRowBytes);
             }
         };
-        const auto arrive = [&](int turn) {
-            if constexpr (Q4) {
-                store4(sh.k[turn & 1], code_k, scale_k);
-                store4(sh.v[turn & 1], code_v, scale_v);
-            } else {
-                wait_copies();
-            }
-            __syncthreads();
+        // 4 bits: a wavefront takes a tile of 16 tokens of every block, a lane a quarter (one scale's dimensions) of a token's key and of its
+        // value, whose bf16 numbers it writes.  (16 lanes the same quarter of 16 tokens, whose rows lie in 16 places)
+        const int sub4 = lane & 15, part4 = lane >> 4;
+        const uint32_t row4 = (uint32_t)(sub4 * kTokenBytes + 16 * part4), scale4 = (uint32_t)(kTileScales + part4 * kTileTokens + sub4);
+        const uint32_t store_at = (uint32_t)((wave * 16 + sub4) * kRowBytes + (((4 * part4) ^ swizzle(sub4)) << 4));
+        uint4 code_k = make_uint4(0, 0, 0, 0), code_v = code_k;
+        uint32_t scale_k = 0, scale_v = 0;
+        int entry = -1;  // of the block table, for the block that is loaded next
+        const auto fetch_entry = [&](int blk) {
+            return gload(a.table + (int64_t)w.b * a.d.table_stride + (min(blk * kPromptKeys + wave * kTileTokens, w.len - 1) >> a.d.page_shift));
         };
+        const auto load4 = [&](int blk) {  // (whether the tile's page is there)
+            const int page = __builtin_amdgcn_readfirstlane(entry), tiles = 1 << (a.d.page_shift - 4);
+            const bool there = (uint32_t)page < (uint32_t)a.d.n_pages;
+            const uint8_t *tile = uniform(a.cache + ((int64_t)(there ? page : 0) * a.d.page_tiles + (int64_t)g * tiles + ((blk * 4 + wave) & (tiles - 1))) * kTileBytes);
+            const u32x4_t k = *(const LYCHEE_GLOBAL u32x4_t *)((const LYCHEE_GLOBAL uint8_t *)tile + row4);
+            const u32x4_t v = *(const LYCHEE_GLOBAL u32x4_t *)((const LYCHEE_GLOBAL uint8_t *)tile + 64 + row4);
+            const uint32_t ks = *((const LYCHEE_GLOBAL uint8_t *)tile + scale4), vs = *((const LYCHEE_GLOBAL uint8_t *)tile + 4 * kTileTokens + scale4);
+            code_k = make_uint4(k[0], k[1], k[2], k[3]);
+            code_v = make_uint4(v[0], v[1], v[2], v[3]);
+            const bool ok = there && blk * kPromptKeys + wave * kTileTokens + sub4 < w.len;
+            scale_k = ok ? ks << 23 : 0u;  // (a scale of 0 makes numbers that are no NaN: a weight of 0 times NaN is NaN)
+            scale_v = ok ? vs << 23 : 0u;
+            return there;
+        };
+        const auto store4 = [&](uint8_t *block, uint4 code, uint32_t scale) {
+            const float f = __builtin_bit_cast(float, scale);
+            const uint32_t c4[4] = {code.x, code.y, code.z, code.w};
 #pragma unroll
-        for (int db = 0; db < 4; ++db) o[db] = zero16();
-        m = -__builtin_inff();
-        l = 0.f;
-        if (turns > 0) {
-            if (Q4) entry = fetch_entry(w.first);
-            fetch(0);
-            arrive(0);
-        }
-        for (int turn = 0; turn < turns; ++turn) {
-            const int j0 = block_of(turn) * kPromptKeys;
-            if (turn + 1 < turns) fetch(turn + 1);
-            if (careful || j0 <= highest) {
-                const LYCHEE_LDS uint8_t *K = (const LYCHEE_LDS uint8_t *)sh.k[turn & 1], *V = (const LYCHEE_LDS uint8_t *)sh.v[turn & 1];
-                const uint32_t kat = opaque(row_at), vat = opaque(turn_at);
-                f32x16_t z[2] = {zero16(), zero16()};
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks)
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) z[x] = mfma(read_rows(K, kat, x, ks), qf[ks], z[x]);
-                // (eight reads ahead of the products that need them)
-                __builtin_amdgcn_sched_group_barrier(kGroupRead, 8, 0);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    __builtin_amdgcn_sched_group_barrier(kGroupMfma, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(kGroupRead, 1, 0);
+            for (int c = 0; c < 4; ++c) *reinterpret_cast<uint4 *>(block + (store_at ^ (uint32_t)(c << 4))) = decode8(c4[c], f);
+        };
+        f32x16_t o[4];
+        float m, l;
+        bool careful = false;
+        for (;;) {
+            // Turns: a block each (with care three of them, take_with_care).
+            const int turns = (careful ? 3 : 1) * max(w.last - w.first, 0);
+            const auto block_of = [&](int turn) { return w.first + (careful ? turn / 3 : turn); };
+            const auto fetch = [&](int turn) {
+                const int blk = block_of(turn);
+                if constexpr (Q4) {
+                    const bool there = load4(blk);
+                    if (lane == 0) sh.bad[turn & 1][wave] = there ? 0 : 0xFFFF;
+                    entry = fetch_entry(block_of(min(turn + 1, turns - 1)));
+                } else {
+                    copy_rows(kb, blk, to_k + (turn & 1) * kBlockBytes);
+                    copy_rows(vb, blk, to_v + (turn & 1) * kBlockBytes);
                 }
-                __builtin_amdgcn_sched_group_barrier(kGroupMfma, 8, 0);
-                bf16x8_t vf[kAhead][4];  // values of the first steps, on their way while the weights are made
+            };
+            const auto store_k = [&](int turn) { if constexpr (Q4) store4(sh.k[turn & 1], code_k, scale_k); };
+            const auto store_v = [&](int turn) { if constexpr (Q4) store4(sh.v[turn & 1], code_v, scale_v); };
+            const auto arrive = [&]() {
+                if constexpr (!Q4) wait_copies();
+                __syncthreads();
+            };
 #pragma unroll
-                for (int s = 0; s < kAhead; ++s)
-#pragma unroll
-                    for (int db = 0; db < 4; ++db) vf[s][db] = read_turned(V, vat, db, s);
-                uint64_t bad = 0;  // keys whose page is not there
-                if (Q4) {
-                    const uint2 words = *reinterpret_cast<const uint2 *>(sh.bad[turn & 1]);
-                    bad = (uint64_t)__builtin_amdgcn_readfirstlane(words.y) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane(words.x);
-                }
-                if (j0 + kPromptKeys - 1 > lowest || bad != 0) {
-                    asm volatile("");  // (a branch: these are many instructions, and rare)
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const int n = min(max(pos - j0 - 32 * x + 1, 0), 32);
-                        uint32_t seen = n == 32 ? ~0u : (1u << n) - 1u;
-                        if (Q4) seen &= ~(uint32_t)(bad >> (32 * x));
-                        seen >>= 4 * hi;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) z[x][i] = seen >> (i % 4 + 8 * (i / 4)) & 1u ? z[x][i] : -__builtin_inff();
+            for (int db = 0; db < 4; ++db) o[db] = zero16();
+            m = -__builtin_inff();
+            l = 0.f;
+            if (turns > 0) {
+                if (Q4) entry = fetch_entry(w.first);
+                fetch(0);
+            }
+            arrived(qf);
+            if (turns > 0) {
+                store_k(0);
+                store_v(0);
+                arrive();
+            }
+            for (int turn = 0; turn < turns; ++turn) {
+                const int j0 = block_of(turn) * kPromptKeys;
+                if (turn + 1 < turns) fetch(turn + 1);
+                if (careful || j0 <= highest) {
+                    const LYCHEE_LDS uint8_t *K = (const LYCHEE_LDS uint8_t *)sh.k[turn & 1], *V = (const LYCHEE_LDS uint8_t *)sh.v[turn & 1];
+                    const uint32_t kat = opaque(row_at), vat = opaque(turn_at);
+                    const bool again = careful && turn % 3 != 0;
+                    if (__builtin_expect(careful, 0)) {
+                        take_with_care(sh.v[turn & 1], kBlockBytes, turn % 3);
+                        __syncthreads();
                     }
-                }
-                float top = z[0][0];
+                    f32x16_t z[2] = {zero16(), zero16()};
+                    bf16x8_t kf[kAhead], vf[kAheadValues];  // read ahead of their products; the first values are on their way while the weights are made
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) top = fmaxf(top, z[x][i]);
-                top = max_halves32(top) * a.scale_log2e;
-                // m is some maximum of late: weights of up to 2^kSlack are as exact as others, and a new maximum costs 65 products.  (By
-                // the row's own scores alone, so that no row's bits depend on another's.)
-                if (__ballot(top > m + kSlack) != 0) {
-                    asm volatile("");
-                    const float up = top > m + kSlack ? top : m;
-                    const float f = m == up ? 1.0f : fast_exp2(m - up);
-                    m = up;
-                    l *= f;
-#pragma unroll
-                    for (int db = 0; db < 4; ++db)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[db][i] *= f;
-                }
-                const float ref = m == -__builtin_inff() ? 0.f : m, before = l;
-                float part[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
+                    for (int i = 0; i < kAhead; ++i) kf[i] = read_rows(K, kat, i % 2, i / 2);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        z[x][i] = fast_exp2(__builtin_fmaf(z[x][i], a.scale_log2e, -ref));
-                        part[i % 4] += z[x][i];
+                        in_order();
+                        z[i % 2] = mfma(kf[i % kAhead], qf[i / 2], z[i % 2]);
+                        if (i + kAhead < 16) kf[i % kAhead] = read_rows(K, kat, (i + kAhead) % 2, (i + kAhead) / 2);
+                        const int early = i - (16 - kAheadValues);
+                        if (early >= 0) vf[early] = read_turned(V, vat, early % 4, early / 4);
                     }
-                l += (part[0] + part[1]) + (part[2] + part[3]);
-                bf16x8_t pf[4] = {operand<0>(z[0]), operand<8>(z[0]), operand<0>(z[1]), operand<8>(z[1])};
-                if (__builtin_expect(careful, 0)) {
-                    __syncthreads();
-                    take_with_care(sh.v[turn & 1], kBlockBytes, turn % 3);
-                    __syncthreads();
-                    if (turn % 3 != 0) {
-                        l = before;
+                    in_order();
+                    uint64_t bad = 0;  // keys whose page is not there
+                    if (Q4) {
+                        const uint2 words = *reinterpret_cast<const uint2 *>(sh.bad[turn & 1]);
+                        bad = (uint64_t)__builtin_amdgcn_readfirstlane(words.y) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane(words.x);
+                    }
+                    if (j0 + kPromptKeys - 1 > lowest || bad != 0) {
+                        asm volatile("");  // (a branch: these are many instructions, and rare)
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const int n = min(max(pos - j0 - 32 * x + 1, 0), 32);
+                            uint32_t seen = n == 32 ? ~0u : (1u << n) - 1u;
+                            if (Q4) seen &= ~(uint32_t)(bad >> (32 * x));
+                            seen >>= 4 * hi;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) z[x][i] = seen >> (i % 4 + 8 * (i / 4)) & 1u ? z[x][i] : -__builtin_inff();
+                        }
+                    }
+                    float top = z[0][0];
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) top = fmaxf(top, z[x][i]);
+                    top = max_halves32(top) * a.scale_log2e;
+                    // m is some maximum of late: weights of up to 2^kSlack are as exact as others, and a new maximum costs 65 products.  (By
+                    // the row's own scores alone, so that no row's bits depend on another's.)
+                    if (__ballot(top > m + kSlack) != 0) {
+                        asm volatile("");
+                        const float up = top > m + kSlack ? top : m;
+                        const float f = m == up ? 1.0f : fast_exp2(m - up);
+                        m = up;
+                        l *= f;
+#pragma unroll
+                        for (int db = 0; db < 4; ++db)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[db][i] *= f;
+                    }
+                    const float ref = m == -__builtin_inff() ? 0.f : m;
+                    float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            z[x][i] = fast_exp2(__builtin_fmaf(z[x][i], a.scale_log2e, -ref));
+                            part[i % 4] += z[x][i];
+                        }
+                    bf16x8_t pf[4] = {operand<0>(z[0]), operand<8>(z[0]), operand<0>(z[1]), operand<8>(z[1])};
+                    if (__builtin_expect(again, 0)) {
 #pragma unroll
                         for (int s = 0; s < 4; ++s) pf[s] = seen_rows(hi, s, 0, pos - j0);
                     }
 #pragma unroll
-                    for (int s = 0; s < kAhead; ++s)
-#pragma unroll
-                        for (int db = 0; db < 4; ++db) vf[s][db] = read_turned(V, vat, db, s);
+                    for (int i = 0; i < 16; ++i) {
+                        in_order();
+                        o[i % 4] = mfma(vf[i % kAheadValues], pf[i / 4], o[i % 4]);
+                        if (i + kAheadValues < 16) vf[i % kAheadValues] = read_turned(V, vat, (i + kAheadValues) % 4, (i + kAheadValues) / 4);
+                        if (i == 10) store_k(turn + 1);  // (the next block's numbers while the products go on)
+                        if (i == 14) store_v(turn + 1);
+                    }
+                    l += again ? 0.f : (part[0] + part[1]) + (part[2] + part[3]);
+                } else {
+                    store_k(turn + 1);
+                    store_v(turn + 1);
                 }
-#pragma unroll
-                for (int s = 0; s < 4; ++s)
-#pragma unroll
-                    for (int db = 0; db < 4; ++db) o[db] = mfma(s < kAhead ? vf[s][db] : read_turned(V, vat, db, s), pf[s], o[db]);
+                arrive();
             }
-            arrive(turn + 1);
+            // A key's value counts for the rows that see it alone, but a weight of zero times an infinite value or NaN is NaN: a
+            // tile in which that may have happened is done again, with care.
+            if (careful || !any_thread(!all_finite(o), wave, sh.said)) break;
+            careful = true;
         }
-        // A key's value counts for the rows that see it alone, but a weight of zero times an infinite value or NaN is NaN: a
-        // tile in which that may have happened is done again, with care.
-        if (careful || !__syncthreads_or(!all_finite(o))) break;
-        careful = true;
-    }
-    l = sum_halves32(l);
-    if (w.parts == 1) {
-        const bool there = row < rows;
-        uint16_t *out = a.out + ((int64_t)(w.start + token) * (p.n_kv_heads * p.group) + head) * kHeadDim;
-        store_row(there ? out : nullptr, lane, o, l == 0.f ? 0.f : 1.f / l);
-        if (a.lse && there && hi == 0)
-            gstore(a.lse + (int64_t)head * p.n_tokens + w.start + token, l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * (1.f / kLog2e));
-    } else {
-        // in the order of the registers: 1 KB a store, read back alike
-        const int64_t at = ((int64_t)w.slot * p.n_kv_heads + g) * kWaves + wave;
-        float *po = a.part_o + at * (64 * 64) + 4 * lane;
+        l = sum_halves32(l);
+        if (slot < 0) {
+            const bool there = row < rows;
+            uint16_t *out = a.out + ((int64_t)(w.start + token) * (p.n_kv_heads * p.group) + head) * kHeadDim;
+            store_row(there ? out : nullptr, lane, o, l == 0.f ? 0.f : 1.f / l);
+            if (a.lse && there && hi == 0)
+                gstore(a.lse + (int64_t)head * p.n_tokens + w.start + token, l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * (1.f / kLog2e));
+        } else if (w.tile * kPromptRows + wave * 32 < rows) {
+            // in the order of the registers: 1 KB a store, read back alike
+            const int64_t part = slot * kWaves + wave;
+            float *po = a.part_o + part * (64 * 64) + 4 * lane;
 #pragma unroll
-        for (int db = 0; db < 4; ++db)
+            for (int db = 0; db < 4; ++db)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                *(LYCHEE_GLOBAL f32x4_t *)(po + (4 * db + j) * 256) = f32x4_t{o[db][4 * j], o[db][4 * j + 1], o[db][4 * j + 2], o[db][4 * j + 3]};
-        if (hi == 0) gstore_f2(a.part_ml + (at * 32 + lane) * 2, make_float2(m, l));
-    }
+                for (int j = 0; j < 4; ++j)
+                    *(LYCHEE_GLOBAL f32x4_t *)(po + (4 * db + j) * 256) = f32x4_t{o[db][4 * j], o[db][4 * j + 1], o[db][4 * j + 2], o[db][4 * j + 3]};
+            if (hi == 0) gstore_f2(a.part_ml + (part * 32 + lane) * 2, make_float2(m, l));
+        }
+    } while (share && at < opaque64(until));
 }
 
 // Rows of split tiles: o = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p, M = max m_p.  A workgroup has 32 rows of a tile and some of the
@@ -261,46 +299,86 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
 constexpr int kMergeBatch = 16;  // pieces whose loads are in flight together
 __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptArgs a)
 {
-    __shared__ SharedPlan sh;
     __shared__ __align__(16) f32x4_t sum[kWaves][64];
     __shared__ float2 ml[kWaves][64];
     const PromptRows &p = a.r;
-    const int sub = blockIdx.x % a.merge_split, unit = blockIdx.x / a.merge_split, rows32 = unit % kWaves, g = unit / kWaves % p.n_kv_heads;
-    const Tile w = find_tile<true>(p, unit / kWaves / p.n_kv_heads, a.slots, sh);
-    if (!w.found || w.parts == 1 || w.slot + w.parts > a.n_slots) return;
+    // (KV heads apart as in the launch before, whose partials lie in the caches of the same part of the device)
+    const int g = blockIdx.x % p.n_kv_heads, unit = blockIdx.x / p.n_kv_heads, sub = unit % a.merge_split, rows32 = unit / a.merge_split % kWaves;
+    const Record w = recorded(a.records, unit / a.merge_split / kWaves);
+    const int parts = w.parts, range = w.range;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rows = w.n * p.group;
+    if (parts == 0 || w.tile * kPromptRows + rows32 * 32 >= rows) return;
     const int row = w.tile * kPromptRows + rows32 * 32 + (lane & 31), token = token_of(p, min(row, rows - 1)), head = g * p.group + min(row, rows - 1) - token * p.group;
     const int64_t to = (int64_t)(w.start + token) * (p.n_kv_heads * p.group) + head;
-    const auto at = [&](int piece) { return ((int64_t)(w.slot + piece) * p.n_kv_heads + g) * kWaves + rows32; };
+    const auto at = [&](int piece) { return part_slot(range + piece, piece == 0, p.n_kv_heads, g) * kWaves + rows32; };
+    const auto store = [&](int dj, f32x4_t o, float f) {  // (dimensions of register group dj: 32 db + 8 j + 4 hi)
+        *(LYCHEE_GLOBAL u32x2_t *)(a.out + to * kHeadDim + 8 * dj + 4 * (lane >> 5)) = u32x2_t{pk_bf16(o[0] * f, o[1] * f), pk_bf16(o[2] * f, o[3] * f)};
+    };
+    const auto store_lse = [&](float m, float l) {
+        if (a.lse && lane < 32)
+            gstore(a.lse + (int64_t)head * p.n_tokens + w.start + token, l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * (1.f / kLog2e));
+    };
+    // Few pieces: a wavefront has all of them of a group of dimensions.
+    const auto few = [&](auto most) {
+        constexpr int kMost = decltype(most)::value;
+        f32x2_t mls[kMost];
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+            mls[i] = f32x2_t{-__builtin_inff(), 0.f};
+            if (i < parts) mls[i] = *(const LYCHEE_GLOBAL f32x2_t *)(a.part_ml + (at(i) * 32 + (lane & 31)) * 2);
+        }
+        float m = -__builtin_inff(), l = 0.f, e[kMost];
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) m = fmaxf(m, mls[i][0]);
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+            e[i] = fast_exp2(mls[i][0] - (m == -__builtin_inff() ? 0.f : m));
+            l += e[i] * mls[i][1];
+        }
+        if (sub == 0 && wave == 0 && row < rows) store_lse(m, l);
+        for (int dj = sub * kWaves + wave; dj < 16; dj += a.merge_split * kWaves) {
+            f32x4_t os[kMost], o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < kMost; ++i) {
+                os[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                if (i < parts) os[i] = *(const LYCHEE_GLOBAL f32x4_t *)(a.part_o + at(i) * (64 * 64) + dj * 256 + 4 * lane);
+            }
+#pragma unroll
+            for (int i = 0; i < kMost; ++i) o += e[i] * os[i];
+            if (row < rows) store(dj, o, l == 0.f ? 0.f : 1.f / l);
+        }
+    };
+    if (parts <= 2) return few(std::integral_constant<int, 2>{});
+    if (parts <= 4) return few(std::integral_constant<int, 4>{});
+    if (parts <= 8) return few(std::integral_constant<int, 8>{});
+    if (parts <= 16) return few(std::integral_constant<int, 16>{});
     for (int dj = sub; dj < 16; dj += a.merge_split) {
         float m = -__builtin_inff(), l = 0.f;
         f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-        for (int first = wave; first < w.parts; first += kWaves * kMergeBatch) {
+        for (int first = wave; first < parts; first += kWaves * kMergeBatch) {
             f32x2_t mls[kMergeBatch];
             f32x4_t os[kMergeBatch];
 #pragma unroll
             for (int i = 0; i < kMergeBatch; ++i) {
-                const int64_t from = at(min(first + kWaves * i, w.parts - 1));
+                mls[i] = f32x2_t{-__builtin_inff(), 0.f};
+                os[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                if (first + kWaves * i >= parts) continue;  // (the last one's place instead, by all wavefronts at once, is a crowd)
+                const int64_t from = at(first + kWaves * i);
                 mls[i] = *(const LYCHEE_GLOBAL f32x2_t *)(a.part_ml + (from * 32 + (lane & 31)) * 2);
                 os[i] = *(const LYCHEE_GLOBAL f32x4_t *)(a.part_o + from * (64 * 64) + dj * 256 + 4 * lane);
             }
             float up = m;
 #pragma unroll
-            for (int i = 0; i < kMergeBatch; ++i) {
-                if (first + kWaves * i >= w.parts) mls[i][0] = -__builtin_inff();
-                up = fmaxf(up, mls[i][0]);
-            }
+            for (int i = 0; i < kMergeBatch; ++i) up = fmaxf(up, mls[i][0]);
             const float ref = up == -__builtin_inff() ? 0.f : up, f = fast_exp2(m - ref);
             m = up;
             l *= f;
             o *= f;
 #pragma unroll
             for (int i = 0; i < kMergeBatch; ++i) {
-                const bool there = first + kWaves * i < w.parts;
                 const float e = fast_exp2(mls[i][0] - ref);
-                l += there ? e * mls[i][1] : 0.f;
-#pragma unroll
-                for (int d = 0; d < 4; ++d) o[d] += there ? e * os[i][d] : 0.f;
+                l += e * mls[i][1];
+                o += e * os[i];
             }
         }
         sum[wave][lane] = o;
@@ -319,12 +397,9 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptArgs a)
                 l += e * ml[i][lane].y;
                 o += e * sum[i][lane];
             }
-            o *= l == 0.f ? 0.f : 1.f / l;
             if (row < rows) {
-                // (dimensions of register group dj: 32 db + 8 j + 4 hi)
-                *(LYCHEE_GLOBAL u32x2_t *)(a.out + to * kHeadDim + 8 * dj + 4 * (lane >> 5)) = u32x2_t{pk_bf16(o[0], o[1]), pk_bf16(o[2], o[3])};
-                if (a.lse && dj == 0 && lane < 32)
-                    gstore(a.lse + (int64_t)head * p.n_tokens + w.start + token, l == 0.f ? -__builtin_inff() : (top + __log2f(l)) * (1.f / kLog2e));
+                store(dj, o, l == 0.f ? 0.f : 1.f / l);
+                if (dj == 0) store_lse(top, l);
             }
         }
         __syncthreads();
@@ -335,12 +410,22 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptArgs a)
 
 hipError_t launch_prompt(const PromptArgs &a, hipStream_t stream)
 {
-    const unsigned grid = (unsigned)a.n_items * (unsigned)a.r.n_kv_heads;
+    const unsigned heads = (unsigned)a.r.n_kv_heads;
+    if (a.n_ranges == 0) {
+        if (a.cache)
+            prompt_kernel<true, false><<<(unsigned)a.n_tiles * heads, kThreads, 0, stream>>>(a);
+        else
+            prompt_kernel<false, false><<<(unsigned)a.n_tiles * heads, kThreads, 0, stream>>>(a);
+        return hipGetLastError();
+    }
+    const unsigned grid = (unsigned)(a.n_ranges > a.n_tiles ? a.n_ranges : a.n_tiles) * heads;
     if (a.cache)
-        prompt_kernel<true><<<grid, kThreads, 0, stream>>>(a);
+        prompt_kernel<true, true><<<grid, kThreads, 0, stream>>>(a);
     else
-        prompt_kernel<false><<<grid, kThreads, 0, stream>>>(a);
-    if (a.slots > 0) prompt_merge_kernel<<<(unsigned)a.n_tiles * (unsigned)a.r.n_kv_heads * kWaves * (unsigned)a.merge_split, kThreads, 0, stream>>>(a);
+        prompt_kernel<false, true><<<grid, kThreads, 0, stream>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    prompt_merge_kernel<<<(unsigned)a.n_records * heads * kWaves * (unsigned)a.merge_split, kThreads, 0, stream>>>(a);
     return hipGetLastError();
 }
 

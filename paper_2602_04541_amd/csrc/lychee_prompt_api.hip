@@ -10,8 +10,7 @@ using namespace lychee;
 
 namespace {
 
-constexpr int32_t kPromptSlots = 512;  // pieces that fill a device: two workgroups a compute unit
-constexpr int64_t kPromptSplitKeys = 1024;
+constexpr int32_t kPromptSlots = 512;  // ranges that fill a device: two workgroups a compute unit
 constexpr int64_t kMaxGrid = 1 << 24;  // workgroups of 256 threads, which are counted in 32 bits
 
 int check_heads_of(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim)
@@ -23,52 +22,64 @@ int check_heads_of(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim)
 
 bool good_stride(int64_t s) { return s >= 0 && s % 8 == 0; }
 
-// Pieces and tiles of a batch's query rows, of a KV head.
+// Tiles of a batch's query rows, or of its keys, of a KV head, and the ranges that they are shared out to.
 struct Grid {
-    int64_t tiles, items;
-    int32_t slots;
+    int64_t tiles, ranges, room;  // (room: ranges that a workspace has partials for, those of every smaller call too)
 };
-Grid grid_of(int32_t batch, int32_t n_kv_heads, int32_t group, int32_t n_tokens, int64_t max_len)
+int64_t ranges_of(int64_t blocks, int32_t smallest, int32_t n_kv_heads)  // what fills the device, no more than there are smallest ranges
+{
+    const int64_t most = blocks / smallest + 1, fill = kPromptSlots / n_kv_heads;
+    return most < fill ? most : fill;
+}
+// Whether lengths are possible with which a launch would share its tiles out (lay_line): a longest request against the least that
+// it and the others can have, of equal lengths and, in a cache, with no keys but their own.
+bool may_share(int32_t batch, int32_t heads, int32_t n_tokens, int64_t max_len, bool packed)
+{
+    const float range = (float)heads / (float)(kPromptRows * kPromptSlots), own = 1.f / (2 * kPromptKeys);
+    const auto weight = [&](float tokens, float of_each) { return tokens * range * (of_each * own + kPromptTileCost); };
+    const auto shared = [&](float longest, float all) { return longest / kPromptKeys + 1 + kPromptTileCost > kPromptShareCost + kPromptShareSize * all; };
+    const float n = (float)n_tokens;
+    if (!packed) return shared((float)max_len, weight(n, n / (float)batch));
+    if (batch == 1) return shared(n, weight(n, n));
+    for (int i = 1; i <= 12; ++i) {  // (one that has more than three quarters of all tokens is not looked for)
+        const float longest = n * (float)i / 16, others = n - longest;
+        if (shared(longest, weight(longest, longest) + weight(others, others / (float)(batch - 1)))) return true;
+    }
+    return false;
+}
+Grid rows_grid(int32_t batch, int32_t n_kv_heads, int32_t group, int32_t n_tokens, int64_t max_len, bool packed)
 {
     Grid w;
     w.tiles = (int64_t)n_tokens * group / kPromptRows + (batch < n_tokens ? batch : n_tokens);
-    // Few tiles over many keys are split along these: a piece has kPromptMinPiece blocks at least.
-    const bool split = w.tiles * n_kv_heads < 2 * kPromptSlots && max_len > kPromptSplitKeys;
-    w.slots = split ? kPromptSlots : 0;
-    w.items = w.tiles + (split ? (kPromptSlots + n_kv_heads - 1) / n_kv_heads : 0);
+    const int64_t longest = max_len / kPromptKeys + 1 + kPromptTileCost;
+    w.room = longest > kPromptShareCost ? ranges_of(w.tiles * longest, kPromptMinRange, n_kv_heads) : 0;
+    w.ranges = w.room > 0 && may_share(batch, n_kv_heads * group, n_tokens, max_len, packed) ? w.room : 0;
     return w;
 }
-
-// Ranges that a KV head's tiles of keys are shared out to in the backward pass: what fills the device, no more than there are
-// smallest pieces.
-struct KeyGrid {
-    int64_t tiles, ranges;
-};
-KeyGrid key_grid_of(int32_t batch, int32_t n_kv_heads, int32_t group, int32_t n_tokens)
+Grid keys_grid(int32_t batch, int32_t n_kv_heads, int32_t group, int32_t n_tokens)
 {
-    KeyGrid w;
+    Grid w;
     w.tiles = n_tokens / kPromptRows + (batch < n_tokens ? batch : n_tokens);
-    const int64_t blocks = w.tiles * ((int64_t)n_tokens * group / kPromptKeys + 1), fill = kPromptSlots / n_kv_heads;
-    w.ranges = blocks / kPromptMinRowPiece + 1;
-    if (w.ranges > fill) w.ranges = fill;
+    w.ranges = w.room = ranges_of(w.tiles * ((int64_t)n_tokens * group / kPromptKeys + 1), kPromptMinKeyRange, n_kv_heads);
     return w;
 }
 
+// A forward call's partials; a backward call's statistics and the partials of one launch after the other.
 struct CarvedPrompt {
     size_t part_ml, stat, part, total;
 };
-CarvedPrompt carve(const Grid &w, int32_t n_kv_heads, int64_t stats, int64_t ranges)
+CarvedPrompt carve(const Grid &w, int32_t n_kv_heads, int64_t stats, int64_t key_ranges)
 {
     CarvedPrompt c;
-    const int64_t rows = w.slots > 0 ? w.items * n_kv_heads * kPromptRows : 0;
-    c.part_ml = (size_t)(rows * kHeadDim * (int64_t)sizeof(float));
-    c.stat = 0;
-    // (the forward pass's partials and those of the backward pass are not needed at once)
-    c.part = (size_t)round_up(stats * 2 * (int64_t)sizeof(float), 256);
-    c.total = c.part + (size_t)(ranges * 2 * n_kv_heads * 2 * kPromptRows * kHeadDim * (int64_t)sizeof(float));
-    const size_t forward = c.part_ml + (size_t)round_up(rows * 2 * (int64_t)sizeof(float), 256);
+    const size_t tile = kPromptRows * kHeadDim * sizeof(float), ml = kPromptRows * 2 * sizeof(float);
+    const size_t of_rows = (size_t)(w.room * 2 * n_kv_heads), of_keys = (size_t)(key_ranges * 2 * n_kv_heads);
+    const size_t records = (size_t)kPromptSlots * kRecordWords * sizeof(int32_t);  // (first)
+    c.part_ml = records + of_rows * tile;
+    c.stat = records;
+    c.part = c.stat + (size_t)round_up(stats * 2 * (int64_t)sizeof(float), 256);
+    const size_t forward = c.part_ml + of_rows * ml, rows = stats > 0 ? of_rows * tile : 0, keys = of_keys * 2 * tile;
+    c.total = c.part + (rows > keys ? rows : keys);
     if (c.total < forward) c.total = forward;
-    if (c.total == 0) c.total = 256;
     return c;
 }
 
@@ -85,19 +96,16 @@ int check_prompt(const lychee_prompt *p)
     if (p->q_stride_tok > kPromptMaxStride || p->q_stride_head > kPromptMaxStride || p->kv_stride_tok > kPromptMaxStride) return LYCHEE_EUNSUPPORTED;
     const int32_t G = p->n_q_heads / p->n_kv_heads;
     if ((int64_t)p->n_tokens * G >= kPromptMaxRows) return LYCHEE_EUNSUPPORTED;
-    if (grid_of(p->batch, p->n_kv_heads, G, p->n_tokens, 0).tiles * p->n_kv_heads >= kMaxGrid) return LYCHEE_EUNSUPPORTED;
+    if (rows_grid(p->batch, p->n_kv_heads, G, p->n_tokens, 0, false).tiles * p->n_kv_heads >= kMaxGrid) return LYCHEE_EUNSUPPORTED;
     return LYCHEE_OK;
 }
 
 // (for either kind of keys: the longer request that a batch may hold)
-Grid grid_of(const lychee_prompt &p)
-{
-    return grid_of(p.batch, p.n_kv_heads, p.n_q_heads / p.n_kv_heads, p.n_tokens, p.max_len > p.n_tokens ? p.max_len : p.n_tokens);
-}
 CarvedPrompt carve(const lychee_prompt &p)
 {
-    return carve(grid_of(p), p.n_kv_heads, (int64_t)p.n_tokens * p.n_q_heads,
-                 key_grid_of(p.batch, p.n_kv_heads, p.n_q_heads / p.n_kv_heads, p.n_tokens).ranges);
+    const int32_t G = p.n_q_heads / p.n_kv_heads;
+    return carve(rows_grid(p.batch, p.n_kv_heads, G, p.n_tokens, p.max_len > p.n_tokens ? p.max_len : p.n_tokens, false), p.n_kv_heads,
+                 (int64_t)p.n_tokens * p.n_q_heads, keys_grid(p.batch, p.n_kv_heads, G, p.n_tokens).room);
 }
 
 PromptRows rows_of(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_tokens, int32_t max_len, int64_t q_tok, int64_t q_head,
@@ -128,15 +136,17 @@ bool still_read(const lychee_ctx *ctx, const void *workspace) { return ctx->pend
 
 void fill_split(PromptArgs &a, const Grid &w, const CarvedPrompt &c, void *workspace)
 {
-    a.part_o = static_cast<float *>(workspace);
+    a.records = static_cast<int32_t *>(workspace);
+    a.part_o = reinterpret_cast<float *>(static_cast<char *>(workspace) + c.stat);
     a.part_ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + c.part_ml);
-    a.slots = w.slots;
+    a.n_ranges = (int32_t)w.ranges;
+    a.n_tiles = (int32_t)w.tiles;
+    a.one_range = w.ranges > 0 ? 1.0 / (double)w.ranges : 0.0;
+    a.by_number = w.tiles < w.ranges;
+    a.n_records = a.by_number ? a.n_tiles : a.n_ranges;
     // (about 1024 workgroups: two that fit a compute unit at a time)
     a.merge_split = 1;
-    while (a.merge_split < 16 && w.tiles * a.r.n_kv_heads * kWaves * a.merge_split < 512) a.merge_split *= 2;
-    a.n_items = (int32_t)w.items;
-    a.n_tiles = (int32_t)w.tiles;
-    a.n_slots = w.slots > 0 ? a.n_items : 0;
+    while (a.merge_split < 16 && a.n_records * a.r.n_kv_heads * kWaves * a.merge_split < 512) a.merge_split *= 2;
     a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)kHeadDim));
 }
 
@@ -174,7 +184,7 @@ int lychee_prompt_attn(lychee_ctx *ctx, const lychee_prompt *prompt, const void 
     a.kv_tok = p.kv_stride_tok;
     a.out = static_cast<uint16_t *>(out);
     a.lse = lse;
-    fill_split(a, grid_of(p.batch, p.n_kv_heads, a.r.group, p.n_tokens, lengths ? p.max_len : p.n_tokens), c, workspace);
+    fill_split(a, rows_grid(p.batch, p.n_kv_heads, a.r.group, p.n_tokens, lengths ? p.max_len : p.n_tokens, !lengths), c, workspace);
     return done(launch_prompt(a, static_cast<hipStream_t>(hip_stream)));
 }
 
@@ -213,15 +223,23 @@ int lychee_prompt_attn_backward(lychee_ctx *ctx, const lychee_prompt *prompt, co
     a.dq = static_cast<uint16_t *>(dq);
     a.dk = static_cast<uint16_t *>(dk);
     a.dv = static_cast<uint16_t *>(dv);
+    a.records = static_cast<int32_t *>(workspace);
     a.stat = reinterpret_cast<float *>(static_cast<char *>(workspace) + c.stat);
     a.scale = (float)(1.0 / sqrt((double)kHeadDim));
     a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)kHeadDim));
     a.root = (float)sqrt((double)kHeadDim);
-    a.n_row_tiles = (int32_t)grid_of(p.batch, p.n_kv_heads, a.r.group, p.n_tokens, 0).tiles;
-    const KeyGrid w = key_grid_of(p.batch, p.n_kv_heads, a.r.group, p.n_tokens);
+    const Grid rows = rows_grid(p.batch, p.n_kv_heads, a.r.group, p.n_tokens, p.n_tokens, true);
+    const Grid keys = keys_grid(p.batch, p.n_kv_heads, a.r.group, p.n_tokens);
     a.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + c.part);
-    a.n_ranges = (int32_t)w.ranges;
-    a.n_key_tiles = (int32_t)w.tiles;
+    a.n_row_ranges = (int32_t)rows.ranges;
+    a.n_key_ranges = (int32_t)keys.ranges;
+    a.n_row_tiles = (int32_t)rows.tiles;
+    a.one_row_range = rows.ranges > 0 ? 1.0 / (double)rows.ranges : 0.0;
+    a.one_key_range = 1.0 / (double)keys.ranges;
+    a.rows_by_number = rows.tiles < rows.ranges;
+    a.n_row_records = (int32_t)(a.rows_by_number ? rows.tiles : rows.ranges);
+    a.keys_by_number = keys.tiles < keys.ranges;
+    a.n_key_records = (int32_t)(a.keys_by_number ? keys.tiles : keys.ranges);
     return done(launch_prompt_grad(a, static_cast<hipStream_t>(hip_stream)));
 }
 
@@ -230,7 +248,7 @@ size_t lychee_q4_prompt_workspace_bytes(const lychee_paged *paged, int32_t n_tok
     if (lychee_check_paged(paged, nullptr, 1) != LYCHEE_OK || n_tokens < 0) return 0;
     const int32_t G = paged->n_q_heads / paged->n_kv_heads;
     if (G > kPromptMaxGroup || (int64_t)n_tokens * G >= kPromptMaxRows) return 0;
-    return carve(grid_of(paged->batch, paged->n_kv_heads, G, n_tokens, (int64_t)paged->max_pages * paged->page_size), paged->n_kv_heads, 0, 0).total;
+    return carve(rows_grid(paged->batch, paged->n_kv_heads, G, n_tokens, (int64_t)paged->max_pages * paged->page_size, false), paged->n_kv_heads, 0, 0).total;
 }
 
 int lychee_q4_prompt_attn(lychee_ctx *ctx, const lychee_paged *paged, const void *q, int64_t q_stride_tok, int64_t q_stride_head,
@@ -246,7 +264,7 @@ int lychee_q4_prompt_attn(lychee_ctx *ctx, const lychee_paged *paged, const void
     const int32_t G = p.n_q_heads / p.n_kv_heads, max_len = p.max_pages * p.page_size;
     if ((int64_t)n_tokens * G >= kPromptMaxRows || q_stride_tok > kPromptMaxStride || q_stride_head > kPromptMaxStride) return LYCHEE_EUNSUPPORTED;
     if (!good_stride(q_stride_tok) || !good_stride(q_stride_head) || q_stride_tok < kHeadDim) return LYCHEE_EINVAL;
-    const Grid w = grid_of(p.batch, p.n_kv_heads, G, n_tokens, max_len);
+    const Grid w = rows_grid(p.batch, p.n_kv_heads, G, n_tokens, max_len, false);
     if (w.tiles * p.n_kv_heads >= kMaxGrid) return LYCHEE_EUNSUPPORTED;
     if (!cache || !block_table || !lengths || !token_start || !aligned(cache, 128) || !aligned(block_table, 4) || !aligned(lengths, 4) ||
         !aligned(token_start, 4))

@@ -69,24 +69,21 @@ __device__ __forceinline__ f32x16_t zero16() { return all16(0.f); }
 // ------------------------------------------------------------------------------ rows
 __device__ __forceinline__ int token_of(const PromptRows &p, int row) { return p.group == 1 ? row : (int)__umulhi((uint32_t)row, p.group_magic); }
 
-// What a workgroup works on: a piece of a tile, which is kPromptRows rows of a (request, KV head).
+// What a workgroup works on: blocks of keys of a tile, which is kPromptRows rows of a (request, KV head).
 struct Tile {
     int b, tile;
-    int n, len;            // query tokens and keys of the request
-    int start;             // its first token among the packed rows
-    int piece, parts;      // this piece and how many the tile has that hold keys (at least 1)
-    int first, last;       // blocks of keys of the piece
-    int slot;              // of the piece's partial in its KV head (in a merge: of the tile's first piece)
+    int n, len;       // query tokens and keys of the request
+    int start;        // its first token among the packed rows
+    int first, last;  // blocks of keys
     bool found;
 };
 
 struct SharedPlan {
     int32_t n[kMaxBatch], len[kMaxBatch], start[kMaxBatch], weight[kMaxBatch];
-    int32_t items[kMaxBatch], slots[kMaxBatch];  // by rank
-    uint8_t who[kMaxBatch];                      // the request of a rank
-    uint32_t wave[2][kWaves];
-    unsigned long long work[kWaves];
-    int32_t found[3];
+    int32_t tiles[kMaxBatch];  // by rank
+    uint8_t who[kMaxBatch];    // the request of a rank
+    uint32_t wave[kWaves];
+    int32_t found[2];
 };
 static_assert(kThreads == kMaxBatch, "a thread a request");
 
@@ -99,208 +96,283 @@ __device__ __forceinline__ void request_of(const PromptRows &p, int b, int &star
 }
 __device__ __forceinline__ int blocks_of(int keys) { return (int)(((int64_t)keys + kPromptKeys - 1) / kPromptKeys); }
 __device__ __forceinline__ int tiles_of(int rows) { return (rows + kPromptRows - 1) / kPromptRows; }
-
-// Sum over the workgroup's threads, for all of them.
-__device__ __forceinline__ unsigned long long sum_all(unsigned long long w, SharedPlan &sh)
+__device__ __forceinline__ int blocks_seen(const PromptRows &p, int tile, int n, int len)  // by a tile's last row
 {
-    for (int d = 32; d > 0; d >>= 1) w += __shfl_xor(w, d);
-    if ((threadIdx.x & 63) == 0) sh.work[threadIdx.x >> 6] = w;
-    __syncthreads();
-    w = 0;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) w += sh.work[i];
-    return w;
+    return blocks_of(max(0, len - n + token_of(p, min((tile + 1) * kPromptRows, n * p.group) - 1) + 1));
 }
 
-// Which request has the `number`th of all the requests' `items`, where thread b knows request b's numbers of items and of `slots`
-// for partials.  Requests come in descending order of `weight`, so that what takes longest begins first.  The answer
-// is sh.found: the request or -1, the number within it, the slots of the requests before it.
-__device__ __forceinline__ void find_request(int batch, int number, int weight, int items, int slots, SharedPlan &sh)
+__device__ __forceinline__ int64_t uniform64(int64_t x)
+{
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+}
+
+// Which request has the `number`th of all the requests' tiles, where thread b knows request b's `tiles`.  Requests come in
+// descending order of `weight`, so that what takes longest begins first.  The answer is sh.found: the request or -1, and the
+// number within it.
+__device__ __forceinline__ void find_request(int batch, int number, int weight, int tiles, SharedPlan &sh)
 {
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     sh.weight[t] = weight;
     if (t == 0) sh.found[0] = -1;
     __syncthreads();
-    int rank = t;
-    if (batch > 1) {
-        rank = 0;
-        for (int i = 0; i < batch; ++i) {
-            const int other = sh.weight[i];
-            rank += other > weight || (other == weight && i < t);
-        }
+    int rank = 0;
+    for (int i = 0; i < batch; ++i) {
+        const int other = sh.weight[i];
+        rank += other > weight || (other == weight && i < t);
     }
     if (t < batch) {
-        sh.items[rank] = items;
-        sh.slots[rank] = slots;
+        sh.tiles[rank] = tiles;
         sh.who[rank] = (uint8_t)t;
     }
     __syncthreads();
-    const uint32_t items_here = t < batch ? (uint32_t)sh.items[t] : 0u, slots_here = t < batch ? (uint32_t)sh.slots[t] : 0u;
-    const uint32_t items_upto = wave_scan(items_here), slots_upto = wave_scan(slots_here);
-    if (lane == 63) {
-        sh.wave[0][wave] = items_upto;
-        sh.wave[1][wave] = slots_upto;
-    }
+    const uint32_t here = t < batch ? (uint32_t)sh.tiles[t] : 0u, upto = wave_scan(here);
+    if (lane == 63) sh.wave[wave] = upto;
     __syncthreads();
-    uint32_t items_before = items_upto - items_here, slots_before = slots_upto - slots_here;
-    for (int i = 0; i < wave; ++i) {
-        items_before += sh.wave[0][i];
-        slots_before += sh.wave[1][i];
-    }
-    if ((uint32_t)number - items_before < items_here) {
+    uint32_t before = upto - here;
+    for (int i = 0; i < wave; ++i) before += sh.wave[i];
+    if ((uint32_t)number - before < here) {
         sh.found[0] = sh.who[t];
-        sh.found[1] = number - (int)items_before;
-        sh.found[2] = (int)slots_before;
+        sh.found[1] = number - (int)before;
     }
     __syncthreads();
 }
 
-// A request that a workgroup has found a piece of: the piece's number within it, and its first partial's.
-struct Found {
-    int b, at, before, start, n, len;
-};
-__device__ __forceinline__ Found found_alone(int number, int items, int start, int n, int len)
-{
-    Found f;
-    f.b = number < __builtin_amdgcn_readfirstlane(items) ? 0 : -1;
-    f.at = number;
-    f.before = 0;
-    f.start = __builtin_amdgcn_readfirstlane(start);
-    f.n = __builtin_amdgcn_readfirstlane(n);
-    f.len = __builtin_amdgcn_readfirstlane(len);
-    return f;
-}
-__device__ __forceinline__ Found found_among(const SharedPlan &sh)
-{
-    Found f;
-    f.b = __builtin_amdgcn_readfirstlane(sh.found[0]);
-    f.at = __builtin_amdgcn_readfirstlane(sh.found[1]);
-    f.before = __builtin_amdgcn_readfirstlane(sh.found[2]);
-    const int b = f.b < 0 ? 0 : f.b;
-    f.start = __builtin_amdgcn_readfirstlane(sh.start[b]);
-    f.n = __builtin_amdgcn_readfirstlane(sh.n[b]);
-    f.len = __builtin_amdgcn_readfirstlane(sh.len[b]);
-    return f;
-}
-
-// The piece with this number (MERGE: the tile); of a request the last tile first, which sees most keys.  `slots` > 0: tiles are
-// split into pieces of so many blocks that there are about `slots` of them in all KV heads.
-template <bool MERGE>
-__device__ __forceinline__ Tile find_tile(const PromptRows &p, int number, int slots, SharedPlan &sh)
+// The tile with this number, all its blocks; of a request the last tile first, which sees most keys.
+__device__ __forceinline__ Tile find_tile(const PromptRows &p, int number, SharedPlan &sh)
 {
     const bool alone = p.batch == 1;  // (nothing to look for, no barrier)
     const int t = alone ? 0 : threadIdx.x;
     int start = 0, n = 0, len = 0;
     if (t < p.batch) request_of(p, t, start, n, len);
-    const int tiles = tiles_of(n * p.group), blocks = blocks_of(len);
-    int size = 1 << 30;
-    if (slots > 0) {
-        unsigned long long w = (unsigned long long)tiles * (unsigned)max(blocks, 1) * (unsigned)p.n_kv_heads;
-        if (!alone) w = sum_all(w, sh);
-        size = __builtin_amdgcn_readfirstlane(max((int)min((w + slots - 1) / slots, 1ull << 30), kPromptMinPiece));
-    }
-    const int items = tiles * max(1, (blocks + size - 1) / size);
-    Found f;
+    const int tiles = tiles_of(n * p.group);
+    Tile w;
+    int at = number;
     if (alone) {
-        f = found_alone(number, MERGE ? tiles : items, start, n, len);
+        w.b = number < __builtin_amdgcn_readfirstlane(tiles) ? 0 : -1;
     } else {
         sh.n[t] = n;
         sh.len[t] = len;
         sh.start[t] = start;
-        find_request(p.batch, number, len, MERGE ? tiles : items, items, sh);
-        f = found_among(sh);
+        find_request(p.batch, number, len, tiles, sh);
+        w.b = __builtin_amdgcn_readfirstlane(sh.found[0]);
+        at = __builtin_amdgcn_readfirstlane(sh.found[1]);
+        const int b = w.b < 0 ? 0 : w.b;
+        start = sh.start[b];
+        n = sh.n[b];
+        len = sh.len[b];
     }
-    Tile w;
-    w.b = f.b;
-    w.found = f.b >= 0;
+    w.found = w.b >= 0;
     if (!w.found) return w;
-    w.n = f.n;
-    w.len = f.len;
-    w.start = f.start;
-    const int rows = w.n * p.group, pieces = max(1, (blocks_of(w.len) + size - 1) / size);
-    w.tile = tiles_of(rows) - 1 - (MERGE ? f.at : f.at / pieces);
-    w.piece = MERGE ? 0 : f.at % pieces;
-    w.slot = f.before + (MERGE ? f.at * pieces : f.at);
-    const int seen = max(0, w.len - w.n + token_of(p, min((w.tile + 1) * kPromptRows, rows) - 1) + 1);  // keys of the last row
-    w.parts = max(1, (blocks_of(seen) + size - 1) / size);
-    w.first = pieces == 1 ? 0 : w.piece * size;
-    w.last = min(blocks_of(seen), pieces == 1 ? 1 << 30 : w.first + size);
+    w.start = __builtin_amdgcn_readfirstlane(start);
+    w.n = __builtin_amdgcn_readfirstlane(n);
+    w.len = __builtin_amdgcn_readfirstlane(len);
+    w.tile = tiles_of(w.n * p.group) - 1 - at;
+    w.first = 0;
+    w.last = blocks_seen(p, w.tile, w.n, w.len);
     return w;
 }
 
-// Tiles of kPromptRows keys, which the rows from the tile's first key on see, as a line of blocks of kPromptKeys rows:
-// request after request and tile after tile.  Tile k of a request with `end` blocks of rows has end - 2 G k of them.  A
-// workgroup has a range of the line, all of the same size, whatever tiles it holds the parts of.
-__device__ __forceinline__ int64_t blocks_before(int64_t tile, int end, int group) { return tile * end - (int64_t)group * tile * (tile - 1); }
+// A number the compiler forgets what it is made of: what derives from it is computed where it is used, an instruction each, and
+// kept in no register from block to block.
+__device__ __forceinline__ uint32_t opaque(uint32_t x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+__device__ __forceinline__ int64_t opaque64(int64_t x)  // (the same for the wavefront)
+{
+    asm volatile("" : "+s"(x));
+    return x;
+}
 
+// Tiles of all requests along a line, which is cut into ranges of the same length, one a workgroup, whatever tiles and parts
+// of tiles they hold: all workgroups have as much to do.  Of rows (kRows): tile k of a request weighs what its last row sees, in units of
+// 1/G key, and kPromptTileCost blocks more for what a tile costs by itself.  Of keys: what rows see its first key, in blocks of them.
+enum { kLineRows, kLineKeys };
 struct SharedLine {
-    int32_t n[kMaxBatch], start[kMaxBatch];
-    int64_t before[kMaxBatch];  // blocks of the requests before
+    int32_t n[kMaxBatch], len[kMaxBatch], start[kMaxBatch];
+    int64_t before[kMaxBatch];        // what the requests before weigh,
+    int32_t tiles_before[kMaxBatch];  //   and their tiles
     int64_t wave[kWaves];
+    int32_t tiles[kWaves], longest[kWaves];
 };
 struct Line {
-    int64_t all, size;  // blocks of the line, and of a range
+    int64_t all, size;  // length of the line, and of a range
+    int tiles;
+    int start, n, len;  // of the only request, where there is one
+    bool share;         // of rows: whether tiles are shared out, or each is one workgroup's
 };
-__device__ __forceinline__ int64_t uniform64(int64_t x)
+// What the tiles before a tile weigh together.
+template <int KIND>
+__device__ __forceinline__ int64_t weight_before(const PromptRows &p, int64_t tile, int n, int len)
 {
-    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+    if (KIND == kLineRows) return tile * ((int64_t)p.group * (max(len - n, 0) + kPromptTileCost * kPromptKeys)) + kPromptRows / 2 * tile * (tile + 1);
+    return tile * blocks_of(n * p.group) - (int64_t)(kPromptRows / kPromptKeys) * p.group * tile * (tile - 1) / 2;
 }
-__device__ __forceinline__ Line lay_line(const PromptRows &p, int ranges, SharedLine &sh)
+template <int KIND>
+__device__ __forceinline__ int line_tiles(const PromptRows &p, int n) { return tiles_of(KIND == kLineRows ? n * p.group : n); }
+
+template <int KIND>
+__device__ __forceinline__ Line lay_line(const PromptRows &p, double one_range, SharedLine &sh)
 {
-    static_assert(kPromptRows == 2 * kPromptKeys, "");
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const bool alone = p.batch == 1;  // (no LDS, no barrier)
+    const int t = alone ? 0 : threadIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int start = 0, n = 0, len = 0;
     if (t < p.batch) request_of(p, t, start, n, len);
-    const int64_t work = blocks_before(tiles_of(n), blocks_of(n * p.group), p.group);
-    int64_t upto = work;
-    if (p.batch > 1) {
+    Line l;
+    l.start = start;
+    l.n = n;
+    l.len = len;
+    l.tiles = line_tiles<KIND>(p, n);
+    l.all = weight_before<KIND>(p, l.tiles, n, len);
+    int longest = n > 0 ? blocks_of(len) : 0;
+    if (!alone) {
+        const int tiles = l.tiles;
+        const int64_t weight = l.all;
+        int tiles_upto = (int)wave_scan((uint32_t)tiles);
+        int64_t upto = weight;
         for (int d = 1; d < 64; d <<= 1) {
             const int64_t x = __shfl_up(upto, d);
             upto += lane >= d ? x : 0;
         }
-        if (lane == 63) sh.wave[wave] = upto;
+        longest = (int)wave_max((uint32_t)longest);
+        if (lane == 63) {
+            sh.longest[wave] = longest;
+            sh.tiles[wave] = tiles_upto;
+            sh.wave[wave] = upto;
+        }
         __syncthreads();
-        for (int i = 0; i < wave; ++i) upto += sh.wave[i];
+        l.tiles = 0;
+        l.all = 0;
+        longest = 0;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+            tiles_upto += i < wave ? sh.tiles[i] : 0;
+            upto += i < wave ? sh.wave[i] : 0;
+            l.tiles += sh.tiles[i];
+            l.all += sh.wave[i];
+            longest = max(longest, sh.longest[i]);
+        }
+        sh.n[t] = n;
+        sh.len[t] = len;
+        sh.start[t] = start;
+        sh.before[t] = upto - weight;
+        sh.tiles_before[t] = tiles_upto - tiles;
+        __syncthreads();
     }
-    sh.n[t] = n;
-    sh.start[t] = start;
-    sh.before[t] = upto - work;
-    __syncthreads();
-    Line l;
-    const int last = p.batch - 1, n_last = sh.n[last];
-    l.all = uniform64(sh.before[last] + blocks_before(tiles_of(n_last), blocks_of(n_last * p.group), p.group));
-    l.size = max((l.all + ranges - 1) / ranges, (int64_t)kPromptMinRowPiece);
+    const int unit = KIND == kLineRows ? p.group * kPromptKeys : 1;  // a block
+    l.size = uniform64((int64_t)((double)l.all * one_range) + 1);
+    l.size = uniform64(max(l.size, (int64_t)(KIND == kLineKeys ? kPromptMinKeyRange : kPromptMinRange) * unit));
+    l.share = KIND == kLineKeys || (float)__builtin_amdgcn_readfirstlane(longest) > kPromptShareCost + kPromptShareSize * (float)l.size / (float)unit;
+    l.all = uniform64(l.all);
+    l.tiles = __builtin_amdgcn_readfirstlane(l.tiles);
+    l.start = __builtin_amdgcn_readfirstlane(l.start);
+    l.n = __builtin_amdgcn_readfirstlane(l.n);
+    l.len = __builtin_amdgcn_readfirstlane(l.len);
     return l;
 }
 
-struct KeyTile {
-    int n, start, tile;
-    int64_t at;       // of its first block on the line
-    int first, end;   // its blocks of rows
+struct LineTile {
+    int b, tile, n, len, start;
+    int number;          // among all requests' tiles
+    int64_t at, weight;  // where the tile begins on the line, and what it weighs
 };
-__device__ __forceinline__ KeyTile key_tile(const PromptRows &p, int b, int tile, int64_t before, const SharedLine &sh)
+// A request on the line: the tile's number is still the request's first one's, its place the request's.
+__device__ __forceinline__ LineTile line_request(const PromptRows &p, int b, const Line &line, const SharedLine &sh)
 {
-    KeyTile k;
-    k.n = __builtin_amdgcn_readfirstlane(sh.n[b]);
-    k.start = __builtin_amdgcn_readfirstlane(sh.start[b]);
-    k.end = blocks_of(k.n * p.group);
-    k.tile = tile;
-    k.first = 2 * p.group * tile;
-    k.at = before + blocks_before(tile, k.end, p.group);
+    LineTile k;
+    k.b = b;
+    if (p.batch == 1) {
+        k.n = line.n;
+        k.len = line.len;
+        k.start = line.start;
+        k.number = 0;
+        k.at = 0;
+    } else {
+        k.n = __builtin_amdgcn_readfirstlane(sh.n[b]);
+        k.len = __builtin_amdgcn_readfirstlane(sh.len[b]);
+        k.start = __builtin_amdgcn_readfirstlane(sh.start[b]);
+        k.number = __builtin_amdgcn_readfirstlane(sh.tiles_before[b]);
+        k.at = uniform64(sh.before[b]);
+    }
+    k.n = __builtin_amdgcn_readfirstlane(k.n);
+    k.len = __builtin_amdgcn_readfirstlane(k.len);
+    k.start = __builtin_amdgcn_readfirstlane(k.start);
+    k.number = __builtin_amdgcn_readfirstlane(k.number);
+    k.at = uniform64(k.at);
     return k;
 }
-// The tile that holds a block of the line.
-__device__ __forceinline__ KeyTile tile_at(const PromptRows &p, int64_t at, const SharedLine &sh)
+// The tile that holds a place on the line.
+template <int KIND>
+__device__ __forceinline__ LineTile line_tile_at(const PromptRows &p, int64_t at, const Line &line, const SharedLine &sh)
 {
     int b = 0;
-    for (int step = kMaxBatch / 2; step > 0; step >>= 1)
-        if (b + step < p.batch && uniform64(sh.before[b + step]) <= at) b += step;
-    const int64_t before = uniform64(sh.before[b]);
-    const int n = __builtin_amdgcn_readfirstlane(sh.n[b]), end = blocks_of(n * p.group), tiles = tiles_of(n);
-    int tile = 0;
+    if (p.batch > 1)
+        for (int step = kMaxBatch / 2; step > 0; step >>= 1)
+            if (b + step < p.batch && uniform64(sh.before[b + step]) <= at) b += step;
+    LineTile k = line_request(p, b, line, sh);
+    const int tiles = line_tiles<KIND>(p, k.n);
+    k.tile = 0;
     for (int step = tiles > 1 ? 1 << (31 - __builtin_clz(tiles - 1)) : 0; step > 0; step >>= 1)
-        if (tile + step < tiles && blocks_before(tile + step, end, p.group) <= at - before) tile += step;
-    return key_tile(p, b, tile, before, sh);
+        if (k.tile + step < tiles && weight_before<KIND>(p, k.tile + step, k.n, k.len) <= at - k.at) k.tile += step;
+    const int64_t from = weight_before<KIND>(p, k.tile, k.n, k.len);
+    k.weight = weight_before<KIND>(p, k.tile + 1, k.n, k.len) - from;
+    k.at += from;
+    k.number += k.tile;
+    return k;
+}
+// Of a tile's blocks those before a place in it: 0 at its beginning, all at its end.  (In between an estimate: all that counts
+// is that who asks for the same place gets the same answer, and for a later one no smaller.)
+__device__ __forceinline__ int cut_at(int64_t place, int64_t weight, int blocks)
+{
+    const int cut = min((int)((float)place * ((float)blocks * __builtin_amdgcn_rcpf((float)weight))), blocks);
+    return __builtin_amdgcn_readfirstlane(place <= 0 ? 0 : place >= weight ? blocks : cut);
+}
+// Which range holds a place on the line.
+__device__ __forceinline__ int range_at(int64_t place, const Line &line)
+{
+    const int64_t size = opaque64(line.size);  // (so that its reciprocal is not kept through all the products)
+    int64_t r = (int64_t)((double)place * __builtin_amdgcn_rcp((double)size));  // (one off at most)
+    if (r * size > place) --r;
+    if ((r + 1) * size <= place) ++r;
+    return __builtin_amdgcn_readfirstlane((int)r);
+}
+// Partials: a range leaves two at most, that of the end of a tile that began in a range before, and that of a tile's beginning.
+__device__ __forceinline__ int64_t part_slot(int64_t range, bool beginning, int n_kv_heads, int g) { return (range * 2 + beginning) * n_kv_heads + g; }
+// For the merge, of a tile that lies in several ranges: how many (0: in one), the first of them, and what the tile is.  Kept by the range
+// it begins in, which is the only one there, or, where there are fewer tiles, by its number.  (A launch's first microseconds
+// go by the code that it runs once, which comes from memory: the merges read this, and lay no line.)
+struct Record {
+    int parts, range, tile, n, start, unused[3];
+};
+static_assert(sizeof(Record) == 4 * kRecordWords, "");
+__device__ __forceinline__ void keep_record(int32_t *records, int at, const Record &r)
+{
+    typedef int i32x4_t __attribute__((ext_vector_type(4)));
+    *(LYCHEE_GLOBAL i32x4_t *)(records + kRecordWords * at) = i32x4_t{r.parts, r.range, r.tile, r.n};
+    gstore(records + kRecordWords * at + 4, r.start);
+}
+// What no tile will fill in; one workgroup's first threads.
+__device__ __forceinline__ void clear_records(int32_t *records, int n_records, bool by_number, const Line &line, int range)
+{
+    if (by_number) {
+        if (range == 0)
+            for (int i = (line.share ? line.tiles : 0) + threadIdx.x; i < n_records; i += kThreads) gstore(records + kRecordWords * i, 0);
+    } else if (threadIdx.x == 0 && range < n_records) {
+        gstore(records + kRecordWords * range, 0);
+    }
+}
+__device__ __forceinline__ void record_tile(int32_t *records, int n_records, bool by_number, const Line &line, const LineTile &k, int range, bool whole)
+{
+    const int at = by_number ? k.number : range;
+    if (threadIdx.x == 0 && at < n_records && (by_number || !whole))
+        keep_record(records, at, {whole ? 0 : range_at(k.at + k.weight - 1, line) - range + 1, range, k.tile, k.n, k.start, {}});
+}
+__device__ __forceinline__ Record recorded(const int32_t *records, int at)
+{
+    const int32_t *r = records + kRecordWords * at;
+    return {__builtin_amdgcn_readfirstlane(gload(r)),     __builtin_amdgcn_readfirstlane(gload(r + 1)), __builtin_amdgcn_readfirstlane(gload(r + 2)),
+            __builtin_amdgcn_readfirstlane(gload(r + 3)), __builtin_amdgcn_readfirstlane(gload(r + 4)), {}};
 }
 
 // ------------------------------------------------------------------------------ LDS
@@ -315,11 +387,11 @@ __device__ __forceinline__ const T *uniform(const T *p)  // (in scalar registers
 }
 __device__ __forceinline__ void copy16(const uint16_t *base, uint32_t offset, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane((int)to)), "v"(offset), "s"(uniform(base)) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
 }
 __device__ __forceinline__ void copy4(const float *base, uint32_t offset, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(__builtin_amdgcn_readfirstlane((int)to)), "v"(offset), "s"(uniform(base)) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
 }
 __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(const LYCHEE_LDS uint8_t *)p; }
@@ -351,12 +423,19 @@ __device__ __forceinline__ bf16x8_t read_turned(const LYCHEE_LDS uint8_t *block,
     typedef short s16x8_t __attribute__((ext_vector_type(8)));
     return __builtin_bit_cast(bf16x8_t, (s16x8_t)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
-// A number the compiler forgets what it is made of: what derives from it is computed where it is used, an instruction each, and
-// kept in no register from block to block.
-__device__ __forceinline__ uint32_t opaque(uint32_t x)
+// Nothing is moved over this: reads of LDS stay as far ahead of the products that need them as they are written.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+// Waits for loads of the compiler's own here.  It does not see that wait_copies() waits for them too, and would wait for them at their
+// first use in the loop, every turn: by then that is a wait for the copies just begun.
+template <int N>
+__device__ __forceinline__ void arrived(bf16x8_t (&x)[N])
 {
-    asm volatile("" : "+v"(x));
-    return x;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        u32x4_t bits = __builtin_bit_cast(u32x4_t, x[i]);
+        asm volatile("" : "+v"(bits));
+        x[i] = __builtin_bit_cast(bf16x8_t, bits);
+    }
 }
 
 // Pairs that must not count have a weight of zero, but zero times an infinity or NaN is NaN.  A workgroup whose sums hold
@@ -369,7 +448,7 @@ constexpr uint32_t kLargest = 0x7F7Fu;
 __device__ __forceinline__ void take_with_care(uint8_t *block, int bytes, int turn)
 {
 #pragma unroll 1
-    for (int i = threadIdx.x; i < bytes / 4; i += kThreads) {
+    for (int i = (int)opaque(threadIdx.x); i < bytes / 4; i += kThreads) {
         uint32_t *at = reinterpret_cast<uint32_t *>(block) + i, both = *at, to = 0;
 #pragma unroll
         for (int h = 0; h < 32; h += 16) {
@@ -402,6 +481,16 @@ __device__ __forceinline__ bool all_finite(const f32x16_t (&x)[4])
 #pragma unroll
         for (int i = 0; i < 16; ++i) bad = __builtin_fmaf(x[d][i], 0.f, bad);
     return bad == 0.f;
+}
+
+// Whether any thread of the workgroup says so.
+__device__ __forceinline__ bool any_thread(bool x, int wave, int (&said)[kWaves])
+{
+    const bool any = __ballot(x) != 0;
+    __syncthreads();  // (the last answer has been read)
+    said[wave] = any;
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(said[0] | said[1] | said[2] | said[3]) != 0;
 }
 
 // A product's D, transposed rows of 128 numbers: column n is row n, registers of db its dimensions 32 db ..+31.  Sixteen bytes a
