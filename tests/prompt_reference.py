@@ -97,3 +97,29 @@ class Keys:
 
     def __call__(self, b, h):
         return self.of(b, h)
+
+
+def dense(q, k, v, pos, g=None):
+    """head() for long requests: the same formulas as products of whole matrices, of 64-bit torch tensors on any device."""
+    import torch
+    c = 1 / math.sqrt(D)
+    m = torch.arange(len(k), device=q.device) <= pos.view(-1, 1)
+    s = (q @ k.T) * c
+    big = torch.where(m, q.abs() @ k.abs().T, 0.0).amax(1) * c
+    each = (2 * (130 * u * big + 4 * u * torch.where(m, s.abs(), 0.0).amax(1)) + 2.0 ** -20).view(-1, 1)
+    s = torch.where(m, s, -math.inf)
+    lse = s.logsumexp(1)
+    p = torch.where(m, (s - lse.view(-1, 1)).exp(), 0.0)
+    out, seen = p @ v, p @ v.abs()
+    off_out = U * out.abs() + (U + 2 * each + SUM) * seen
+    got = {"out": (out, off_out), "lse": (lse, each[:, 0] + 4 * u * lse.abs() + 2.0 ** -20)}
+    if g is not None:
+        dp, delta = g @ v.T, (out * g).sum(1, keepdim=True)
+        ds = p * (dp - delta)
+        off_dp = (g.abs() * off_out).sum(1, keepdim=True) + 130 * u * (g.abs() @ v.abs().T + (g.abs() * out.abs()).sum(1, keepdim=True))
+        off_ds = torch.where(m, (U + each + SUM) * ds.abs() + p * off_dp, 0.0)
+        dq = c * ds @ k
+        got["dq"] = (dq, U * dq.abs() + c * off_ds @ k.abs())
+        got["dk"] = (c * ds.T @ q, c * off_ds.T @ q.abs())
+        got["dv"] = (p.T @ g, ((U + 2 * each + SUM) * p).T @ g.abs())
+    return got

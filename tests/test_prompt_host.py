@@ -254,3 +254,28 @@ def test_reference_leaves_out_what_is_not_seen():
     v[2:] = np.nan
     got = R.head(q, k, v, np.array([-1, 0, 1, 9]))
     assert (got["out"][0][:3] == want["out"][0][:3]).all() and np.isnan(got["out"][0][3]).all()
+
+
+def test_reference_in_matrices():
+    gen = torch.Generator().manual_seed(3)
+    q, g = (torch.randn((9, 128), dtype=torch.float64, generator=gen) for _ in range(2))
+    k, v = (torch.randn((30, 128), dtype=torch.float64, generator=gen) for _ in range(2))
+    pos = torch.arange(21, 30)
+    one, two = R.head(*(x.numpy() for x in (q, k, v, pos, g))), R.dense(q, k, v, pos, g)
+    assert one.keys() == two.keys()
+    for name in one:
+        for a, b in zip(one[name], two[name]):
+            assert abs(a - b.numpy()).max() <= 1e-12, name
+
+
+def test_a_workspace_serves_smaller_calls(lb):
+    """Fewer tokens, requests or keys need no more, whether a call shares its tiles out or not."""
+    for batch in (1, 3, 256):
+        for max_len in (1, 700, 5000, 1 << 20):
+            sizes = [lb.prompt_workspace_bytes(shape(lb, batch=batch, n_tokens=n, max_len=max_len)) for n in (1, 77, 300, 2000, 5000, 70000, 1 << 20)]
+            assert sizes == sorted(sizes) and sizes[0] > 0
+        sizes = [lb.q4_prompt_workspace_bytes(paged(lb, batch=batch), n) for n in (0, 1, 77, 300, 2000, 70000)]
+        assert sizes == sorted(sizes)
+    for n in (1, 300, 5000):
+        sizes = [lb.prompt_workspace_bytes(shape(lb, batch=b, n_tokens=n, max_len=m)) for b, m in ((1, 1), (1, 900), (2, 900), (2, 9000), (9, 9000), (256, 1 << 20))]
+        assert sizes == sorted(sizes)
