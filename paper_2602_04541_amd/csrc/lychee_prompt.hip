@@ -10,6 +10,14 @@
 // token's group shares a tile.  Scores are made turned, S^T = K Q^T: a lane has one row (column) and half of a
 // block's keys, the running maximum and sum need one exchange between two lanes, and the weights are the B operand of the second
 // product O^T = V^T P^T as they stand.
+//
+// What bounds it, long: the products, 64 of 32x32x16 for 128 rows and 64 keys.  16384 tokens of 32 heads (8 KV heads) take 2.08 ms,
+// 1.06 PFLOP/s; a library's product of 8192 x 8192 x 8192 reaches 1.30 on the same card at the clock that power leaves either,
+// about 1.9 GHz.  The matrix units are busy 55 % of the cycles, no read of LDS meets a bank twice, and the same loop without its copies
+// is 10 % faster.  Two wavefronts a unit share the rest: exponentials and sums of one beside the products of the other; the next
+// block's scores begun beside a block's weights, weights made between products and priorities by wavefront all cost more than they
+// gave.  Short: a launch and what it reads once, 6 us for 77 tokens.  Few rows over many keys: HBM and the merge, 51 us for 32
+// rows over 32768 keys of 8 heads, of which the launch over the keys takes 29 (134 MB, 4.6 TB/s) and the merge 8.
 #include "lychee_prompt_device.h"
 
 #include <type_traits>
@@ -18,8 +26,8 @@ namespace lychee {
 namespace {
 
 // Reads of keys ahead of their products (four, six and eight are as fast).  Of values eight are read before the weights are made, six of
-// a 4-bit cache, whose next block is written into LDS between the last products: 6.69 ms for two pieces of 4096 tokens behind 64 K
-// (7.00 with the block written behind them).
+// a 4-bit cache, whose next block is written into LDS between the last products: 6.69 ms for two pieces of 4001 to 4096 tokens that end
+// at 32 K to 61 K (7.00 with the block written behind them).
 constexpr int kAhead = 6;
 constexpr float kSlack = 8.f;    // powers of two by which a score may exceed the maximum that weights are measured against
 
@@ -34,6 +42,7 @@ struct SharedPrompt {
     };
 };
 
+// SHARE: a workgroup has a range of all tiles where lengths make it worth it (lay_line), else a tile like the other kernel's.
 template <bool Q4, bool SHARE>
 __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
 {
@@ -110,7 +119,8 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
             }
         };
         // 4 bits: a wavefront takes a tile of 16 tokens of every block, a lane a quarter (one scale's dimensions) of a token's key and of its
-        // value, whose bf16 numbers it writes.  (16 lanes the same quarter of 16 tokens, whose rows lie in 16 places)
+        // value, whose bf16 numbers it writes.  (Writes go eight lanes at a time and meet a bank twice; in an order of tokens in which none
+        // does they are no faster, 6.75 ms either way for the case above.)
         const int sub4 = lane & 15, part4 = lane >> 4;
         const uint32_t row4 = (uint32_t)(sub4 * kTokenBytes + 16 * part4), scale4 = (uint32_t)(kTileScales + part4 * kTileTokens + sub4);
         const uint32_t store_at = (uint32_t)((wave * 16 + sub4) * kRowBytes + (((4 * part4) ^ swizzle(sub4)) << 4));
@@ -293,10 +303,12 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
     } while (share && at < opaque64(until));
 }
 
-// Rows of split tiles: o = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p, M = max m_p.  A workgroup has 32 rows of a tile and some of the
+// Rows of tiles that several ranges share: o = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p, M = max m_p.  A workgroup has 32 rows of a tile and some of the
 // 16 groups of eight dimensions, its wavefronts a fourth of the pieces each, a lane four dimensions of a row, as the pieces left
 // them; the wavefronts' sums meet in LDS.
-constexpr int kMergeBatch = 16;  // pieces whose loads are in flight together
+// Pieces whose loads are in flight together; those of pieces that are not there are left out (all wavefronts at the last one's place
+// instead: 10 us where 64 pieces of 8 heads take 8, and 54 where a call of 9 pieces takes 37).
+constexpr int kMergeBatch = 16;
 __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptArgs a)
 {
     __shared__ __align__(16) f32x4_t sum[kWaves][64];
@@ -362,7 +374,7 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptArgs a)
             for (int i = 0; i < kMergeBatch; ++i) {
                 mls[i] = f32x2_t{-__builtin_inff(), 0.f};
                 os[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-                if (first + kWaves * i >= parts) continue;  // (the last one's place instead, by all wavefronts at once, is a crowd)
+                if (first + kWaves * i >= parts) continue;
                 const int64_t from = at(first + kWaves * i);
                 mls[i] = *(const LYCHEE_GLOBAL f32x2_t *)(a.part_ml + (from * 32 + (lane & 31)) * 2);
                 os[i] = *(const LYCHEE_GLOBAL f32x4_t *)(a.part_o + from * (64 * 64) + dj * 256 + 4 * lane);

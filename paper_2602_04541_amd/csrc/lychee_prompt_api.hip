@@ -32,7 +32,8 @@ int64_t ranges_of(int64_t blocks, int32_t smallest, int32_t n_kv_heads)  // what
     return most < fill ? most : fill;
 }
 // Whether lengths are possible with which a launch would share its tiles out (lay_line): a longest request against the least that
-// it and the others can have, of equal lengths and, in a cache, with no keys but their own.
+// it and the others can have, of equal lengths and, in a cache, with no keys but their own.  (To find out on the device, and a merge
+// with nothing to do, cost 7 us.)
 bool may_share(int32_t batch, int32_t heads, int32_t n_tokens, int64_t max_len, bool packed)
 {
     const float range = (float)heads / (float)(kPromptRows * kPromptSlots), own = 1.f / (2 * kPromptKeys);
