@@ -47,7 +47,7 @@ __device__ __forceinline__ uint4 decode8(uint32_t c, float scale)
                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3)));
 }
 
-// Eight neighbouring registers of a product's D as the B operand of the next.  The rounding to bf16 is one of 2^-9 of a
+// Eight neighbouring registers of a product's D as the B operand of the next.  The rounding to bf16 is one of 2^-8 of a
 // number at most, with either sign, like that of the output.
 template <int kFirst>
 __device__ __forceinline__ bf16x8_t operand(const f32x16_t &d)

@@ -223,6 +223,37 @@ def test_layouts_that_the_binding_takes(lb):
     assert says(lb, p0, "prompt_attn", a).startswith("lychee_prompt_attn failed")
 
 
+@pytest.mark.parametrize("method, cached", [("prompt_attn", False), ("prompt_attn", True), ("prompt_attn_backward", False)])
+def test_usual_and_unusual_layouts_go_on_alike(lb, monkeypatch, method, cached):
+    """One row: its stride to the next does not count, but the binding looks at such arguments one by one."""
+    H, Hkv = 8, 2
+    rows = half(1, 12, 128)
+    q, k, v = rows.split((H, Hkv, Hkv), 1)
+    if cached:
+        k, v = half(1, Hkv, 64, 128), half(1, Hkv, 64, 128)
+    p = lb.make_prompt(1, q, k)
+    grads = half(1, 12, 128).split((H, Hkv, Hkv), 1)
+    args = dict(q=q, k=k, v=v, token_start=ints(2), out=half(1, H, 128), lse=torch.zeros(H, 1), workspace=lb.alloc_prompt_workspace(p, "cpu"))
+    args.update(dict(lengths=ints(1) if cached else None) if method == "prompt_attn" else dict(zip(("dq", "dk", "dv"), grads), d_out=half(1, H, 128)))
+    passed = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: passed.append((name,) + a) or 0
+
+    monkeypatch.setattr(lb, "_lib", Library())
+    c = object.__new__(lb.Context)
+    c._h, c.device = None, -1
+    getattr(c, method)(p, stream=0, **args)
+    for name in ("q", "k", "dv"):
+        if name in args:
+            t = args[name]
+            odd = t.as_strided(t.shape, (t.stride(0) + 8,) + t.stride()[1:], t.storage_offset())
+            getattr(c, method)(p, stream=0, **dict(args, **{name: odd}))
+    assert len(passed) >= 3 and all(x == passed[0] for x in passed)
+    c._h = None
+
+
 # ------------------------------------------------------------------ the reference
 
 
