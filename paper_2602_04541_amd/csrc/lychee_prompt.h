@@ -13,6 +13,9 @@ constexpr int kPromptKeys = 64;           // keys a workgroup takes at a time
 // and of key tiles.
 constexpr int kPromptMinRange = 3;
 constexpr int kPromptMinKeyRange = 2;
+// Blocks of all key tiles that are one range, which needs no merge: 64 tokens of 8 heads, 8 KV heads, both passes 22 us, 25 with the merge; from
+// 8 blocks on one workgroup takes longer than ranges and their merge (100 tokens of 8 heads, 2 KV heads: 39 us, 32 in ranges).
+constexpr int kPromptOneRange = 4;
 // Rows' tiles are shared out where the longest has kPromptShareCost blocks more than kPromptShareSize times a range's (lay_line).
 constexpr int kPromptShareCost = 14;
 constexpr float kPromptShareSize = 1.6f;

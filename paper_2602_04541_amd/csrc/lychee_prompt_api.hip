@@ -61,7 +61,9 @@ Grid keys_grid(int32_t batch, int32_t n_kv_heads, int32_t group, int32_t n_token
 {
     Grid w;
     w.tiles = n_tokens / kPromptRows + (batch < n_tokens ? batch : n_tokens);
-    w.ranges = w.room = ranges_of(w.tiles * ((int64_t)n_tokens * group / kPromptKeys + 1), kPromptMinKeyRange, n_kv_heads);
+    const int64_t blocks = w.tiles * ((int64_t)n_tokens * group / kPromptKeys + 1);
+    w.room = ranges_of(blocks, kPromptMinKeyRange, n_kv_heads);
+    w.ranges = blocks <= kPromptOneRange ? 1 : w.room;
     return w;
 }
 

@@ -489,6 +489,7 @@ hipError_t launch_prompt_grad(const PromptGradArgs &a, hipStream_t stream)
         prompt_dq_kernel<false><<<(unsigned)a.n_row_tiles * heads, kThreads, 0, stream>>>(a);
     }
     prompt_dkv_kernel<<<(unsigned)a.n_key_ranges * heads, kThreads, 0, stream>>>(a);
+    if (a.n_key_ranges == 1) return hipGetLastError();  // (no tile lies in several)
     prompt_dkv_merge_kernel<<<(unsigned)a.n_key_records * heads * kWaves * 2, kThreads, 0, stream>>>(a);
     return hipGetLastError();
 }

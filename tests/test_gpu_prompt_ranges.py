@@ -55,6 +55,9 @@ SHARED = [  # few tiles, the longest longer than a fair share of all
     ([1, 1650, 40, 0], 2, 2, 0, 5),
     ([1300, 1290], 3, 3, 0, 0),
     ([2600], 6, 2, 0, 0),
+    ([16, 30], 1, 1, 0, 2),     # so few keys that they are one range, which needs no merge
+    ([20, 0, 1], 3, 1, 1, 0),
+    ([60, 5], 2, 2, 0, 0),
 ]
 
 
