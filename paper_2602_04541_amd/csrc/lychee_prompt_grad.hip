@@ -122,7 +122,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dq_kernel(PromptGradArgs a
         const int rows = w.n * p.group, row = w.tile * kPromptRows + wave * 32 + (lane & 31);
         const int row_in = min(row, rows - 1), pos = token_of(p, row_in), head = g * p.group + row_in - pos * p.group;
         const int lowest = token_of(p, min(w.tile * kPromptRows + wave * 32, rows - 1));
-        const int highest = token_of(p, min(w.tile * kPromptRows + wave * 32 + 31, rows - 1));
+        const int highest = w.tile * kPromptRows + wave * 32 < rows ? token_of(p, min(w.tile * kPromptRows + wave * 32 + 31, rows - 1)) : -1;  // (no rows: no products)
         const int64_t token = w.start + pos, packed = (token * (p.n_kv_heads * p.group) + head) * kHeadDim;
         const int64_t q_at = token * p.q_tok + (int64_t)head * p.q_head;
 
