@@ -413,8 +413,9 @@ int lychee_select_scores(lychee_ctx *ctx, const lychee_paged *paged, const float
  *     lychee_plan_pages numbers them.  token_start is int32 [batch + 1], in ascending order; values are clamped to
  *     [0, n_tokens].  A request may have no tokens.  Rows that belong to no request are left as they were.
  *   - Its keys are L_b in number, and its n_b query tokens are the last n_b of them: query i sits at position
- *     p = L_b - n_b + i and attends to the positions 0 .. p.  A query with p < 0 has nothing to attend to: its output
- *     is zero, its lse -infinity.
+ *     p = L_b - n_b + i and attends to the positions 0 .. p.  A query with p < 0 (or, in pages, no page to attend to) has
+ *     nothing to attend to: its output is zero, its lse -infinity.  One whose scores are all -infinity has output NaN,
+ *     lse -infinity.
  *   - Query head h uses KV head h / (n_q_heads / n_kv_heads), up to LYCHEE_PROMPT_MAX_GROUP query heads a KV head.
  *   - What a query does not see has no influence on its results, infinities and NaN included.
  *   - Softmax statistics and sums are fp32; weights, and dS in the backward pass, are rounded to bf16 for the matrix units.

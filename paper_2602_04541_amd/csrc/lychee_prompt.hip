@@ -30,6 +30,9 @@ namespace {
 // at 32 K to 61 K (7.00 with the block written behind them).
 constexpr int kAhead = 6;
 constexpr float kSlack = 8.f;    // powers of two by which a score may exceed the maximum that weights are measured against
+// The maximum of a row whose scores are all -infinity (sum 0, NaN), which is not taken for one that sees nothing (maximum -infinity; zero).
+constexpr float kLeast = -3.40282347e38f;
+__device__ __forceinline__ float factor(float m, float l) { return l != 0.f ? 1.f / l : m == -__builtin_inff() ? 0.f : __builtin_nanf(""); }
 
 struct SharedPrompt {
     __align__(16) uint8_t k[2][kBlockBytes];
@@ -284,10 +287,16 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
             careful = true;
         }
         l = sum_halves32(l);
+        if (l == 0.f) {  // (found out here, because a block's scores have no instruction to spare: 0.5 to 0.9 % of long calls)
+            bool sees = false;
+            for (int j = w.first * kPromptKeys; !sees && j <= min(pos, w.last * kPromptKeys - 1); j = ((j >> a.d.page_shift) + 1) << a.d.page_shift)
+                sees = !Q4 || (uint32_t)gload(a.table + (int64_t)w.b * a.d.table_stride + (j >> a.d.page_shift)) < (uint32_t)a.d.n_pages;
+            if (sees) m = kLeast;
+        }
         if (slot < 0) {
             const bool there = row < rows;
             uint16_t *out = a.out + ((int64_t)(w.start + token) * (p.n_kv_heads * p.group) + head) * kHeadDim;
-            store_row(there ? out : nullptr, lane, o, l == 0.f ? 0.f : 1.f / l);
+            store_row(there ? out : nullptr, lane, o, factor(m, l));
             if (a.lse && there && hi == 0)
                 gstore(a.lse + (int64_t)head * p.n_tokens + w.start + token, l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * (1.f / kLog2e));
         } else if (w.tile * kPromptRows + wave * 32 < rows) {
@@ -358,7 +367,7 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptArgs a)
             }
 #pragma unroll
             for (int i = 0; i < kMost; ++i) o += e[i] * os[i];
-            if (row < rows) store(dj, o, l == 0.f ? 0.f : 1.f / l);
+            if (row < rows) store(dj, o, factor(m, l));
         }
     };
     if (parts <= 2) return few(std::integral_constant<int, 2>{});
@@ -411,7 +420,7 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptArgs a)
                 o += e * sum[i][lane];
             }
             if (row < rows) {
-                store(dj, o, l == 0.f ? 0.f : 1.f / l);
+                store(dj, o, factor(m, l));
                 if (dj == 0) store_lse(top, l);
             }
         }

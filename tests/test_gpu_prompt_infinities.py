@@ -1,0 +1,77 @@
+"""Attention over prompts where scores or values are infinite: rows whose every score is -infinity are NaN, and not those that see nothing."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests import prompt_reference as R
+from tests.test_gpu_prompt import DEV, Packed, ctx, forward, host, ints, near, paged_case, q4  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def nothing_but_minus_infinity(out, lse, rows, heads):
+    assert torch.isnan(out[rows, heads]).all(), "rows whose scores are all -infinity"
+    assert (lse[heads, rows] == -math.inf).all()
+
+
+@pytest.mark.parametrize("n", [1, 50, 64, 130, 1500])
+def test_scores_that_are_all_minus_infinity(ctx, n):  # noqa: F811
+    """The last token's query is infinite in a dimension in which all keys are negative; one head of a KV head's two."""
+    s = Packed(81, [n, 9], 2, 1, 1, 1)
+    s.k[:, :, 7] = -s.k[:, :, 7].abs() - 0.5
+    clean, clean_lse, _, _ = forward(ctx, s)
+    s.q[n, 1, 7] = math.inf
+    out, lse, _, _ = forward(ctx, s)
+    nothing_but_minus_infinity(out, lse, n, 1)
+    out[n, 1], lse[1, n] = clean[n, 1], clean_lse[1, n]
+    assert torch.equal(out, clean) and torch.equal(lse, clean_lse)
+
+
+def test_rows_that_see_nothing_are_zero_whatever_their_query(ctx):  # noqa: F811
+    s = Packed(82, [7, 70, 3], 4, 2)
+    lens = [3, 66, 0]
+    k, v = (torch.randn((3, 2, 70, 128), device=DEV, generator=s.gen).bfloat16() for _ in range(2))
+    k[..., 7] = -k[..., 7].abs() - 0.5
+    s.q[:, :, 7] = math.inf
+    out, lse, _, _ = forward(ctx, s, ints(lens), k, v)
+    for b, n in enumerate(lens):
+        first, new = int(s.start[b]), s.new[b]
+        unseen = slice(first, first + new - n)
+        assert (out[unseen] == 0).all() and (lse[:, unseen] == -math.inf).all()
+        nothing_but_minus_infinity(out, lse, slice(first + new - n, first + new), slice(0, 4))
+
+
+@pytest.mark.parametrize("length", [60, 200, 5000])
+def test_scores_of_minus_infinity_among_others(ctx, length):  # noqa: F811
+    """Keys whose scores are -infinity have no weight, also where a row's first blocks hold no others."""
+    s = Packed(83, [3], 2, 1)
+    k, v = (torch.randn((1, 1, length, 128), device=DEV, generator=s.gen).bfloat16() for _ in range(2))
+    s.q[:, :, 5] = s.q[:, :, 5].abs() + 0.5
+    gone = torch.arange(length, device=DEV) < length - 17
+    gone[::11] = True
+    k[0, 0, gone, 5] = -math.inf
+    out, lse, _, _ = forward(ctx, s, ints([length]), k, v)
+    there = torch.nonzero(~gone).flatten()
+    K, V = host(k[0, 0, there]), host(v[0, 0, there])
+    for h in range(2):
+        pos = np.searchsorted(there.cpu().numpy(), length - 3 + np.arange(3), side="right") - 1   # (positions among the others)
+        want = R.head(host(s.q[:, h]), K, V, pos)
+        near(host(out[:, h]), want["out"], "out of head %d" % h)
+        near(host(lse[h]), want["lse"], "lse of head %d" % h)
+
+
+def test_minus_infinity_over_the_paged_cache(ctx):  # noqa: F811
+    """The same, a token and its neighbours; and where a row's every page is absent it sees nothing."""
+    lens, new = [100, 2500, 40], [4, 3, 2]
+    s, p, table, cache = paged_case(84, new, lens, 4, 2, 16)
+    cache.bytes[:, 3:2048:128] = (cache.bytes[:, 3:2048:128] & 0x0F) | 0xA0    # dimension 7 of every key: -1 times its scale
+    table[2] = -1
+    clean = q4(ctx, s, p, table, cache, lens)
+    s.q[:, :, 7] = math.inf
+    s.q[5, 2:, 7] = 1.0
+    ordinary = q4(ctx, s, p, table, cache, lens)
+    assert torch.isnan(ordinary[:5]).all() and torch.isnan(ordinary[6]).all() and torch.isnan(ordinary[5, :2]).all()
+    assert torch.isfinite(ordinary[5, 2:]).all()
+    assert (ordinary[7:] == 0).all() and (clean[7:] == 0).all()
