@@ -420,7 +420,7 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptArgs a)
                 o += e * sum[i][lane];
             }
             if (row < rows) {
-                store(dj, o, factor(m, l));
+                store(dj, o, factor(top, l));
                 if (dj == 0) store_lse(top, l);
             }
         }

@@ -75,3 +75,16 @@ def test_minus_infinity_over_the_paged_cache(ctx):  # noqa: F811
     assert torch.isnan(ordinary[:5]).all() and torch.isnan(ordinary[6]).all() and torch.isnan(ordinary[5, :2]).all()
     assert torch.isfinite(ordinary[5, 2:]).all()
     assert (ordinary[7:] == 0).all() and (clean[7:] == 0).all()
+
+
+@pytest.mark.parametrize("there", [0, 13, 150, 373])
+def test_minus_infinity_in_one_of_many_pieces(ctx, there):  # noqa: F811
+    """Rows over 6000 tokens of which a single page is there: merged from more than 16 pieces, of which one sees a key."""
+    s, p, table, cache = paged_case(88, [3], [6000], 1, 1, 16)
+    cache.bytes[:, 3:2048:128] = (cache.bytes[:, 3:2048:128] & 0x0F) | 0xA0
+    kept = table[0, there]
+    table[0, :] = -1
+    s.q[:, :, 7] = math.inf
+    assert (q4(ctx, s, p, table, cache, [6000]) == 0).all()
+    table[0, there] = kept
+    assert torch.isnan(q4(ctx, s, p, table, cache, [6000])).all()
