@@ -418,6 +418,8 @@ int lychee_select_scores(lychee_ctx *ctx, const lychee_paged *paged, const float
  *     lse -infinity.
  *   - Query head h uses KV head h / (n_q_heads / n_kv_heads), up to LYCHEE_PROMPT_MAX_GROUP query heads a KV head.
  *   - What a query does not see has no influence on its results, infinities and NaN included.
+ *     An infinite value or NaN that it does see reaches its output whatever its weight, one that rounds to zero included: the
+ *     output is infinite there, or NaN where it sees a NaN or infinities of both signs.
  *   - Softmax statistics and sums are fp32; weights, and dS in the backward pass, are rounded to bf16 for the matrix units.
  *   - A forward call enqueues one or two kernel launches, a backward call two to four (none for n_tokens = 0).  Calls may be
  *     captured and leave the caller's current device as it was; their launches are not timed by lychee_timing_enable.

@@ -158,15 +158,15 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
         float m, l;
         bool careful = false;
         for (;;) {
-            // Turns: a block each (with care three of them, take_with_care).
-            const int turns = (careful ? 3 : 1) * max(w.last - w.first, 0);
-            const auto block_of = [&](int turn) { return w.first + (careful ? turn / 3 : turn); };
-            const auto fetch = [&](int turn) {
-                const int blk = block_of(turn);
+            // Turns: a block each.  With care all blocks come three times (take_with_care): infinities are put back when all scores have been
+            // seen and no sum is rescaled any more, by a factor that might round to zero.
+            const int blocks = max(w.last - w.first, 0), turns = (careful ? 3 : 1) * blocks;
+            const auto after = [&](int blk) { return blk + 1 == w.last ? w.first : blk + 1; };
+            const auto fetch = [&](int blk, int turn) {
                 if constexpr (Q4) {
                     const bool there = load4(blk);
                     if (lane == 0) sh.bad[turn & 1][wave] = there ? 0 : 0xFFFF;
-                    entry = fetch_entry(block_of(min(turn + 1, turns - 1)));
+                    entry = fetch_entry(after(blk));
                 } else {
                     copy_rows(kb, blk, to_k + (turn & 1) * kBlockBytes);
                     copy_rows(vb, blk, to_v + (turn & 1) * kBlockBytes);
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
             l = 0.f;
             if (turns > 0) {
                 if (Q4) entry = fetch_entry(w.first);
-                fetch(0);
+                fetch(w.first, 0);
             }
             arrived(qf);
             if (turns > 0) {
@@ -192,15 +192,15 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
                 store_v(0);
                 arrive();
             }
-            for (int turn = 0; turn < turns; ++turn) {
-                const int j0 = block_of(turn) * kPromptKeys;
-                if (turn + 1 < turns) fetch(turn + 1);
+            for (int turn = 0, blk = w.first; turn < turns; ++turn, blk = after(blk)) {
+                const int j0 = blk * kPromptKeys;
+                if (turn + 1 < turns) fetch(after(blk), turn + 1);
                 if (careful || j0 <= highest) {
                     const LYCHEE_LDS uint8_t *K = (const LYCHEE_LDS uint8_t *)sh.k[turn & 1], *V = (const LYCHEE_LDS uint8_t *)sh.v[turn & 1];
                     const uint32_t kat = opaque(row_at), vat = opaque(turn_at);
-                    const bool again = careful && turn % 3 != 0;
+                    const bool again = careful && turn >= blocks;
                     if (__builtin_expect(careful, 0)) {
-                        take_with_care(sh.v[turn & 1], kBlockBytes, turn % 3);
+                        take_with_care(sh.v[turn & 1], kBlockBytes, turn / blocks);
                         __syncthreads();
                     }
                     f32x16_t z[2] = {zero16(), zero16()};
@@ -340,6 +340,23 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptArgs a)
         if (a.lse && lane < 32)
             gstore(a.lse + (int64_t)head * p.n_tokens + w.start + token, l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * (1.f / kLog2e));
     };
+    // A piece's infinity stays one, though its weight may round to zero: sums that are no numbers are made again.
+    const auto with_infinities = [&](f32x4_t o, int dj, float m) {
+        const auto no_number = [](float x) { return !(__builtin_fabsf(x) < __builtin_inff()); };
+        if (__builtin_expect(no_number(o[0]) || no_number(o[1]) || no_number(o[2]) || no_number(o[3]), 0)) {
+            f32x4_t again = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+            for (int i = 0; i < parts; ++i) {
+                const f32x4_t x = *(const LYCHEE_GLOBAL f32x4_t *)(a.part_o + at(i) * (64 * 64) + dj * 256 + 4 * lane);
+                const float e = fast_exp2(gload(a.part_ml + (at(i) * 32 + (lane & 31)) * 2) - (m == -__builtin_inff() ? 0.f : m));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) again[j] += (__builtin_isinf(x[j]) ? 1.f : e) * x[j];
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = no_number(o[j]) ? again[j] : o[j];
+        }
+        return o;
+    };
     // Few pieces: a wavefront has all of them of a group of dimensions.
     const auto few = [&](auto most) {
         constexpr int kMost = decltype(most)::value;
@@ -367,7 +384,7 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptArgs a)
             }
 #pragma unroll
             for (int i = 0; i < kMost; ++i) o += e[i] * os[i];
-            if (row < rows) store(dj, o, factor(m, l));
+            if (row < rows) store(dj, with_infinities(o, dj, m), factor(m, l));
         }
     };
     if (parts <= 2) return few(std::integral_constant<int, 2>{});
@@ -420,7 +437,7 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptArgs a)
                 o += e * sum[i][lane];
             }
             if (row < rows) {
-                store(dj, o, factor(top, l));
+                store(dj, with_infinities(o, dj, top), factor(top, l));
                 if (dj == 0) store_lse(top, l);
             }
         }

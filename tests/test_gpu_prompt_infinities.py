@@ -1,12 +1,14 @@
-"""Attention over prompts where scores or values are infinite: rows whose every score is -infinity are NaN, and not those that see nothing."""
+"""Attention over prompts where scores or values are infinite: rows whose every score is -infinity are NaN and not those that see nothing,
+and an infinite value that a row sees reaches its output however small its weight, whole, rescaled or merged."""
 import math
 
 import numpy as np
 import pytest
 import torch
 
+from tests import paged_reference as P
 from tests import prompt_reference as R
-from tests.test_gpu_prompt import DEV, Packed, ctx, forward, host, ints, near, paged_case, q4  # noqa: F401
+from tests.test_gpu_prompt import DEV, Packed, check_forward, ctx, forward, host, ints, near, paged_case, q4  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -88,3 +90,54 @@ def test_minus_infinity_in_one_of_many_pieces(ctx, there):  # noqa: F811
     assert (q4(ctx, s, p, table, cache, [6000]) == 0).all()
     table[0, there] = kept
     assert torch.isnan(q4(ctx, s, p, table, cache, [6000])).all()
+
+
+def steep(s, k, low, high):
+    """Queries and keys whose scores rise along the keys: low nats for the first, high for the last (rounded to bf16)."""
+    root = math.sqrt(128)
+    s.q[:, :, 0] = 16.0
+    n = k.shape[-2]
+    k[..., 0] = (torch.linspace(low, high, n, device=DEV) * root / 16).bfloat16()
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("new, length", [(3, 60), (3, 200), (70, 700), (2, 6000)])
+def test_infinite_values_of_small_weight(ctx, bad, new, length):  # noqa: F811
+    """Weights from e^-600 on: zero in 32 bits, not in the formula.  Rescaled within a range (from 65 keys on) and merged (6000)."""
+    s = Packed(85, [new], 2, 1, sharp=0.3)
+    k, v = (torch.randn((1, 1, length, 128), device=DEV, generator=s.gen).bfloat16() for _ in range(2))
+    steep(s, k, -300.0, 300.0)
+    v[0, 0, 2, 9] = bad
+    v[0, 0, length - new - 1, 40] = bad
+    out, lse, _, _ = forward(ctx, s, ints([length]), k, v)
+    check_forward(s, out, lse, R.Keys(1, lambda b, h: host(k[b, h])), R.Keys(1, lambda b, h: host(v[b, h])), [length])
+
+
+def test_infinite_values_of_both_signs(ctx):  # noqa: F811
+    s = Packed(86, [300], 1, 1, sharp=0.3)
+    steep(s, s.rows[:, 1:2].transpose(0, 1), -300.0, 300.0)
+    s.v[2, 0, 9], s.v[200, 0, 9] = math.inf, -math.inf
+    out, lse, _, _ = forward(ctx, s)
+    check_forward(s, out, lse, s.keys(s.k), s.keys(s.v), [300])
+    assert (out[2:200, 0, 9] == math.inf).all() and torch.isnan(out[200:, 0, 9]).all()
+
+
+def test_infinite_values_of_small_weight_in_the_paged_cache(ctx):  # noqa: F811
+    """A group under scale byte 255, which is NaN."""
+    lens, new = [2600], [2]
+    s, p, table, cache = paged_case(87, new, lens, 2, 1, 32)
+    s.q[:] = 0
+    s.q[:, :, 0] = 16.0
+    slots = P.slots_of(table[0], 2600, 32, p.n_pages)
+    for t in range(2600):   # dimension 0 of the key: 6 times the scale, the scale's sign and size along the keys
+        tile, r = cache._at(slots[t], 0)
+        cache.bytes[tile, r * 128] = (cache.bytes[tile, r * 128] & 0xF0) | (0xF if t < 1300 else 0x7)
+        cache.bytes[tile, 2048 + r] = 127 + (5 if 100 < t < 2500 else 6)
+    tile, r = cache._at(slots[10], 0)
+    cache.bytes[tile, 2048 + 5 * 16 + r] = 255
+    out = q4(ctx, s, p, table, cache, lens)
+    assert torch.isnan(out[:, :, 32:64]).all()
+    k, v = cache.rows(slots, 0)
+    want = R.prompt(host(s.q), R.Keys(1, lambda b, h: k), R.Keys(1, lambda b, h: v), s.start, lens)["out"]
+    near(host(out)[..., :32], want[..., :32], "out")
+    near(host(out)[..., 64:], want[..., 64:], "out")
