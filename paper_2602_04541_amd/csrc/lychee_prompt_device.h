@@ -465,14 +465,15 @@ __device__ __forceinline__ void take_with_care(uint8_t *block, int bytes, int tu
         *at = to;
     }
 }
-// The pairs that count, of step s in the order of read_turned: rows least .. most of the block's.
-__device__ __forceinline__ bf16x8_t seen_rows(int hi, int s, int least, int most)
+// The pairs that count, of step s in the order of read_turned: rows least .. most of the block's.  Weights that are not positive, dS of an
+// infinite key, are 0 or no number, and make NaN of its infinities: turn 1 twice, the second time with `largest` negative.
+__device__ __forceinline__ bf16x8_t seen_rows(int hi, int s, int least, int most, uint32_t largest = kLargest)
 {
     u32x4_t u;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
         const int row = 16 * s + 4 * hi + (w & 1) * 2 + (w >> 1) * 8;
-        u[w] = (row >= least && row <= most ? kLargest : 0u) | (row + 1 >= least && row + 1 <= most ? kLargest << 16 : 0u);
+        u[w] = (row >= least && row <= most ? largest : 0u) | (row + 1 >= least && row + 1 <= most ? largest << 16 : 0u);
     }
     return __builtin_bit_cast(bf16x8_t, u);
 }

@@ -89,7 +89,8 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dq_kernel(PromptGradArgs a
     Tile w;
     Line line;
     bool share = false;
-    int64_t at = 0, until = 0, slot = -1;
+    int64_t at = 0, until = 0;
+    int slot = -1;
     const int range = blockIdx.x / p.n_kv_heads;
     if (SHARE) {
         line = lay_line<kLineRows>(p, a.one_row_range, sh.line);
@@ -114,7 +115,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dq_kernel(PromptGradArgs a
             const int blocks = w.last;
             w.first = cut_at(from, k.weight, blocks);
             w.last = cut_at(to, k.weight, blocks);
-            slot = from == 0 && to == k.weight ? -1 : part_slot(range, from == 0, p.n_kv_heads, g);
+            slot = from == 0 && to == k.weight ? -1 : (int)part_slot(range, from == 0, p.n_kv_heads, g);
             if (from == 0 && g == 0) record_tile(a.records, a.n_row_records, a.rows_by_number, line, k, range, to == k.weight);
             at += to - from;
         }
@@ -219,11 +220,11 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dq_kernel(PromptGradArgs a
                         bf16x8_t ds[2] = {operand<0>(z), operand<8>(z)};
                         if (__builtin_expect(careful, 0)) {
                             __syncthreads();
-                            take_with_care(sh.a[buf], kBlockBytes, turn / 2 % 3);
+                            take_with_care(sh.a[buf], kBlockBytes, min(turn / 2 % 3, 1));
                             __syncthreads();
                             if (turn / 2 % 3 != 0) {
 #pragma unroll
-                                for (int s = 0; s < 2; ++s) ds[s] = seen_rows(hi, 2 * x + s, 0, pos - j0);
+                                for (int s = 0; s < 2; ++s) ds[s] = seen_rows(hi, 2 * x + s, 0, pos - j0, turn / 2 % 3 == 1 ? kLargest : 0x8000u | kLargest);
                             }
 #pragma unroll
                             for (int i = 0; i < kAheadTurned; ++i) turned[i] = read_second(i);
@@ -246,7 +247,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dq_kernel(PromptGradArgs a
         if (slot < 0) {
             store_row(row < rows ? a.dq + q_at : nullptr, lane, dq, a.scale);
         } else {
-            float *to = a.part + (slot * kWaves + wave) * (kPartFloats / 2) + 4 * lane;
+            float *to = a.part + (int64_t)(slot * kWaves + wave) * (kPartFloats / 2) + 4 * lane;
 #pragma unroll
             for (int db = 0; db < 4; ++db)
 #pragma unroll

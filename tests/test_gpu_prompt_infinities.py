@@ -8,7 +8,7 @@ import torch
 
 from tests import paged_reference as P
 from tests import prompt_reference as R
-from tests.test_gpu_prompt import DEV, Packed, check_forward, ctx, forward, host, ints, near, paged_case, q4  # noqa: F401
+from tests.test_gpu_prompt import DEV, Packed, backward, check_forward, ctx, forward, host, ints, near, one_like, paged_case, q4  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -141,3 +141,53 @@ def test_infinite_values_of_small_weight_in_the_paged_cache(ctx):  # noqa: F811
     want = R.prompt(host(s.q), R.Keys(1, lambda b, h: k), R.Keys(1, lambda b, h: v), s.start, lens)["out"]
     near(host(out)[..., :32], want[..., :32], "out")
     near(host(out)[..., 64:], want[..., 64:], "out")
+
+
+@pytest.mark.parametrize("n", [90, 1500])
+def test_gradients_of_rows_whose_scores_are_all_minus_infinity(ctx, n):  # noqa: F811
+    """Such a row has no gradient (NaN), and neither have the keys that it sees; other heads and requests keep theirs."""
+    s = Packed(89, [n, 70], 4, 2, sharp=1.2)
+    s.k[:, :, 7] = -s.k[:, :, 7].abs() - 0.5
+    g = one_like(s)
+    out, lse, p, ws = forward(ctx, s)
+    clean = backward(ctx, s, p, out, lse, ws, g)
+    at = n // 2
+    s.q[at, 1, 7] = math.inf
+    out, lse, p, ws = forward(ctx, s)
+    got = backward(ctx, s, p, out, lse, ws, g)
+    (dq, dk, dv), (cq, ck, cv) = (x.split((4, 2, 2), 1) for x in (got, clean))
+    assert torch.isnan(dq[at, 1]).all()
+    dq[at, 1] = cq[at, 1]
+    assert torch.equal(dq, cq)
+    for x, y in ((dk, ck), (dv, cv)):
+        assert torch.isnan(x[:at + 1, 0]).all()
+        assert torch.equal(x[at + 1:], y[at + 1:]) and torch.equal(x[:, 1], y[:, 1])
+
+
+@pytest.mark.parametrize("n, at", [(90, 10), (90, 64), (200, 3), (1500, 700)])
+def test_gradients_of_keys_whose_scores_are_minus_infinity(ctx, n, at):  # noqa: F811
+    """A key with an infinity has no weight and no gradient; for the rows that see it, dq is 0 times infinity there, which is NaN, and as
+    without the key elsewhere."""
+    s = Packed(90, [n], 2, 1, sharp=1.2)
+    s.q[:, :, 9] = s.q[:, :, 9].abs() + 0.5
+    s.k[at, 0, 9] = -math.inf
+    g = one_like(s)
+    out, lse, p, ws = forward(ctx, s)
+    got = backward(ctx, s, p, out, lse, ws, g)
+    dq, dk, dv = (host(x) for x in got.split((2, 1, 1), 1))
+    assert np.isfinite(dq[:at]).all() and np.isnan(dq[at:, :, 9]).all()
+    assert (dk[at] == 0).all() and (dv[at] == 0).all()
+    others = np.arange(n) != at
+    K, V = (x[:, 0].double()[torch.from_numpy(others).to(DEV)] for x in (s.k, s.v))
+    pos = torch.arange(n, device=DEV) - (torch.arange(n, device=DEV) >= at).long()    # (positions among the others)
+    dims = np.arange(128) != 9
+    wk = wv = 0
+    for h in range(2):
+        want = R.dense(s.q[:, h].double(), K, V, pos, g[:, h].double())
+        value, off = (x.cpu().numpy() for x in want["dq"])
+        near(dq[:, h][:, dims], (value[:, dims], off[:, dims]), "dq of head %d" % h)
+        near(dq[:at, h], (value[:at], off[:at]), "dq of head %d" % h)
+        wk, wv = (a + np.stack([x.cpu().numpy() for x in want[name]]) for a, name in ((wk, "dk"), (wv, "dv")))
+    for name, got, want in (("dk", dk, wk), ("dv", dv, wv)):
+        want[1] += R.U * np.abs(want[0])
+        near(got[others, 0], tuple(want), name)
