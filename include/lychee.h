@@ -460,8 +460,8 @@ int lychee_prompt_attn(lychee_ctx *ctx, const lychee_prompt *prompt, const void 
                        size_t workspace_bytes, void *hip_stream);
 
 /* Its gradient for packed sequences: d_out and out bf16 [n_tokens][H_q][128], out and lse as the call above wrote them; dq
- * strided like q, dk and dv like k and v, summed over the query heads of a KV head.  Heads must not share rows
- * (strides of heads >= 128).  Gradients are written, not added to; rows of no request are left as they were. */
+ * strided like q, dk and dv like k and v, summed over the query heads of a KV head.  No two rows (of a token and a head)
+ * may have an element in common: EINVAL.  Gradients are written, not added to; rows of no request are left as they were. */
 int lychee_prompt_attn_backward(lychee_ctx *ctx, const lychee_prompt *prompt, const void *d_out, const void *q,
                                 const void *k, const void *v, const void *out, const float *lse,
                                 const int32_t *token_start, void *dq, void *dk, void *dv, void *workspace,

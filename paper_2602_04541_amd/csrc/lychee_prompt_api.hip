@@ -103,6 +103,19 @@ int check_prompt(const lychee_prompt *p)
     return LYCHEE_OK;
 }
 
+// Whether two rows, of tokens `tok` and heads `head` elements apart, have an element in common.
+bool rows_meet(int64_t n_tokens, int64_t tok, int64_t n_heads, int64_t head)
+{
+    if (n_tokens == 0) return false;
+    if ((n_tokens > 1 && tok < kHeadDim) || (n_heads > 1 && head < kHeadDim)) return true;
+    if (n_tokens == 1 || n_heads == 1 || head >= (n_tokens - 1) * tok + kHeadDim || tok >= (n_heads - 1) * head + kHeadDim) return false;
+    for (int64_t h = 1; h < n_heads; ++h) {  // head h of a token against the other tokens' first heads
+        const int64_t t = h * head / tok, over = h * head - t * tok;
+        if ((t > 0 && t < n_tokens && over < kHeadDim) || (t + 1 < n_tokens && tok - over < kHeadDim)) return true;
+    }
+    return false;
+}
+
 // (for either kind of keys: the longer request that a batch may hold)
 CarvedPrompt carve(const lychee_prompt &p)
 {
@@ -200,6 +213,9 @@ int lychee_prompt_attn_backward(lychee_ctx *ctx, const lychee_prompt *prompt, co
     if (rc != LYCHEE_OK) return rc;
     const lychee_prompt &p = *prompt;
     if (!token_start || !aligned(token_start, 4) || !aligned(lse, 4)) return LYCHEE_EINVAL;
+    // gradients of rows that meet would be written by several workgroups
+    if (rows_meet(p.n_tokens, p.q_stride_tok, p.n_q_heads, p.q_stride_head) || rows_meet(p.n_tokens, p.kv_stride_tok, p.n_kv_heads, p.kv_stride_head))
+        return LYCHEE_EINVAL;
     const CarvedPrompt c = carve(p);
     if ((rc = check_workspace(workspace, workspace_bytes, c)) != LYCHEE_OK) return rc;
     if (p.n_tokens == 0) return LYCHEE_OK;
@@ -207,8 +223,6 @@ int lychee_prompt_attn_backward(lychee_ctx *ctx, const lychee_prompt *prompt, co
     if (!aligned(d_out, 16) || !aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16) || !aligned(dq, 16) ||
         !aligned(dk, 16) || !aligned(dv, 16))
         return LYCHEE_EINVAL;
-    // heads that share rows would share their gradients' too
-    if ((p.n_q_heads > 1 && p.q_stride_head < kHeadDim) || (p.n_kv_heads > 1 && p.kv_stride_head < kHeadDim)) return LYCHEE_EINVAL;
     if (still_read(ctx, workspace)) return LYCHEE_EINVAL;
     const OnDevice dev(ctx);
     if (!dev.ok) return LYCHEE_EHIP;

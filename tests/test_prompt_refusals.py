@@ -1,0 +1,63 @@
+"""Calls of attention over prompts that are refused on the host, without a GPU.  Calls that would be accepted are made without a
+workspace, which is what they are refused for then: nothing is launched, and no context looked into."""
+import itertools
+
+import pytest
+import torch
+
+from tests.test_prompt_host import lb, refused, shape  # noqa: F401
+
+BACKWARD = "lychee_prompt_attn_backward"
+
+
+def rows_meet(tokens, tok, heads, head):
+    """Whether two of the rows [i * tok + h * head, + 128) have an element in common."""
+    at = sorted(i * tok + h * head for i, h in itertools.product(range(tokens), range(heads)))
+    return any(b - a < 128 for a, b in zip(at, at[1:]))
+
+
+@pytest.mark.parametrize("tokens, tok, head", [
+    (9, 1024, 128),            # as a projection leaves them
+    (9, 1536, 128),
+    (9, 128, 9 * 128),         # head after head
+    (9, 160, 9 * 160),
+    (9, 128, 128),             # every token's head where the next token's is
+    (9, 128, 256),
+    (9, 256, 128),
+    (9, 896, 128),             # one head short of a row's
+    (9, 1016, 128),            # eight elements short of it
+    (9, 128, 8 * 128),         # one token short of a head's
+    (9, 136, 136 * 8 + 120),
+    (1, 128, 128),             # a single token
+    (2, 128, 128),
+    (2, 1000 * 8, 136),
+    (3, 256, 384),             # rows that meet though neither stride holds all of the other's
+    (2, 384, 256),
+    (3, 16 * 128, 3 * 128),
+    (5, 3 * 128, 5 * 128),     # and that do not
+    (9, 128, 1 << 24),
+    (0, 128, 128),
+])
+def test_gradients_whose_rows_meet_are_refused(lb, tokens, tok, head):  # noqa: F811
+    """They would be written by several workgroups at once."""
+    meet = rows_meet(tokens, tok, 8, head)
+    p = shape(lb, n_tokens=tokens, q_stride_tok=tok, q_stride_head=head, kv_stride_tok=4096)
+    assert refused(lb, BACKWARD, p, ws=None) == (lb.EINVAL if meet else lb.EWORKSPACE)
+    assert refused(lb, "lychee_prompt_attn", p, ws=None) == lb.EWORKSPACE      # (reading them is no harm)
+    p = shape(lb, n_q_heads=32, n_kv_heads=8, n_tokens=tokens, q_stride_tok=32 * 128, kv_stride_tok=tok, kv_stride_head=head)
+    assert refused(lb, BACKWARD, p, ws=None) == (lb.EINVAL if meet else lb.EWORKSPACE)
+    if meet:
+        assert refused(lb, BACKWARD, p) == lb.EINVAL
+
+
+def test_rows_that_meet_against_all_pairs(lb):  # noqa: F811
+    for tokens, tok, head in itertools.product((2, 3, 7), range(128, 1200, 72), range(128, 1200, 56)):
+        p = shape(lb, n_tokens=tokens, q_stride_tok=tok, q_stride_head=head, kv_stride_tok=4096)
+        want = lb.EINVAL if rows_meet(tokens, tok, 8, head) else lb.EWORKSPACE
+        assert refused(lb, BACKWARD, p, ws=None) == want, (tokens, tok, head)
+
+
+def test_strides_of_key_heads_of_any_size(lb):  # noqa: F811
+    for head in (1 << 40, 1 << 60, (1 << 63) - 8):
+        p = shape(lb, kv_stride_tok=128, kv_stride_head=head)
+        assert refused(lb, BACKWARD, p, ws=None) == lb.EWORKSPACE
