@@ -424,7 +424,8 @@ int lychee_select_scores(lychee_ctx *ctx, const lychee_paged *paged, const float
  *   - A forward call enqueues one or two kernel launches, a backward call two to four (none for n_tokens = 0).  Calls may be
  *     captured and leave the caller's current device as it was; their launches are not timed by lychee_timing_enable.
  *     Results do not depend on the order in which workgroups run: the same call gives the same bits.
- *   - What a call writes must not overlap what it reads (views that share rows of a fused projection do not overlap).
+ *   - What a call writes must not overlap what it reads, nor the rest of what it writes (views that share rows of a fused
+ *     projection do not overlap).  The same address for an output and another argument is refused: EINVAL.
  *   - The workspace is scratch (256-byte aligned, contents don't care).  One that is large enough for a call is large enough
  *     for every call with the same heads and no more requests, tokens and max_len.  Calls that run at the same time need one each.
  * ========================================================================================== */

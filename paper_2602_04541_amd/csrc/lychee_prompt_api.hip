@@ -147,6 +147,16 @@ int check_workspace(const void *workspace, size_t bytes, const CarvedPrompt &c)
     return workspace == nullptr || !aligned(workspace, 256) || bytes < c.total ? LYCHEE_EWORKSPACE : LYCHEE_OK;
 }
 
+// Whether the first `written` of these addresses (NULL: left out) are no other argument's.
+template <size_t N>
+bool apart(const void *const (&at)[N], size_t written)
+{
+    for (size_t i = 0; i < written; ++i)
+        for (size_t j = i + 1; j < N; ++j)
+            if (at[i] != nullptr && at[i] == at[j]) return false;
+    return true;
+}
+
 // A pending select still reads its workspace.
 bool still_read(const lychee_ctx *ctx, const void *workspace) { return ctx->pending.active && ctx->pending.workspace == workspace; }
 
@@ -186,6 +196,7 @@ int lychee_prompt_attn(lychee_ctx *ctx, const lychee_prompt *prompt, const void 
     if ((rc = check_workspace(workspace, workspace_bytes, c)) != LYCHEE_OK) return rc;
     if (p.n_tokens == 0) return LYCHEE_OK;
     if (!q || !k || !v || !out || !aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16)) return LYCHEE_EINVAL;
+    if (!apart({out, lse, workspace, q, k, v, token_start, lengths}, 3)) return LYCHEE_EINVAL;
     if (still_read(ctx, workspace)) return LYCHEE_EINVAL;
     const OnDevice dev(ctx);
     if (!dev.ok) return LYCHEE_EHIP;
@@ -223,6 +234,7 @@ int lychee_prompt_attn_backward(lychee_ctx *ctx, const lychee_prompt *prompt, co
     if (!aligned(d_out, 16) || !aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16) || !aligned(dq, 16) ||
         !aligned(dk, 16) || !aligned(dv, 16))
         return LYCHEE_EINVAL;
+    if (!apart({dq, dk, dv, workspace, d_out, q, k, v, out, lse, token_start}, 4)) return LYCHEE_EINVAL;
     if (still_read(ctx, workspace)) return LYCHEE_EINVAL;
     const OnDevice dev(ctx);
     if (!dev.ok) return LYCHEE_EHIP;
@@ -290,6 +302,7 @@ int lychee_q4_prompt_attn(lychee_ctx *ctx, const lychee_paged *paged, const void
     if ((rc = check_workspace(workspace, workspace_bytes, c)) != LYCHEE_OK) return rc;
     if (n_tokens == 0) return LYCHEE_OK;
     if (!q || !out || !aligned(q, 16) || !aligned(out, 16)) return LYCHEE_EINVAL;
+    if (!apart({out, workspace, q, cache, block_table, lengths, token_start}, 2)) return LYCHEE_EINVAL;
     if (still_read(ctx, workspace)) return LYCHEE_EINVAL;
     const OnDevice dev(ctx);
     if (!dev.ok) return LYCHEE_EHIP;

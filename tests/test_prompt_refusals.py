@@ -5,7 +5,7 @@ import itertools
 import pytest
 import torch
 
-from tests.test_prompt_host import lb, refused, shape  # noqa: F401
+from tests.test_prompt_host import lb, paged, refused, shape  # noqa: F401
 
 BACKWARD = "lychee_prompt_attn_backward"
 
@@ -61,3 +61,29 @@ def test_strides_of_key_heads_of_any_size(lb):  # noqa: F811
     for head in (1 << 40, 1 << 60, (1 << 63) - 8):
         p = shape(lb, kv_stride_tok=128, kv_stride_head=head)
         assert refused(lb, BACKWARD, p, ws=None) == lb.EWORKSPACE
+
+
+# Arguments at addresses of their own, 16 MiB apart (made up: a refused call touches none of them).
+OUTPUTS = {
+    "lychee_prompt_attn": ("out lse", "q k v start lengths"),
+    BACKWARD: ("dq dk dv", "d_out q k v out lse start"),
+    "lychee_q4_prompt_attn": ("out", "q cache table lengths start"),
+}
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="an accepted call would be launched")
+@pytest.mark.parametrize("name", sorted(OUTPUTS))
+def test_outputs_at_the_address_of_another_argument_are_refused(lb, name):  # noqa: F811
+    outputs, inputs = (x.split() for x in OUTPUTS[name])
+    apart = {arg: (i + 1) << 24 for i, arg in enumerate(outputs + inputs)}
+    p = paged(lb) if "q4" in name else shape(lb)
+    ws = 1 << 30
+    assert refused(lb, name, p, ws=ws, **apart) == lb.EHIP     # (taken, and no device to launch on)
+    for i, out in enumerate(outputs):
+        for other in outputs[:i] + inputs:
+            assert refused(lb, name, p, ws=ws, **dict(apart, **{out: apart[other]})) == lb.EINVAL, (out, other)
+        assert refused(lb, name, p, ws=apart[out], **apart) == lb.EINVAL, (out, "workspace")
+    for arg in inputs:
+        assert refused(lb, name, p, ws=apart[arg], **apart) == lb.EINVAL, (arg, "workspace")
+    if name == BACKWARD:                                       # what is only read may be the same
+        assert refused(lb, name, p, ws=ws, **dict(apart, d_out=apart["out"], q=apart["out"])) == lb.EHIP
