@@ -470,7 +470,8 @@ int lychee_prompt_attn_backward(lychee_ctx *ctx, const lychee_prompt *prompt, co
 
 /* The same attention over the paged 4-bit cache, for the pieces of prompts (and single tokens) that lychee_plan_pages
  * gave slots to and lychee_q4_append has written: lengths as after the step (lengths_out), token_start as planned.
- * Tokens whose table entry is no page are left out.  q strided like above, out bf16 [n_tokens][H_q][128]. */
+ * Tokens whose table entry is no page are left out.  q strided like above, out bf16 [n_tokens][H_q][128].
+ * lychee_q4_prompt_workspace_bytes is 0 for sizes that the call refuses. */
 size_t lychee_q4_prompt_workspace_bytes(const lychee_paged *paged, int32_t n_tokens);
 int lychee_q4_prompt_attn(lychee_ctx *ctx, const lychee_paged *paged, const void *q, int64_t q_stride_tok,
                           int64_t q_stride_head, int32_t n_tokens, const void *cache, const int32_t *block_table,

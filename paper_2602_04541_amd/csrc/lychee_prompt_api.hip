@@ -116,6 +116,20 @@ bool rows_meet(int64_t n_tokens, int64_t tok, int64_t n_heads, int64_t head)
     return false;
 }
 
+// The sizes of a call over the paged cache, and the tiles of its rows.
+int check_q4(const lychee_paged *paged, int32_t n_tokens, Grid *rows)
+{
+    int rc = lychee_check_paged(paged, nullptr, 1);
+    if (rc != LYCHEE_OK) return rc;
+    const lychee_paged &p = *paged;
+    if (n_tokens < 0) return LYCHEE_EINVAL;
+    if ((rc = check_heads_of(p.n_q_heads, p.n_kv_heads, p.head_dim)) != LYCHEE_OK) return rc;
+    const int32_t G = p.n_q_heads / p.n_kv_heads;
+    if ((int64_t)n_tokens * G >= kPromptMaxRows) return LYCHEE_EUNSUPPORTED;
+    *rows = rows_grid(p.batch, p.n_kv_heads, G, n_tokens, (int64_t)p.max_pages * p.page_size, false);
+    return rows->tiles * p.n_kv_heads >= kMaxGrid ? LYCHEE_EUNSUPPORTED : LYCHEE_OK;
+}
+
 // (for either kind of keys: the longer request that a batch may hold)
 CarvedPrompt carve(const lychee_prompt &p)
 {
@@ -274,10 +288,8 @@ int lychee_prompt_attn_backward(lychee_ctx *ctx, const lychee_prompt *prompt, co
 
 size_t lychee_q4_prompt_workspace_bytes(const lychee_paged *paged, int32_t n_tokens)
 {
-    if (lychee_check_paged(paged, nullptr, 1) != LYCHEE_OK || n_tokens < 0) return 0;
-    const int32_t G = paged->n_q_heads / paged->n_kv_heads;
-    if (G > kPromptMaxGroup || (int64_t)n_tokens * G >= kPromptMaxRows) return 0;
-    return carve(rows_grid(paged->batch, paged->n_kv_heads, G, n_tokens, (int64_t)paged->max_pages * paged->page_size, false), paged->n_kv_heads, 0, 0).total;
+    Grid w;
+    return check_q4(paged, n_tokens, &w) == LYCHEE_OK ? carve(w, paged->n_kv_heads, 0, 0).total : 0;
 }
 
 int lychee_q4_prompt_attn(lychee_ctx *ctx, const lychee_paged *paged, const void *q, int64_t q_stride_tok, int64_t q_stride_head,
@@ -285,16 +297,12 @@ int lychee_q4_prompt_attn(lychee_ctx *ctx, const lychee_paged *paged, const void
                           const int32_t *token_start, void *out, void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     if (ctx == nullptr) return LYCHEE_EINVAL;
-    int rc = lychee_check_paged(paged, nullptr, 1);
+    Grid w;
+    int rc = check_q4(paged, n_tokens, &w);
     if (rc != LYCHEE_OK) return rc;
     const lychee_paged &p = *paged;
-    if (n_tokens < 0) return LYCHEE_EINVAL;
-    if ((rc = check_heads_of(p.n_q_heads, p.n_kv_heads, p.head_dim)) != LYCHEE_OK) return rc;
-    const int32_t G = p.n_q_heads / p.n_kv_heads, max_len = p.max_pages * p.page_size;
-    if ((int64_t)n_tokens * G >= kPromptMaxRows || q_stride_tok > kPromptMaxStride || q_stride_head > kPromptMaxStride) return LYCHEE_EUNSUPPORTED;
+    if (q_stride_tok > kPromptMaxStride || q_stride_head > kPromptMaxStride) return LYCHEE_EUNSUPPORTED;
     if (!good_stride(q_stride_tok) || !good_stride(q_stride_head) || q_stride_tok < kHeadDim) return LYCHEE_EINVAL;
-    const Grid w = rows_grid(p.batch, p.n_kv_heads, G, n_tokens, max_len, false);
-    if (w.tiles * p.n_kv_heads >= kMaxGrid) return LYCHEE_EUNSUPPORTED;
     if (!cache || !block_table || !lengths || !token_start || !aligned(cache, 128) || !aligned(block_table, 4) || !aligned(lengths, 4) ||
         !aligned(token_start, 4))
         return LYCHEE_EINVAL;
@@ -308,7 +316,7 @@ int lychee_q4_prompt_attn(lychee_ctx *ctx, const lychee_paged *paged, const void
     if (!dev.ok) return LYCHEE_EHIP;
     PromptArgs a;
     memset(&a, 0, sizeof a);
-    a.r = rows_of(p.batch, p.n_q_heads, p.n_kv_heads, n_tokens, max_len, q_stride_tok, q_stride_head, token_start, lengths);
+    a.r = rows_of(p.batch, p.n_q_heads, p.n_kv_heads, n_tokens, p.max_pages * p.page_size, q_stride_tok, q_stride_head, token_start, lengths);
     a.q = static_cast<const uint16_t *>(q);
     a.cache = static_cast<const uint8_t *>(cache);
     a.table = block_table;

@@ -87,3 +87,19 @@ def test_outputs_at_the_address_of_another_argument_are_refused(lb, name):  # no
         assert refused(lb, name, p, ws=apart[arg], **apart) == lb.EINVAL, (arg, "workspace")
     if name == BACKWARD:                                       # what is only read may be the same
         assert refused(lb, name, p, ws=ws, **dict(apart, d_out=apart["out"], q=apart["out"])) == lb.EHIP
+
+
+@pytest.mark.parametrize("kv_heads, group, n", [(64, 4, 1 << 25), (64, 1, 1 << 26), (8, 16, 1 << 24), (8, 17, 9), (1, 4, 1 << 26)])
+def test_sizes_without_a_workspace_are_those_that_are_refused(lb, kv_heads, group, n):  # noqa: F811
+    """More tokens, heads or workgroups than a call over the paged cache takes: no size, and no buffer."""
+    p = paged(lb, n_q_heads=kv_heads * group, n_kv_heads=kv_heads)
+    name = "lychee_q4_prompt_attn"
+    assert refused(lb, name, p, n=n, tok=1 << 20, ws=None) == lb.EUNSUPPORTED
+    assert lb.q4_prompt_workspace_bytes(p, n) == 0
+    with pytest.raises(lb.LycheeError) as e:
+        lb.alloc_q4_prompt_workspace(p, n, "cpu")
+    assert e.value.code == lb.EUNSUPPORTED
+    fewer = max(1, n >> 3) if group <= 16 else 0
+    if fewer:
+        assert refused(lb, name, p, n=fewer, tok=1 << 20, ws=None) == lb.EWORKSPACE
+        assert lb.q4_prompt_workspace_bytes(p, fewer) > 0
