@@ -64,6 +64,9 @@ class Paged(ctypes.Structure):
                 ("k", ctypes.c_int32)]
 
 
+_MAX_STRIDE = 1 << 24  # of tokens and query heads, as lychee.h has it
+
+
 class Prompt(ctypes.Structure):
     """Mirror of `lychee_prompt`."""
     _fields_ = [("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
@@ -217,14 +220,22 @@ def paged_workspace_bytes(paged: Paged) -> int:
     return int(_lib.lychee_paged_workspace_bytes(ctypes.byref(paged)))
 
 
+def _stride(t: torch.Tensor, dim: int, least: int, packed: int) -> int:
+    """A tensor's stride; that of a dimension of one entry is any number, also one that the library does not take: `packed` then."""
+    stride = t.stride(dim)
+    return stride if t.shape[dim] > 1 or (stride % 8 == 0 and least <= stride <= _MAX_STRIDE) else packed
+
+
 def make_prompt(batch: int, q: torch.Tensor, kv: torch.Tensor) -> Prompt:
     """A `lychee_prompt` for q [n_tokens, H_q, 128] and keys (and values) like kv: [n_tokens, H_kv, 128], packed like q, or a cache
     [B, H_kv, L_cap, 128]; sizes and strides are theirs."""
+    (T, heads, d), n_kv = q.shape, kv.shape[1]
     if kv.dim() == 4:
-        n_kv, max_len, strides = kv.shape[1], kv.shape[2], (kv.stride(0), kv.stride(1), kv.stride(2))
+        max_len, of_rows = kv.shape[2], _stride(kv, 2, d, d)
+        strides = (_stride(kv, 0, 0, n_kv * max_len * d), _stride(kv, 1, 0, max_len * d), of_rows)
     else:
-        n_kv, max_len, strides = kv.shape[1], 0, (0, kv.stride(1), kv.stride(0))
-    return Prompt(batch, q.shape[1], n_kv, q.shape[2], q.shape[0], max_len, q.stride(0), q.stride(1), *strides)
+        max_len, strides = 0, (0, _stride(kv, 1, 0, d), _stride(kv, 0, d, n_kv * d))
+    return Prompt(batch, heads, n_kv, d, T, max_len, _stride(q, 0, d, heads * d), _stride(q, 1, 0, d), *strides)
 
 
 def check_prompt(prompt: Prompt) -> int:
@@ -672,6 +683,8 @@ class Context:
         device, B, heads, d, pages, width = self.device, paged.batch, paged.n_q_heads, paged.head_dim, paged.n_pages, paged.table_stride
         try:
             n, strides = q.shape[0], q.stride()
+            if n == 1 or heads == 1:
+                strides = (_stride(q, 0, d, heads * d), _stride(q, 1, 0, d)) + strides[2:]
             fine = (q.dtype is out.dtype is _BF16 and lengths.dtype is token_start.dtype is block_table.dtype is _I32
                     and cache.element_size() == 1
                     and q.get_device() == cache.get_device() == block_table.get_device() == lengths.get_device() == token_start.get_device()
@@ -689,7 +702,7 @@ class Context:
         else:
             call = "lychee_q4_prompt_attn"
             n = q.shape[0] if isinstance(q, torch.Tensor) and q.dim() == 3 else 0
-            strides = (q.stride(0), q.stride(1), 1) if n else (d, 0, 1)
+            strides = (_stride(q, 0, d, heads * d), _stride(q, 1, 0, d), 1) if n else (d, 0, 1)
             at_q = _strided_at(call, "q", q, (n, heads, d), strides, device)
             length, start, at_out, ws = _arrays(
                 call, device, ("lengths", lengths, _I32, B), ("token_start", token_start, _I32, B + 1), ("out", out, _BF16, n * heads * d),

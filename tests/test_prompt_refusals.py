@@ -103,3 +103,51 @@ def test_sizes_without_a_workspace_are_those_that_are_refused(lb, kv_heads, grou
     if fewer:
         assert refused(lb, name, p, n=fewer, tok=1 << 20, ws=None) == lb.EWORKSPACE
         assert lb.q4_prompt_workspace_bytes(p, fewer) > 0
+
+
+def half(*size):
+    return torch.zeros(size, dtype=torch.bfloat16)
+
+
+MAX = 1 << 24
+
+
+@pytest.mark.parametrize("q, kv", [
+    (half(8, 128, 1).permute(2, 0, 1), half(2, 128, 1).permute(2, 0, 1)),               # one token: a stride of 1
+    (half(9, 128, 1).transpose(1, 2), half(9, 128, 1).transpose(1, 2)),                 # one head
+    (half(9, 8, 128), half(2, 64, 128, 1).permute(3, 0, 1, 2)),                         # one request
+    (half(9, 8, 128), half(1, 64, 128).unsqueeze(1)),
+    (half(1, 8, 128), half(2, 2, 128, 1).permute(0, 1, 3, 2)),                          # a cache of one row
+    (half(1, 8, 128), half(3, 128, 1).permute(0, 2, 1).unsqueeze(1)),                   # and one head
+    (half(8 * 9 * 128).as_strided((9, 1, 128), (128, 2 * MAX, 1)), half(9, 1, 128)),    # one head of many that lie far apart
+    (half(8, 128).as_strided((1, 8, 128), (2 * MAX, 128, 1)), half(1, 2, 128)),
+])
+def test_strides_of_dimensions_of_one_entry_do_not_count(lb, monkeypatch, q, kv):  # noqa: F811
+    batch = kv.shape[0] if kv.dim() == 4 else 1
+    p = lb.make_prompt(batch, q, kv)
+    assert lb.check_prompt(p) == lb.OK
+    for name, t, strides in (("q", q, (p.q_stride_tok, p.q_stride_head)), ("kv", kv, (p.kv_stride_tok, p.kv_stride_head))):
+        dims = (0, 1) if t.dim() == 3 else (2, 1)
+        assert all(t.shape[i] == 1 or t.stride(i) == s for i, s in zip(dims, strides)), name
+    calls = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: calls.append((name,) + a) or 0
+
+    ws = lb.alloc_prompt_workspace(p, "cpu")
+    monkeypatch.setattr(lb, "_lib", Library())
+    c = object.__new__(lb.Context)
+    c._h, c.device = None, -1
+    T, H = q.shape[:2]
+    start, lengths = torch.zeros(batch + 1, dtype=torch.int32), torch.zeros(batch, dtype=torch.int32)
+    out, lse = half(T, H, 128), torch.zeros(H, T)
+    c.prompt_attn(p, q, kv, kv, start, lengths if kv.dim() == 4 else None, out, lse, ws, stream=0)
+    assert calls[-1][3:6] == (q.data_ptr(), kv.data_ptr(), kv.data_ptr())
+    pg = lb.make_paged(1, H, kv.shape[1], 10, 16, 4)
+    table, cache = torch.zeros((1, 4), dtype=torch.int32), torch.zeros((10, pg.page_tiles * lb.Q4_TILE_BYTES), dtype=torch.uint8)
+    c.q4_prompt_attn(pg, q, cache, table, lengths[:1], start[:2], out, ws, stream=0)
+    tok, head = calls[-1][4:6]
+    assert calls[-1][3] == q.data_ptr() and 128 <= tok <= MAX and 0 <= head <= MAX and tok % 8 == 0 == head % 8
+    assert (T == 1 or tok == q.stride(0)) and (H == 1 or head == q.stride(1))
+    c._h = None
