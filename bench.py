@@ -27,6 +27,7 @@ import argparse
 import hashlib
 import json
 import os
+import re
 import sys
 import time
 
@@ -39,12 +40,20 @@ TRAFFIC_FILE = os.path.join(ROOT, "profiles", "lychee_layer_kernel_c3_pmc.txt")
 CSRC = os.path.join(ROOT, "paper_2602_04541_amd", "csrc")
 
 
-def source_stamp() -> str:
-    """A short hash of the kernel sources: a counter summary is only quoted for the build it was taken on."""
-    h = hashlib.sha256()
-    for name in sorted(os.listdir(CSRC)):
-        if name.endswith((".hip", ".h")):
-            h.update(open(os.path.join(CSRC, name), "rb").read())
+LAYER_SOURCES = ("lychee_layer.hip", "lychee_api.hip")  # the kernel, and what lays out its launches
+
+
+def source_stamp(names=LAYER_SOURCES) -> str:
+    """A short hash of these sources and of what they include: a counter summary is only quoted for the sources it was taken on, and
+    those of other kernels are none of its."""
+    h, found, left = hashlib.sha256(), {}, list(names)
+    while left:
+        name = left.pop()
+        if name not in found:
+            found[name] = open(os.path.join(CSRC, name), "rb").read()
+            left += re.findall(r'^#include "(\w+\.h)"', found[name].decode(), re.M)
+    for name in sorted(found):
+        h.update(found[name])
     return h.hexdigest()[:16]
 
 
