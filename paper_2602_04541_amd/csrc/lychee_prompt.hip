@@ -33,6 +33,7 @@ constexpr float kSlack = 8.f;    // powers of two by which a score may exceed th
 // The maximum of a row whose scores are all -infinity (sum 0, NaN), which is not taken for one that sees nothing (maximum -infinity; zero).
 constexpr float kLeast = -3.40282347e38f;
 __device__ __forceinline__ float factor(float m, float l) { return l != 0.f ? 1.f / l : m == -__builtin_inff() ? 0.f : __builtin_nanf(""); }
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * (1.f / kLog2e); }
 
 struct SharedPrompt {
     __align__(16) uint8_t k[2][kBlockBytes];
@@ -53,44 +54,20 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
     constexpr int kAheadValues = Q4 ? 6 : 8;
     const PromptRows &p = a.r;
     const int g = blockIdx.x % p.n_kv_heads;
-    Tile w;
-    Line line;
-    bool share = false;
-    int64_t at = 0, until = 0, slot = -1;
-    const int range = blockIdx.x / p.n_kv_heads;
-    if (SHARE) {
-        line = lay_line<kLineRows>(p, a.one_range, sh.line);
-        share = line.share;
-        at = range * line.size;
-        until = share ? min(at + line.size, line.all) : 0;
-        if (g == 0) clear_records(a.records, a.n_records, a.by_number, line, range);
-        if (share && at >= until) return;
-    }
-    if (!share) {
-        if (SHARE) __syncthreads();
-        w = find_tile(p, range, sh.plan);
-        if (!w.found) return;
-    }
+    Work work;
+    if (!begin_work<SHARE>(work, p, g, a.one_range, a.records, a.n_records, a.by_number, sh.line, sh.plan)) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     do {
-        if (share) {
-            const LineTile k = line_tile_at<kLineRows>(p, at, line, sh.line);
-            w = Tile{k.b, k.tile, k.n, k.len, k.start, 0, blocks_seen(p, k.tile, k.n, k.len), true};
-            const int64_t from = at - k.at, to = min(opaque64(until) - k.at, k.weight);
-            const int blocks = w.last;
-            w.first = cut_at(from, k.weight, blocks);
-            w.last = cut_at(to, k.weight, blocks);
-            slot = from == 0 && to == k.weight ? -1 : part_slot(range, from == 0, p.n_kv_heads, g);
-            if (from == 0 && g == 0) record_tile(a.records, a.n_records, a.by_number, line, k, range, to == k.weight);
-            at += to - from;
-        }
+        next_tile(work, p, g, a.records, a.n_records, a.by_number, sh.line);
+        const Tile w = work.w;
         const int lane = (int)opaque(threadIdx.x & 63), hi = lane >> 5;
-        const int rows = w.n * p.group, row = w.tile * kPromptRows + wave * 32 + (lane & 31);
+        const int rows = w.n * p.group, first_row = w.tile * kPromptRows + wave * 32, row = first_row + (lane & 31);
         const int row_in = min(row, rows - 1), token = token_of(p, row_in), head = g * p.group + row_in - token * p.group;
         const int pos = w.len - w.n + token;  // keys 0 .. pos are seen
-        const int lowest = w.len - w.n + token_of(p, min(w.tile * kPromptRows + wave * 32, rows - 1));  // of the wavefront's rows
-        const int highest = w.tile * kPromptRows + wave * 32 < rows ? w.len - w.n + token_of(p, min(w.tile * kPromptRows + wave * 32 + 31, rows - 1)) : -1;  // (no rows, no products: a token of
-        // 32 heads, 16 KV heads, over 25 K 4-bit keys takes 41 us, 49 with them)
+        // Of the wavefront's rows.  One without rows makes no products: a token of 32 heads, 16 KV heads, over 25 K 4-bit keys takes
+        // 41 us, 49 with them.
+        const int lowest = w.len - w.n + token_of(p, min(first_row, rows - 1));
+        const int highest = first_row < rows ? w.len - w.n + token_of(p, min(first_row + 31, rows - 1)) : -1;
 
         bf16x8_t qf[8];
         {
@@ -122,9 +99,9 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
                     copy16(at, (uint32_t)min(fetch_row + 16 * i, left) * (uint32_t)(2 * a.kv_tok) + fetch_chunk, to + i * 16 * kRowBytes);
             }
         };
-        // 4 bits: a wavefront takes a tile of 16 tokens of every block, a lane a quarter (one scale's dimensions) of a token's key and of its
-        // value, whose bf16 numbers it writes.  (Writes go eight lanes at a time and meet a bank twice; in an order of tokens in which none
-        // does they are no faster, 6.75 ms either way for the case above.)
+        // 4 bits: a wavefront takes a tile of 16 tokens of every block, a lane a quarter (one scale's dimensions) of a token's key and
+        // of its value, whose bf16 numbers it writes.  (Writes go eight lanes at a time and meet a bank twice; in an order of tokens in
+        // which none does they are no faster, 6.75 ms either way for the case above.)
         const int sub4 = lane & 15, part4 = lane >> 4;
         const uint32_t row4 = (uint32_t)(sub4 * kTokenBytes + 16 * part4), scale4 = (uint32_t)(kTileScales + part4 * kTileTokens + sub4);
         const uint32_t store_at = (uint32_t)((wave * 16 + sub4) * kRowBytes + (((4 * part4) ^ swizzle(sub4)) << 4));
@@ -132,15 +109,18 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
         uint32_t scale_k = 0, scale_v = 0;
         int entry = -1;  // of the block table, for the block that is loaded next
         const auto fetch_entry = [&](int blk) {
-            return gload(a.table + (int64_t)w.b * a.d.table_stride + (min(blk * kPromptKeys + wave * kTileTokens, w.len - 1) >> a.d.page_shift));
+            const int token = min(blk * kPromptKeys + wave * kTileTokens, w.len - 1);
+            return gload(a.table + (int64_t)w.b * a.d.table_stride + (token >> a.d.page_shift));
         };
         const auto load4 = [&](int blk) {  // (whether the tile's page is there)
             const int page = __builtin_amdgcn_readfirstlane(entry), tiles = 1 << (a.d.page_shift - 4);
             const bool there = (uint32_t)page < (uint32_t)a.d.n_pages;
-            const uint8_t *tile = uniform(a.cache + ((int64_t)(there ? page : 0) * a.d.page_tiles + (int64_t)g * tiles + ((blk * 4 + wave) & (tiles - 1))) * kTileBytes);
+            const int64_t number = (int64_t)(there ? page : 0) * a.d.page_tiles + (int64_t)g * tiles + ((blk * 4 + wave) & (tiles - 1));
+            const uint8_t *tile = uniform(a.cache + number * kTileBytes);
             const u32x4_t k = *(const LYCHEE_GLOBAL u32x4_t *)((const LYCHEE_GLOBAL uint8_t *)tile + row4);
             const u32x4_t v = *(const LYCHEE_GLOBAL u32x4_t *)((const LYCHEE_GLOBAL uint8_t *)tile + 64 + row4);
-            const uint32_t ks = *((const LYCHEE_GLOBAL uint8_t *)tile + scale4), vs = *((const LYCHEE_GLOBAL uint8_t *)tile + 4 * kTileTokens + scale4);
+            const uint32_t ks = *((const LYCHEE_GLOBAL uint8_t *)tile + scale4);
+            const uint32_t vs = *((const LYCHEE_GLOBAL uint8_t *)tile + 4 * kTileTokens + scale4);
             code_k = make_uint4(k[0], k[1], k[2], k[3]);
             code_v = make_uint4(v[0], v[1], v[2], v[3]);
             const bool ok = there && blk * kPromptKeys + wave * kTileTokens + sub4 < w.len;
@@ -158,8 +138,8 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
         float m, l;
         bool careful = false;
         for (;;) {
-            // Turns: a block each.  With care all blocks come three times (take_with_care): infinities are put back when all scores have been
-            // seen and no sum is rescaled any more, by a factor that might round to zero.
+            // Turns: a block each.  With care all blocks come three times (take_with_care): infinities are put back when all scores have
+            // been seen and no sum is rescaled any more, by a factor that might round to zero.
             const int blocks = max(w.last - w.first, 0), turns = (careful ? 3 : 1) * blocks;
             const auto after = [&](int blk) { return blk + 1 == w.last ? w.first : blk + 1; };
             const auto fetch = [&](int blk, int turn) {
@@ -196,7 +176,8 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
                 const int j0 = blk * kPromptKeys;
                 if (turn + 1 < turns) fetch(after(blk), turn + 1);
                 if (careful || j0 <= highest) {
-                    const LYCHEE_LDS uint8_t *K = (const LYCHEE_LDS uint8_t *)sh.k[turn & 1], *V = (const LYCHEE_LDS uint8_t *)sh.v[turn & 1];
+                    const LYCHEE_LDS uint8_t *K = (const LYCHEE_LDS uint8_t *)sh.k[turn & 1];
+                    const LYCHEE_LDS uint8_t *V = (const LYCHEE_LDS uint8_t *)sh.v[turn & 1];
                     const uint32_t kat = opaque(row_at), vat = opaque(turn_at);
                     const bool again = careful && turn >= blocks;
                     if (__builtin_expect(careful, 0)) {
@@ -204,7 +185,8 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
                         __syncthreads();
                     }
                     f32x16_t z[2] = {zero16(), zero16()};
-                    bf16x8_t kf[kAhead], vf[kAheadValues];  // read ahead of their products; the first values are on their way while the weights are made
+                    // read ahead of their products; the first values are on their way while the weights are made
+                    bf16x8_t kf[kAhead], vf[kAheadValues];
 #pragma unroll
                     for (int i = 0; i < kAhead; ++i) kf[i] = read_rows(K, kat, i % 2, i / 2);
 #pragma unroll
@@ -239,8 +221,8 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) top = fmaxf(top, z[x][i]);
                     top = max_halves32(top) * a.scale_log2e;
-                    // m is some maximum of late: weights of up to 2^kSlack are as exact as others, and a new maximum costs 65 products.  (By
-                    // the row's own scores alone, so that no row's bits depend on another's.)
+                    // m is some maximum of late: weights of up to 2^kSlack are as exact as others, and a new maximum costs 65
+                    // products.  (By the row's own scores alone, so that no row's bits depend on another's.)
                     if (__ballot(top > m + kSlack) != 0) {
                         asm volatile("");
                         const float up = top > m + kSlack ? top : m;
@@ -270,7 +252,8 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
                     for (int i = 0; i < 16; ++i) {
                         in_order();
                         o[i % 4] = mfma(vf[i % kAheadValues], pf[i / 4], o[i % 4]);
-                        if (i + kAheadValues < 16) vf[i % kAheadValues] = read_turned(V, vat, (i + kAheadValues) % 4, (i + kAheadValues) / 4);
+                        const int next = i + kAheadValues;
+                        if (next < 16) vf[i % kAheadValues] = read_turned(V, vat, next % 4, next / 4);
                         if (i == 10) store_k(turn + 1);  // (the next block's numbers while the products go on)
                         if (i == 14) store_v(turn + 1);
                     }
@@ -289,33 +272,27 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a)
         l = sum_halves32(l);
         if (l == 0.f) {  // (found out here, because a block's scores have no instruction to spare: 0.5 to 0.9 % of long calls)
             bool sees = false;
-            for (int j = w.first * kPromptKeys; !sees && j <= min(pos, w.last * kPromptKeys - 1); j = ((j >> a.d.page_shift) + 1) << a.d.page_shift)
+            const int from = w.first * kPromptKeys, to = min(pos, w.last * kPromptKeys - 1);
+            for (int j = from; !sees && j <= to; j = ((j >> a.d.page_shift) + 1) << a.d.page_shift)
                 sees = !Q4 || (uint32_t)gload(a.table + (int64_t)w.b * a.d.table_stride + (j >> a.d.page_shift)) < (uint32_t)a.d.n_pages;
             if (sees) m = kLeast;
         }
-        if (slot < 0) {
+        if (work.slot < 0) {
             const bool there = row < rows;
             uint16_t *out = a.out + ((int64_t)(w.start + token) * (p.n_kv_heads * p.group) + head) * kHeadDim;
             store_row(there ? out : nullptr, lane, o, factor(m, l));
-            if (a.lse && there && hi == 0)
-                gstore(a.lse + (int64_t)head * p.n_tokens + w.start + token, l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * (1.f / kLog2e));
-        } else if (w.tile * kPromptRows + wave * 32 < rows) {
-            // in the order of the registers: 1 KB a store, read back alike
-            const int64_t part = slot * kWaves + wave;
-            float *po = a.part_o + part * (64 * 64) + 4 * lane;
-#pragma unroll
-            for (int db = 0; db < 4; ++db)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    *(LYCHEE_GLOBAL f32x4_t *)(po + (4 * db + j) * 256) = f32x4_t{o[db][4 * j], o[db][4 * j + 1], o[db][4 * j + 2], o[db][4 * j + 3]};
+            if (a.lse && there && hi == 0) gstore(a.lse + (int64_t)head * p.n_tokens + w.start + token, lse_of(m, l));
+        } else if (first_row < rows) {
+            const int64_t part = (int64_t)work.slot * kWaves + wave;
+            store_part(a.part_o + part * (64 * 64) + 4 * lane, o);
             if (hi == 0) gstore_f2(a.part_ml + (part * 32 + lane) * 2, make_float2(m, l));
         }
-    } while (share && at < opaque64(until));
+    } while (more_work(work));
 }
 
-// Rows of tiles that several ranges share: o = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p, M = max m_p.  A workgroup has 32 rows of a tile and some of the
-// 16 groups of eight dimensions, its wavefronts a fourth of the pieces each, a lane four dimensions of a row, as the pieces left
-// them; the wavefronts' sums meet in LDS.
+// Rows of tiles that several ranges share: o = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p, M = max m_p.  A workgroup has 32 rows of
+// a tile and some of the 16 groups of eight dimensions, its wavefronts a fourth of the pieces each, a lane four dimensions of a row, as
+// the pieces left them; the wavefronts' sums meet in LDS.
 // Pieces whose loads are in flight together; those of pieces that are not there are left out (all wavefronts at the last one's place
 // instead: 10 us where 64 pieces of 8 heads take 8, and 54 where a call of 9 pieces takes 37).
 constexpr int kMergeBatch = 16;
@@ -325,20 +302,21 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptArgs a)
     __shared__ float2 ml[kWaves][64];
     const PromptRows &p = a.r;
     // (KV heads apart as in the launch before, whose partials lie in the caches of the same part of the device)
-    const int g = blockIdx.x % p.n_kv_heads, unit = blockIdx.x / p.n_kv_heads, sub = unit % a.merge_split, rows32 = unit / a.merge_split % kWaves;
+    const int g = blockIdx.x % p.n_kv_heads, unit = blockIdx.x / p.n_kv_heads;
+    const int sub = unit % a.merge_split, rows32 = unit / a.merge_split % kWaves;
     const Record w = recorded(a.records, unit / a.merge_split / kWaves);
     const int parts = w.parts, range = w.range;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rows = w.n * p.group;
     if (parts == 0 || w.tile * kPromptRows + rows32 * 32 >= rows) return;
-    const int row = w.tile * kPromptRows + rows32 * 32 + (lane & 31), token = token_of(p, min(row, rows - 1)), head = g * p.group + min(row, rows - 1) - token * p.group;
+    const int row = w.tile * kPromptRows + rows32 * 32 + (lane & 31), row_in = min(row, rows - 1);
+    const int token = token_of(p, row_in), head = g * p.group + row_in - token * p.group;
     const int64_t to = (int64_t)(w.start + token) * (p.n_kv_heads * p.group) + head;
     const auto at = [&](int piece) { return part_slot(range + piece, piece == 0, p.n_kv_heads, g) * kWaves + rows32; };
     const auto store = [&](int dj, f32x4_t o, float f) {  // (dimensions of register group dj: 32 db + 8 j + 4 hi)
-        *(LYCHEE_GLOBAL u32x2_t *)(a.out + to * kHeadDim + 8 * dj + 4 * (lane >> 5)) = u32x2_t{pk_bf16(o[0] * f, o[1] * f), pk_bf16(o[2] * f, o[3] * f)};
+        store_four(a.out + to * kHeadDim + 8 * dj + 4 * (lane >> 5), o, f);
     };
     const auto store_lse = [&](float m, float l) {
-        if (a.lse && lane < 32)
-            gstore(a.lse + (int64_t)head * p.n_tokens + w.start + token, l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * (1.f / kLog2e));
+        if (a.lse && lane < 32) gstore(a.lse + (int64_t)head * p.n_tokens + w.start + token, lse_of(m, l));
     };
     // A piece's infinity stays one, though its weight may round to zero: sums that are no numbers are made again.
     const auto with_infinities = [&](f32x4_t o, int dj, float m) {

@@ -38,7 +38,9 @@ bool may_share(int32_t batch, int32_t heads, int32_t n_tokens, int64_t max_len, 
 {
     const float range = (float)heads / (float)(kPromptRows * kPromptSlots), own = 1.f / (2 * kPromptKeys);
     const auto weight = [&](float tokens, float of_each) { return tokens * range * (of_each * own + kPromptTileCost); };
-    const auto shared = [&](float longest, float all) { return longest / kPromptKeys + 1 + kPromptTileCost > kPromptShareCost + kPromptShareSize * all; };
+    const auto shared = [&](float longest, float all) {
+        return longest / kPromptKeys + 1 + kPromptTileCost > kPromptShareCost + kPromptShareSize * all;
+    };
     const float n = (float)n_tokens;
     if (!packed) return shared((float)max_len, weight(n, n / (float)batch));
     if (batch == 1) return shared(n, weight(n, n));
@@ -96,7 +98,8 @@ int check_prompt(const lychee_prompt *p)
         !good_stride(p->kv_stride_head) || !good_stride(p->kv_stride_tok) || p->q_stride_tok < kHeadDim || p->kv_stride_tok < kHeadDim)
         return LYCHEE_EINVAL;
     if (p->batch > kMaxBatch || p->max_len > kMaxContext) return LYCHEE_EUNSUPPORTED;
-    if (p->q_stride_tok > kPromptMaxStride || p->q_stride_head > kPromptMaxStride || p->kv_stride_tok > kPromptMaxStride) return LYCHEE_EUNSUPPORTED;
+    if (p->q_stride_tok > kPromptMaxStride || p->q_stride_head > kPromptMaxStride || p->kv_stride_tok > kPromptMaxStride)
+        return LYCHEE_EUNSUPPORTED;
     const int32_t G = p->n_q_heads / p->n_kv_heads;
     if ((int64_t)p->n_tokens * G >= kPromptMaxRows) return LYCHEE_EUNSUPPORTED;
     if (rows_grid(p->batch, p->n_kv_heads, G, p->n_tokens, 0, false).tiles * p->n_kv_heads >= kMaxGrid) return LYCHEE_EUNSUPPORTED;
@@ -198,8 +201,9 @@ int lychee_check_prompt(const lychee_prompt *prompt) { return check_prompt(promp
 
 size_t lychee_prompt_workspace_bytes(const lychee_prompt *prompt) { return check_prompt(prompt) == LYCHEE_OK ? carve(*prompt).total : 0; }
 
-int lychee_prompt_attn(lychee_ctx *ctx, const lychee_prompt *prompt, const void *q, const void *k, const void *v, const int32_t *token_start,
-                       const int32_t *lengths, void *out, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream)
+int lychee_prompt_attn(lychee_ctx *ctx, const lychee_prompt *prompt, const void *q, const void *k, const void *v,
+                       const int32_t *token_start, const int32_t *lengths, void *out, float *lse, void *workspace,
+                       size_t workspace_bytes, void *hip_stream)
 {
     if (ctx == nullptr) return LYCHEE_EINVAL;
     int rc = check_prompt(prompt);
@@ -229,8 +233,8 @@ int lychee_prompt_attn(lychee_ctx *ctx, const lychee_prompt *prompt, const void 
     return done(launch_prompt(a, static_cast<hipStream_t>(hip_stream)));
 }
 
-int lychee_prompt_attn_backward(lychee_ctx *ctx, const lychee_prompt *prompt, const void *d_out, const void *q, const void *k, const void *v,
-                                const void *out, const float *lse, const int32_t *token_start, void *dq, void *dk, void *dv,
+int lychee_prompt_attn_backward(lychee_ctx *ctx, const lychee_prompt *prompt, const void *d_out, const void *q, const void *k,
+                                const void *v, const void *out, const float *lse, const int32_t *token_start, void *dq, void *dk, void *dv,
                                 void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     if (ctx == nullptr) return LYCHEE_EINVAL;
@@ -239,7 +243,8 @@ int lychee_prompt_attn_backward(lychee_ctx *ctx, const lychee_prompt *prompt, co
     const lychee_prompt &p = *prompt;
     if (!token_start || !aligned(token_start, 4) || !aligned(lse, 4)) return LYCHEE_EINVAL;
     // gradients of rows that meet would be written by several workgroups
-    if (rows_meet(p.n_tokens, p.q_stride_tok, p.n_q_heads, p.q_stride_head) || rows_meet(p.n_tokens, p.kv_stride_tok, p.n_kv_heads, p.kv_stride_head))
+    if (rows_meet(p.n_tokens, p.q_stride_tok, p.n_q_heads, p.q_stride_head) ||
+        rows_meet(p.n_tokens, p.kv_stride_tok, p.n_kv_heads, p.kv_stride_head))
         return LYCHEE_EINVAL;
     const CarvedPrompt c = carve(p);
     if ((rc = check_workspace(workspace, workspace_bytes, c)) != LYCHEE_OK) return rc;
@@ -316,7 +321,8 @@ int lychee_q4_prompt_attn(lychee_ctx *ctx, const lychee_paged *paged, const void
     if (!dev.ok) return LYCHEE_EHIP;
     PromptArgs a;
     memset(&a, 0, sizeof a);
-    a.r = rows_of(p.batch, p.n_q_heads, p.n_kv_heads, n_tokens, p.max_pages * p.page_size, q_stride_tok, q_stride_head, token_start, lengths);
+    a.r = rows_of(p.batch, p.n_q_heads, p.n_kv_heads, n_tokens, p.max_pages * p.page_size, q_stride_tok, q_stride_head, token_start,
+                  lengths);
     a.q = static_cast<const uint16_t *>(q);
     a.cache = static_cast<const uint8_t *>(cache);
     a.table = block_table;

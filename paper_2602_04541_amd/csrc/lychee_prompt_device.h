@@ -28,7 +28,10 @@ constexpr int kBlockBytes = kPromptKeys * kRowBytes;
 
 __device__ __forceinline__ int swizzle(int row) { return (row & 3) << 2 | ((row >> 2) & 3); }
 
-__device__ __forceinline__ f32x16_t mfma(bf16x8_t a, bf16x8_t b, f32x16_t c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16_t mfma(bf16x8_t a, bf16x8_t b, f32x16_t c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
 
 __device__ __forceinline__ uint32_t pk_bf16(float a, float b)  // round to nearest even, a in the low half
 {
@@ -66,7 +69,10 @@ __device__ __forceinline__ f32x16_t all16(float x)
 __device__ __forceinline__ f32x16_t zero16() { return all16(0.f); }
 
 // ------------------------------------------------------------------------------ rows
-__device__ __forceinline__ int token_of(const PromptRows &p, int row) { return p.group == 1 ? row : (int)__umulhi((uint32_t)row, p.group_magic); }
+__device__ __forceinline__ int token_of(const PromptRows &p, int row)
+{
+    return p.group == 1 ? row : (int)__umulhi((uint32_t)row, p.group_magic);
+}
 
 // What a workgroup works on: blocks of keys of a tile, which is kPromptRows rows of a (request, KV head).
 struct Tile {
@@ -102,7 +108,8 @@ __device__ __forceinline__ int blocks_seen(const PromptRows &p, int tile, int n,
 
 __device__ __forceinline__ int64_t uniform64(int64_t x)
 {
-    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+    const uint32_t high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32));
+    return (int64_t)((uint64_t)high << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
 }
 
 // Which request has the `number`th of all the requests' tiles, where thread b knows request b's `tiles`.  Requests come in
@@ -207,7 +214,8 @@ struct Line {
 template <int KIND>
 __device__ __forceinline__ int64_t weight_before(const PromptRows &p, int64_t tile, int n, int len)
 {
-    if (KIND == kLineRows) return tile * ((int64_t)p.group * (max(len - n, 0) + kPromptTileCost * kPromptKeys)) + kPromptRows / 2 * tile * (tile + 1);
+    if (KIND == kLineRows)
+        return tile * ((int64_t)p.group * (max(len - n, 0) + kPromptTileCost * kPromptKeys)) + kPromptRows / 2 * tile * (tile + 1);
     return tile * blocks_of(n * p.group) - (int64_t)(kPromptRows / kPromptKeys) * p.group * tile * (tile - 1) / 2;
 }
 template <int KIND>
@@ -267,7 +275,8 @@ __device__ __forceinline__ Line lay_line(const PromptRows &p, double one_range, 
     // A workgroup alone on its unit takes 1.2 us a block, one of two 2.05; a range costs its beginning, its partials and their merge.  One
     // prompt of 16 heads (4 KV heads), shared and not: 2048 tokens 43.5 us and 46, 3500 80 and 81, 5120 143 and 126, 6144 195 and 164;
     // of 4 heads (2) 1100 tokens 22 and 28, 2048 26 and 45, 8192 95 and 157.
-    l.share = KIND == kLineKeys || (float)__builtin_amdgcn_readfirstlane(longest) > kPromptShareCost + kPromptShareSize * (float)l.size / (float)unit;
+    l.share = KIND == kLineKeys ||
+              (float)__builtin_amdgcn_readfirstlane(longest) > kPromptShareCost + kPromptShareSize * (float)l.size / (float)unit;
     l.all = uniform64(l.all);
     l.tiles = __builtin_amdgcn_readfirstlane(l.tiles);
     l.start = __builtin_amdgcn_readfirstlane(l.start);
@@ -342,7 +351,10 @@ __device__ __forceinline__ int range_at(int64_t place, const Line &line)
     return __builtin_amdgcn_readfirstlane((int)r);
 }
 // Partials: a range leaves two at most, that of the end of a tile that began in a range before, and that of a tile's beginning.
-__device__ __forceinline__ int64_t part_slot(int64_t range, bool beginning, int n_kv_heads, int g) { return (range * 2 + beginning) * n_kv_heads + g; }
+__device__ __forceinline__ int64_t part_slot(int64_t range, bool beginning, int n_kv_heads, int g)
+{
+    return (range * 2 + beginning) * n_kv_heads + g;
+}
 // For the merge, of a tile that lies in several ranges: how many (0: in one), the first of them, and what the tile is.  Kept by the range
 // it begins in, which is the only one there, or, where there are fewer tiles, by its number.  (A launch's first microseconds
 // go by the code that it runs once, which comes from memory: the merges read this, and lay no line.)
@@ -366,7 +378,8 @@ __device__ __forceinline__ void clear_records(int32_t *records, int n_records, b
         gstore(records + kRecordWords * range, 0);
     }
 }
-__device__ __forceinline__ void record_tile(int32_t *records, int n_records, bool by_number, const Line &line, const LineTile &k, int range, bool whole)
+__device__ __forceinline__ void record_tile(int32_t *records, int n_records, bool by_number, const Line &line, const LineTile &k, int range,
+                                            bool whole)
 {
     const int at = by_number ? k.number : range;
     if (threadIdx.x == 0 && at < n_records && (by_number || !whole))
@@ -375,9 +388,56 @@ __device__ __forceinline__ void record_tile(int32_t *records, int n_records, boo
 __device__ __forceinline__ Record recorded(const int32_t *records, int at)
 {
     const int32_t *r = records + kRecordWords * at;
-    return {__builtin_amdgcn_readfirstlane(gload(r)),     __builtin_amdgcn_readfirstlane(gload(r + 1)), __builtin_amdgcn_readfirstlane(gload(r + 2)),
-            __builtin_amdgcn_readfirstlane(gload(r + 3)), __builtin_amdgcn_readfirstlane(gload(r + 4)), {}};
+    const auto word = [&](int i) { return __builtin_amdgcn_readfirstlane(gload(r + i)); };
+    return {word(0), word(1), word(2), word(3), word(4), {}};
 }
+
+// What a workgroup works on: where tiles are shared out a range of the line, tile after tile and parts of tiles at its ends; else one tile.
+struct Work {
+    Line line;
+    bool share;
+    int range;
+    int64_t at, until;  // what is left of the range
+    int slot;           // of the present tile's partials; -1: the workgroup has all of its blocks
+    Tile w;
+};
+// (whether there is anything to do)
+template <bool SHARE>
+__device__ __forceinline__ bool begin_work(Work &k, const PromptRows &p, int g, double one_range, int32_t *records, int n_records,
+                                           bool by_number, SharedLine &line, SharedPlan &plan)
+{
+    k.share = false;
+    k.range = blockIdx.x / p.n_kv_heads;
+    k.at = k.until = 0;
+    k.slot = -1;
+    if (SHARE) {
+        k.line = lay_line<kLineRows>(p, one_range, line);
+        k.share = k.line.share;
+        k.at = k.range * k.line.size;
+        k.until = k.share ? min(k.at + k.line.size, k.line.all) : 0;
+        if (g == 0) clear_records(records, n_records, by_number, k.line, k.range);
+        if (k.share) return k.at < k.until;
+        __syncthreads();
+    }
+    k.w = find_tile(p, k.range, plan);
+    return k.w.found;
+}
+// The next tile of a range, and which of its blocks.
+__device__ __forceinline__ void next_tile(Work &k, const PromptRows &p, int g, int32_t *records, int n_records, bool by_number,
+                                          const SharedLine &line)
+{
+    if (!k.share) return;
+    const LineTile t = line_tile_at<kLineRows>(p, k.at, k.line, line);
+    k.w = Tile{t.b, t.tile, t.n, t.len, t.start, 0, blocks_seen(p, t.tile, t.n, t.len), true};
+    const int64_t from = k.at - t.at, to = min(opaque64(k.until) - t.at, t.weight);
+    const int blocks = k.w.last;
+    k.w.first = cut_at(from, t.weight, blocks);
+    k.w.last = cut_at(to, t.weight, blocks);
+    k.slot = from == 0 && to == t.weight ? -1 : (int)part_slot(k.range, from == 0, p.n_kv_heads, g);
+    if (from == 0 && g == 0) record_tile(records, n_records, by_number, k.line, t, k.range, to == t.weight);
+    k.at += to - from;
+}
+__device__ __forceinline__ bool more_work(const Work &k) { return k.share && k.at < opaque64(k.until); }
 
 // ------------------------------------------------------------------------------ LDS
 // Sixteen bytes a lane from global memory to LDS, lane after lane from `to` on (base and to: the same for the wavefront).  In
@@ -387,7 +447,8 @@ template <typename T>
 __device__ __forceinline__ const T *uniform(const T *p)  // (in scalar registers, whatever the compiler knows of it)
 {
     const uint64_t u = reinterpret_cast<uint64_t>(p);
-    return reinterpret_cast<const T *>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)u));
+    const uint32_t high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(u >> 32));
+    return reinterpret_cast<const T *>((uint64_t)high << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)u));
 }
 __device__ __forceinline__ void copy16(const uint16_t *base, uint32_t offset, uint32_t to)
 {
@@ -423,7 +484,8 @@ __device__ __forceinline__ bf16x8_t read_turned(const LYCHEE_LDS uint8_t *block,
 {
     const LYCHEE_LDS uint8_t *p = block + s * 16 * kRowBytes;
     const s16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LYCHEE_LDS s16x4_t *)(p + (place ^ (uint32_t)(db << 6))));
-    const s16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LYCHEE_LDS s16x4_t *)(p + 8 * kRowBytes + (place ^ (uint32_t)(db << 6 | 32))));
+    const s16x4_t b =
+        __builtin_amdgcn_ds_read_tr16_b64_v4i16((LYCHEE_LDS s16x4_t *)(p + 8 * kRowBytes + (place ^ (uint32_t)(db << 6 | 32))));
     typedef short s16x8_t __attribute__((ext_vector_type(8)));
     return __builtin_bit_cast(bf16x8_t, (s16x8_t)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
@@ -517,6 +579,23 @@ __device__ __forceinline__ void store_row(uint16_t *row, int lane, const f32x16_
             }
             if (row) *(LYCHEE_GLOBAL u32x4_t *)(row + 32 * db + 16 * j + 8 * (lane >> 5)) = u;
         }
+}
+
+// A wavefront's sums as a partial, in the order of the registers: 1 KB a store, read back alike.
+__device__ __forceinline__ void store_part(float *to, const f32x16_t (&x)[4])
+{
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const f32x4_t y = {x[db][4 * j], x[db][4 * j + 1], x[db][4 * j + 2], x[db][4 * j + 3]};
+            *(LYCHEE_GLOBAL f32x4_t *)(to + (4 * db + j) * 256) = y;
+        }
+}
+// Four neighbouring dimensions of a merged row.
+__device__ __forceinline__ void store_four(uint16_t *to, f32x4_t x, float f)
+{
+    *(LYCHEE_GLOBAL u32x2_t *)to = u32x2_t{pk_bf16(x[0] * f, x[1] * f), pk_bf16(x[2] * f, x[3] * f)};
 }
 
 }  // namespace

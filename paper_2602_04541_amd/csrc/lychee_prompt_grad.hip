@@ -86,44 +86,18 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dq_kernel(PromptGradArgs a
     __shared__ SharedGrad sh;
     const PromptRows &p = a.r;
     const int g = blockIdx.x % p.n_kv_heads;
-    Tile w;
-    Line line;
-    bool share = false;
-    int64_t at = 0, until = 0;
-    int slot = -1;
-    const int range = blockIdx.x / p.n_kv_heads;
-    if (SHARE) {
-        line = lay_line<kLineRows>(p, a.one_row_range, sh.line);
-        share = line.share;
-        at = range * line.size;
-        until = share ? min(at + line.size, line.all) : 0;
-        if (g == 0) clear_records(a.records, a.n_row_records, a.rows_by_number, line, range);
-        if (share && at >= until) return;
-    }
-    if (!share) {
-        if (SHARE) __syncthreads();
-        w = find_tile(p, range, sh.plan);
-        if (!w.found) return;
-        __syncthreads();  // (the plan's part of LDS is free)
-    }
+    Work work;
+    if (!begin_work<SHARE>(work, p, g, a.one_row_range, a.records, a.n_row_records, a.rows_by_number, sh.line, sh.plan)) return;
+    if (!work.share) __syncthreads();  // (the plan's part of LDS is free)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     do {
-        if (share) {
-            const LineTile k = line_tile_at<kLineRows>(p, at, line, sh.line);
-            w = Tile{k.b, k.tile, k.n, k.len, k.start, 0, blocks_seen(p, k.tile, k.n, k.len), true};
-            const int64_t from = at - k.at, to = min(opaque64(until) - k.at, k.weight);
-            const int blocks = w.last;
-            w.first = cut_at(from, k.weight, blocks);
-            w.last = cut_at(to, k.weight, blocks);
-            slot = from == 0 && to == k.weight ? -1 : (int)part_slot(range, from == 0, p.n_kv_heads, g);
-            if (from == 0 && g == 0) record_tile(a.records, a.n_row_records, a.rows_by_number, line, k, range, to == k.weight);
-            at += to - from;
-        }
+        next_tile(work, p, g, a.records, a.n_row_records, a.rows_by_number, sh.line);
+        const Tile w = work.w;
         const int lane = (int)opaque(threadIdx.x & 63), hi = lane >> 5;
-        const int rows = w.n * p.group, row = w.tile * kPromptRows + wave * 32 + (lane & 31);
+        const int rows = w.n * p.group, first_row = w.tile * kPromptRows + wave * 32, row = first_row + (lane & 31);
         const int row_in = min(row, rows - 1), pos = token_of(p, row_in), head = g * p.group + row_in - pos * p.group;
-        const int lowest = token_of(p, min(w.tile * kPromptRows + wave * 32, rows - 1));
-        const int highest = w.tile * kPromptRows + wave * 32 < rows ? token_of(p, min(w.tile * kPromptRows + wave * 32 + 31, rows - 1)) : -1;  // (no rows: no products)
+        const int lowest = token_of(p, min(first_row, rows - 1));
+        const int highest = first_row < rows ? token_of(p, min(first_row + 31, rows - 1)) : -1;  // (no rows: no products)
         const int64_t token = w.start + pos, packed = (token * (p.n_kv_heads * p.group) + head) * kHeadDim;
         const int64_t q_at = token * p.q_tok + (int64_t)head * p.q_head;
 
@@ -155,7 +129,8 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dq_kernel(PromptGradArgs a
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int64_t from = base + (int64_t)(whole ? j0 + 16 * i : j0) * a.kv_tok;
-                const uint32_t off = whole ? fetch_at : (uint32_t)min(fetch_row + 16 * i, w.len - 1 - j0) * (uint32_t)(2 * a.kv_tok) + fetch_chunk;
+                const uint32_t last = (uint32_t)min(fetch_row + 16 * i, w.len - 1 - j0);
+                const uint32_t off = whole ? fetch_at : last * (uint32_t)(2 * a.kv_tok) + fetch_chunk;
                 copy16(a.k + from, off, to_k + buf * kBlockBytes + i * 16 * kRowBytes);
                 copy16(a.v + from, off, to_v + buf * kBlockBytes + i * 16 * kRowBytes);
             }
@@ -223,8 +198,9 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dq_kernel(PromptGradArgs a
                             take_with_care(sh.a[buf], kBlockBytes, min(turn / 2 % 3, 1));
                             __syncthreads();
                             if (turn / 2 % 3 != 0) {
+                                const uint32_t largest = turn / 2 % 3 == 1 ? kLargest : 0x8000u | kLargest;
 #pragma unroll
-                                for (int s = 0; s < 2; ++s) ds[s] = seen_rows(hi, 2 * x + s, 0, pos - j0, turn / 2 % 3 == 1 ? kLargest : 0x8000u | kLargest);
+                                for (int s = 0; s < 2; ++s) ds[s] = seen_rows(hi, 2 * x + s, 0, pos - j0, largest);
                             }
 #pragma unroll
                             for (int i = 0; i < kAheadTurned; ++i) turned[i] = read_second(i);
@@ -244,17 +220,12 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dq_kernel(PromptGradArgs a
             if (careful || !any_thread(!all_finite(dq), wave, sh.said)) break;
             careful = true;
         }
-        if (slot < 0) {
+        if (work.slot < 0) {
             store_row(row < rows ? a.dq + q_at : nullptr, lane, dq, a.scale);
         } else {
-            float *to = a.part + (int64_t)(slot * kWaves + wave) * (kPartFloats / 2) + 4 * lane;
-#pragma unroll
-            for (int db = 0; db < 4; ++db)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    *(LYCHEE_GLOBAL f32x4_t *)(to + (4 * db + j) * 256) = f32x4_t{dq[db][4 * j], dq[db][4 * j + 1], dq[db][4 * j + 2], dq[db][4 * j + 3]};
+            store_part(a.part + (int64_t)(work.slot * kWaves + wave) * (kPartFloats / 2) + 4 * lane, dq);
         }
-    } while (share && at < opaque64(until));
+    } while (more_work(work));
 }
 
 // The sums of tiles that lie in several ranges, range after range: a workgroup has 32 rows, a wavefront every fourth group of
@@ -267,20 +238,21 @@ __global__ __launch_bounds__(kThreads) void prompt_dq_merge_kernel(PromptGradArg
     const int parts = w.parts, range = w.range;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rows = w.n * p.group;
     if (parts == 0 || w.tile * kPromptRows + rows32 * 32 >= rows) return;
-    const int row = w.tile * kPromptRows + rows32 * 32 + (lane & 31), token = token_of(p, min(row, rows - 1)), head = g * p.group + min(row, rows - 1) - token * p.group;
+    const int row = w.tile * kPromptRows + rows32 * 32 + (lane & 31), row_in = min(row, rows - 1);
+    const int token = token_of(p, row_in), head = g * p.group + row_in - token * p.group;
     f32x4_t sum[4];
     sum_parts<4>(sum, parts, [&](int piece, int i) {
-        return a.part + (part_slot(range + piece, piece == 0, p.n_kv_heads, g) * kWaves + rows32) * (kPartFloats / 2) + (4 * i + wave) * 256 + 4 * lane;
+        const int64_t part = part_slot(range + piece, piece == 0, p.n_kv_heads, g) * kWaves + rows32;
+        return a.part + part * (kPartFloats / 2) + (4 * i + wave) * 256 + 4 * lane;
     });
     if (row >= rows) return;
     uint16_t *to = a.dq + (int64_t)(w.start + token) * p.q_tok + (int64_t)head * p.q_head + 4 * (lane >> 5);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        *(LYCHEE_GLOBAL u32x2_t *)(to + 8 * (4 * i + wave)) = u32x2_t{pk_bf16(sum[i][0] * a.scale, sum[i][1] * a.scale), pk_bf16(sum[i][2] * a.scale, sum[i][3] * a.scale)};
+    for (int i = 0; i < 4; ++i) store_four(to + 8 * (4 * i + wave), sum[i], a.scale);
 }
 
-// dk and dv.  A wavefront has 32 keys, whose rows of K stay in registers and of V in LDS, and goes over the rows that see them, 32 at a time:
-// queries and output gradients in LDS, scores and dP with a lane for a key, so that P and dS are B operands of the sums over
+// dk and dv.  A wavefront has 32 keys, whose rows of K stay in registers and of V in LDS, and goes over the rows that see them, 32 at a
+// time: queries and output gradients in LDS, scores and dP with a lane for a key, so that P and dS are B operands of the sums over
 // the rows.
 __global__ __launch_bounds__(kThreads, 2) void prompt_dkv_kernel(PromptGradArgs a)
 {
@@ -446,13 +418,8 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_dkv_kernel(PromptGradArgs 
             store_row(key < w.n ? a.dv + to : nullptr, lane, dv, 1.f);
         } else if (tile * kPromptRows + wave * 32 < w.n) {
             float *to = a.part + (part_slot(range, place == 0, p.n_kv_heads, g) * kWaves + wave) * kPartFloats + 4 * lane;
-#pragma unroll
-            for (int db = 0; db < 4; ++db)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    *(LYCHEE_GLOBAL f32x4_t *)(to + (4 * db + j) * 256) = f32x4_t{dk[db][4 * j], dk[db][4 * j + 1], dk[db][4 * j + 2], dk[db][4 * j + 3]};
-                    *(LYCHEE_GLOBAL f32x4_t *)(to + (16 + 4 * db + j) * 256) = f32x4_t{dv[db][4 * j], dv[db][4 * j + 1], dv[db][4 * j + 2], dv[db][4 * j + 3]};
-                }
+            store_part(to, dk);
+            store_part(to + kPartFloats / 2, dv);
         }
     }
 }
@@ -468,14 +435,14 @@ __global__ __launch_bounds__(kThreads) void prompt_dkv_merge_kernel(PromptGradAr
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, key = w.tile * kPromptRows + keys32 * 32 + (lane & 31);
     f32x4_t sum[4];
     sum_parts<4>(sum, parts, [&](int piece, int i) {
-        return a.part + (part_slot(range + piece, piece == 0, p.n_kv_heads, g) * kWaves + keys32) * kPartFloats + (16 * of_v + 4 * i + wave) * 256 + 4 * lane;
+        const int64_t part = part_slot(range + piece, piece == 0, p.n_kv_heads, g) * kWaves + keys32;
+        return a.part + part * kPartFloats + (16 * of_v + 4 * i + wave) * 256 + 4 * lane;
     });
     if (key >= w.n) return;
     uint16_t *to = (of_v ? a.dv : a.dk) + (int64_t)(w.start + key) * a.kv_tok + (int64_t)g * a.kv_head + 4 * (lane >> 5);
     const float f = of_v ? 1.f : a.scale;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        *(LYCHEE_GLOBAL u32x2_t *)(to + 8 * (4 * i + wave)) = u32x2_t{pk_bf16(sum[i][0] * f, sum[i][1] * f), pk_bf16(sum[i][2] * f, sum[i][3] * f)};
+    for (int i = 0; i < 4; ++i) store_four(to + 8 * (4 * i + wave), sum[i], f);
 }
 
 }  // namespace
@@ -484,7 +451,8 @@ hipError_t launch_prompt_grad(const PromptGradArgs &a, hipStream_t stream)
 {
     const unsigned heads = (unsigned)a.r.n_kv_heads;
     if (a.n_row_ranges > 0) {
-        prompt_dq_kernel<true><<<(unsigned)(a.n_row_ranges > a.n_row_tiles ? a.n_row_ranges : a.n_row_tiles) * heads, kThreads, 0, stream>>>(a);
+        const unsigned work = (unsigned)(a.n_row_ranges > a.n_row_tiles ? a.n_row_ranges : a.n_row_tiles);
+        prompt_dq_kernel<true><<<work * heads, kThreads, 0, stream>>>(a);
         prompt_dq_merge_kernel<<<(unsigned)a.n_row_records * heads * kWaves, kThreads, 0, stream>>>(a);
     } else {
         prompt_dq_kernel<false><<<(unsigned)a.n_row_tiles * heads, kThreads, 0, stream>>>(a);
