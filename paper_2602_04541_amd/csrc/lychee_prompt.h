@@ -13,8 +13,10 @@ constexpr int kPromptKeys = 64;           // keys a workgroup takes at a time
 // and of key tiles.
 constexpr int kPromptMinRange = 3;
 constexpr int kPromptMinKeyRange = 2;
-// Blocks of all key tiles that are one range, which needs no merge: 64 tokens of 8 heads, 8 KV heads, both passes 22 us, 25 with the merge; from
-// 8 blocks on one workgroup takes longer than ranges and their merge (100 tokens of 8 heads, 2 KV heads: 39 us, 32 in ranges).
+// Blocks of all key tiles (keys_grid counts them) that are one range, which needs no merge; more take a workgroup longer than ranges and
+// their merge.  A backward call of 8 heads, 2 KV heads, in one range and in ranges: 32 tokens (3 blocks) 17.5 and 19.5 us, 48 (4) 20.5
+// and 21.9, 64 (5) 23.3 and 22.1, 80 (6) 26.5 and 22.7, 96 (7) 30.3 and 24.0; of 64 heads, 16 KV heads, the same to 0.3 us.  (Three
+// requests of 20 tokens, 8 heads each, 3 blocks in as many tiles: 22.4 and 19.8.)
 constexpr int kPromptOneRange = 4;
 // Rows' tiles are shared out where the longest has kPromptShareCost blocks more than kPromptShareSize times a range's (lay_line).
 constexpr int kPromptShareCost = 14;

@@ -11,13 +11,15 @@
 // block's keys, the running maximum and sum need one exchange between two lanes, and the weights are the B operand of the second
 // product O^T = V^T P^T as they stand.
 //
-// What bounds it, long: the products, 64 of 32x32x16 for 128 rows and 64 keys.  16384 tokens of 32 heads (8 KV heads) take 2.08 ms,
-// 1.06 PFLOP/s; a library's product of 8192 x 8192 x 8192 reaches 1.30 on the same card at the clock that power leaves either,
-// about 1.9 GHz.  The matrix units are busy 55 % of the cycles, no read of LDS meets a bank twice, and the same loop without its copies
-// is 10 % faster.  Two wavefronts a unit share the rest: exponentials and sums of one beside the products of the other; the next
+// What bounds it, long: the products, 64 of 32x32x16 for 128 rows and 64 keys, and the issue slots that are left between them.  16384
+// tokens of 32 heads (8 KV heads) take 2.02 ms, 1.09 PFLOP/s; a library's product of 8192 x 8192 x 8192 reaches 1.30.  Power leaves
+// either a clock of about 1.9 GHz, at which the matrix units could make 2.0: they are busy 55 to 57 % of the cycles here, 65 to 70 % in
+// the library's product, which has no exponentials and sums to make.  No read of LDS meets a bank twice, and the same loop without its
+// copies is 10 % faster.  Two wavefronts a unit share the rest: exponentials and sums of one beside the products of the other; the next
 // block's scores begun beside a block's weights, weights made between products and priorities by wavefront all cost more than they
-// gave.  Short: a launch and what it reads once, 6 us for 77 tokens.  Few rows over many keys: HBM and the merge, 51 us for 32
-// rows over 32768 keys of 8 heads, of which the launch over the keys takes 29 (134 MB, 4.6 TB/s) and the merge 8.
+// gave.  Short: a launch and what it reads once, 6 us for 77 tokens.  Few rows over many keys: the memory's latency and the merge, 51 us
+// for 32 rows over 32768 keys of 8 heads, of which the launch over the keys takes 43 (134 MB, 3.1 TB/s; 29 where the 256 MB
+// last-level cache holds them) and the merge 8.5.
 #include "lychee_prompt_device.h"
 
 #include <type_traits>

@@ -33,7 +33,7 @@ int64_t ranges_of(int64_t blocks, int32_t smallest, int32_t n_kv_heads)  // what
 }
 // Whether lengths are possible with which a launch would share its tiles out (lay_line): a longest request against the least that
 // it and the others can have, of equal lengths and, in a cache, with no keys but their own.  (To find out on the device, and a merge
-// with nothing to do, cost 7 us.)
+// with nothing to do, cost 3 us: 17 tokens over 300 4-bit keys take 12.2 under a table for 512, 15.5 for 1024 and more.)
 bool may_share(int32_t batch, int32_t heads, int32_t n_tokens, int64_t max_len, bool packed)
 {
     const float range = (float)heads / (float)(kPromptRows * kPromptSlots), own = 1.f / (2 * kPromptKeys);
@@ -187,7 +187,7 @@ void fill_split(PromptArgs &a, const Grid &w, const CarvedPrompt &c, void *works
     a.one_range = w.ranges > 0 ? 1.0 / (double)w.ranges : 0.0;
     a.by_number = w.tiles < w.ranges;
     a.n_records = a.by_number ? a.n_tiles : a.n_ranges;
-    // (about 1024 workgroups: two that fit a compute unit at a time)
+    // (512 workgroups at least, two a compute unit, if 16 groups of dimensions are enough for that)
     a.merge_split = 1;
     while (a.merge_split < 16 && a.n_records * a.r.n_kv_heads * kWaves * a.merge_split < 512) a.merge_split *= 2;
     a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)kHeadDim));

@@ -4,17 +4,18 @@
 // the gradient of out_r:
 //     dP_rj = g_r . v_j,  delta_r = g_r . out_r,  dS_rj = P_rj (dP_rj - delta_r)
 //     dq_r = c sum_j dS_rj k_j,  dk_j = c sum_r dS_rj q_r,  dv_j = sum_r P_rj g_r,  c = 1 / sqrt(128)
-// Two launches, so that every sum is made by one wavefront in a fixed order and none needs atomics: the first goes over the keys
-// of 128 rows, the second over the rows of 128 keys (all query heads of the KV head, so that nothing is left to add up).
+// Two launches, so that every sum is made in a fixed order and none needs atomics: the first goes over the keys of 128 rows, the second
+// over the rows of 128 keys (all query heads of the KV head).  A wavefront makes a sum alone, or its range's part of one, and a merge
+// adds the parts up, range after range.
 // Scores and weights are made in both: seven products of a pair of tiles where five would do.
 // P and dS are rounded to bf16 for the products that sum them, at most 2^-8 of each with either sign: as much again as the results' own
 // rounding.  delta comes from the rounded out, which is all that the call has of it.
 //
-// What bounds it: the products and the registers.  8192 tokens of 32 heads (8 KV heads), forward and backward: 2.30 ms, of which
-// the forward pass takes 0.52, dq 0.70 (three products: 1.18 PFLOP/s), dk and dv 1.00 (four: 1.10 PFLOP/s) and their merge 0.025.
+// What bounds it: the products and the registers.  8192 tokens of 32 heads (8 KV heads), forward and backward: 2.26 ms, of which
+// the forward pass takes 0.52, dq 0.71 (three products: 1.17 PFLOP/s), dk and dv 1.01 (four: 1.09 PFLOP/s) and their merge 0.026.
 // Sums of 128 keys and a block of scores fill the 256 registers of two wavefronts a unit, so K's rows stay in registers, V's in
 // LDS, and 32 rows come at a time (64 at a time: 2.52 ms in all where 32 took 2.44).  No read of LDS meets a bank twice.
-// Short: four launches, 50 us in all for four sequences of 93 to 311 tokens.
+// Short: four launches, 49 us in all for four sequences of 93 to 311 tokens.
 #include "lychee_prompt_device.h"
 
 namespace lychee {
