@@ -92,6 +92,19 @@ def test_minus_infinity_in_one_of_many_pieces(ctx, there):  # noqa: F811
     assert torch.isnan(q4(ctx, s, p, table, cache, [6000])).all()
 
 
+@pytest.mark.parametrize("new, length, absent", [(20, 20, [0]), (70, 130, [4, 5]), (40, 40, [1]), (3, 300, range(18)), (3, 300, range(19))])
+def test_rows_that_see_no_page_among_others(ctx, new, length, absent):  # noqa: F811
+    """Of a block's rows those before its first page are zero, and the others, whose scores are all -infinity, NaN."""
+    s, p, table, cache = paged_case(91, [new], [length], 2, 1, 16)
+    cache.bytes[:, 3:2048:128] = (cache.bytes[:, 3:2048:128] & 0x0F) | 0xA0
+    table[0, list(absent)] = -1
+    s.q[:, :, 7] = math.inf
+    out = q4(ctx, s, p, table, cache, [length])
+    there = np.nonzero(P.slots_of(table[0], length, 16, p.n_pages) >= 0)[0]
+    sees = torch.from_numpy(length - new + np.arange(new) >= (there[0] if len(there) else length)).to(DEV)
+    assert torch.isnan(out[sees]).all() and (out[~sees] == 0).all()
+
+
 def steep(s, k, low, high):
     """Queries and keys whose scores rise along the keys: low nats for the first, high for the last (rounded to bf16)."""
     root = math.sqrt(128)
