@@ -421,9 +421,9 @@ int lychee_select_scores(lychee_ctx *ctx, const lychee_paged *paged, const float
  *     An infinite value or NaN that it does see reaches its output whatever its weight, one that rounds to zero included: the
  *     output is infinite there, or NaN where it sees a NaN or infinities of both signs.
  *   - Softmax statistics and sums are fp32; weights, and dS in the backward pass, are rounded to bf16 for the matrix units, and
- *     the backward pass has out as it was rounded.  out and dv are 0.0018 to 0.0024 of their norm off, dq and dk 0.0024 to
- *     0.0028, where their own rounding makes 0.0017.  (lychee_q4_decode_attn keeps weights to 2^-17: a single token has the
- *     more exact output there.)
+ *     the backward pass has out as it was rounded.  out and dv are 0.0017 to 0.0024 of their norm off, dq and dk 0.0024 to
+ *     0.0031 (most where sequences are short), where their own rounding makes 0.0017.  (lychee_q4_decode_attn keeps weights to
+ *     2^-17: a single token has the more exact output there.)
  *   - A forward call enqueues one or two kernel launches, a backward call two to four (none for n_tokens = 0).  Calls may be
  *     captured and leave the caller's current device as it was; their launches are not timed by lychee_timing_enable.
  *     Results do not depend on the order in which workgroups run: the same call gives the same bits.
